@@ -444,6 +444,153 @@ pced_status pced_model_generate(pced_ctx* ctx, const void* model, const void* lm
                                 const int32_t* first_tokens, int32_t* tokens_out,
                                 const pced_step_out* last_extra, hipStream_t stream);
 
+/*
+ * Layer-wise calls, for programs that own their projections and run a decoder
+ * layer by layer (Section 3: every expert's pass over the shared tokens). n_tokens
+ * new tokens per sequence go through the layers; their rows are those of
+ * pced_model_prefill: row s * n_tokens + i is token i of sequence s, at position
+ * len_s + i. Per layer
+ *     pced_append   writes the rows' K / V behind the sequence's tokens (rotated)
+ *     pced_attend   lets every row attend to its sequence, itself included
+ * and after the last layer pced_advance makes the rows part of the sequences. Until
+ * then the lengths stay, and the calls may be repeated (with other rows, or for
+ * fewer of them: a verifier may advance by the tokens it accepts). Positions and
+ * lengths are fixed at the call: a captured call replays with those it was captured
+ * with.
+ */
+
+/* Rotation of q and K rows: pairs of the first rot_dim dims of every head are turned
+ * by pos * theta^(-2j/rot_dim), j the pair's number; the angle's cos and sin come from
+ * fp64, the rotation is done in fp32 and rounded once. */
+typedef struct pced_rope {
+  double theta;      /* > 1                                                            */
+  int32_t rot_dim;   /* 0 .. head_dim, even; with halves a multiple of 16 (bf16) or 8 (f32) */
+  int32_t halves;    /* 0: pairs (2j, 2j + 1); 1: pairs (j, j + rot_dim / 2)           */
+} pced_rope;
+
+/* New rows, device, storage type. A row is [n_layers][heads][head_dim]; *_row is the
+ * distance in elements from one row to the next (0: rows follow each other), so that
+ * the three may be parts of one projection's output. Pointers and distances are
+ * multiples of 16 bytes. */
+typedef struct pced_rows {
+  const void* q;     /* [S * n_tokens] rows of [n_layers][Hq][D], or NULL (K / V only) */
+  const void* k;     /* [S * n_tokens] rows of [n_layers][Hkv][D]                      */
+  const void* v;
+  int64_t q_row, k_row, v_row;
+} pced_rows;
+
+/*
+ * Write the new rows of layers [layer, layer + n_layers) into the pool, K rotated, and
+ * the rotated q rows to q_out.
+ *   rope   NULL: no rotation
+ *   q_out  device [S * n_tokens][n_layers][Hq][D], 16-byte aligned; may be rows->q itself
+ *          where its rows follow each other; otherwise it may overlap no input. NULL
+ *          exactly when rows->q is
+ * With summaries bound (pced_bind_summary) and up to date, pages that the rows fill are
+ * summarised. Slots of the pages behind the last row are left as they are.
+ * Errors: STATE (nothing loaded), CAPACITY (pages), INVALID_ARG, HIP.
+ */
+pced_status pced_append(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
+                        const pced_rope* rope, void* q_out, hipStream_t stream);
+
+/* Make n_tokens appended tokens part of every sequence. Host-only. Errors: STATE
+ * (nothing loaded, or a layer got fewer rows since the lengths last changed),
+ * INVALID_ARG (n_tokens < 1). */
+pced_status pced_advance(pced_ctx* ctx, int32_t n_tokens);
+
+/*
+ * Page summaries, for attention that reads part of a cache: per complete page,
+ * layer and kv-head the largest and the smallest value of each key dimension over
+ * the page's 16 keys, in int8 with a power of two as scale, rounded outward (1/32 of
+ * the bf16 cache). pced_summary_bytes: size of the buffer for cfg (0 if invalid).
+ * pced_bind_summary (host-only) gives the context a caller-owned device buffer of
+ * that size, 256-byte aligned, without contents (NULL: none). pced_summarize brings
+ * it up to date with the loaded caches and all appended tokens: call it after
+ * binding, after pced_load_caches, and after steps or prefills made by other calls
+ * than pced_append, which keeps an up-to-date buffer so. Work is enqueued for pages
+ * not covered yet only.
+ * Errors: INVALID_ARG (misaligned), STATE (nothing loaded, none bound), HIP.
+ */
+size_t pced_summary_bytes(const pced_config* cfg);
+pced_status pced_bind_summary(pced_ctx* ctx, void* summary);
+pced_status pced_summarize(pced_ctx* ctx, hipStream_t stream);
+
+/* Pages that a row attends to: the sequence's first n_first and last n_last pages (the
+ * row's own among them), and of those between the ones that may hold the keys of the
+ * highest scores, n_pages in all; every page where there are no more than n_pages.
+ * The measure of a page, per row and kv-head: sum_d (w+_d max_d + w-_d min_d) over its
+ * summary, with w+ / w- the sums over the kv-head's q-heads of max(q, 0) / min(q, 0),
+ * rounded to int8 with a power of two as scale: an upper bound, up to that rounding,
+ * on sum_g q_g . k for the page's keys. It is computed exactly, so equal inputs give
+ * equal pages; of equal measures the lower page comes first. */
+typedef struct pced_select {
+  int32_t n_pages;   /* >= n_first + n_last */
+  int32_t n_first;   /* >= 0                */
+  int32_t n_last;    /* >= 1                */
+} pced_select;
+
+/*
+ * Attention of the new tokens, after pced_append of the same layers: row (s, i)
+ * attends to tokens 0 .. len_s + i of its sequence, as far as they are in its pages
+ * (grouped-query attention, scale 1/sqrt(head_dim)); sums and softmax in fp32.
+ *   q          device [S * n_tokens][n_layers][Hq][D], storage type, 16-byte aligned
+ *   sel        pages to attend to, or NULL: all
+ *   x_out      device [S * n_tokens][n_layers][Hq * D], storage type, 16-byte aligned;
+ *              may not overlap q
+ *   pages_out  optional device [S * n_tokens][n_layers][Hkv][n_pages]: the pages
+ *              (numbers within the sequence) of each row and kv-head, ascending, -1
+ *              behind the last (needs sel)
+ * Errors: STATE (nothing loaded; fewer rows appended to a layer; summaries wanted but
+ * not bound or not up to date), INVALID_ARG, CAPACITY (pages), HIP.
+ */
+pced_status pced_attend(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q,
+                        const pced_select* sel, void* x_out, int32_t* pages_out, hipStream_t stream);
+
+/*
+ * Adjustments of a query's logits before a token is chosen. All pointers are device
+ * memory, read when the call runs. For query b and token v, with h the number of
+ * history entries that are v:
+ *     h > 0:  s = s > 0 ? s / repetition : s * repetition;
+ *             s = s - frequency * h - presence
+ *     s = s + bias(v)                the last of the query's entries that name v
+ *     s = -inf                       where the mask's bit of v is 0
+ * in fp32, in this order. Entries outside [0, V) count for nothing (-1 may fill a
+ * padded batch); a query's entries are those from off[b] to off[b + 1], cut to the
+ * array's size. Members that are NULL adjust nothing.
+ */
+typedef struct pced_adjust {
+  const int32_t* history;      /* [n_history] tokens                                  */
+  const int32_t* history_off;  /* [B + 1]                                             */
+  const float* repetition;     /* [B] > 0                                             */
+  const float* presence;       /* [B]                                                 */
+  const float* frequency;      /* [B]                                                 */
+  const int32_t* bias_token;   /* [n_bias]                                            */
+  const float* bias_value;     /* [n_bias]                                            */
+  const int32_t* bias_off;     /* [B + 1]                                             */
+  const uint32_t* mask;        /* [B] rows of mask_row words: bit v % 32 of word v / 32 */
+  int64_t mask_row;            /* 0: ceil(V / 32)                                     */
+  int32_t n_history, n_bias;
+} pced_adjust;
+
+/*
+ * Stage entry: out[s][v] = the adjusted logits of every sequence of the loaded batch
+ * (each sequence has its query's adjustments). logits, out: device [S][V] fp32, rows
+ * in load order; out may be logits itself, else they may not overlap.
+ * Errors: STATE (nothing loaded), INVALID_ARG, HIP.
+ */
+pced_status pced_adjust_logits(pced_ctx* ctx, const float* logits, const pced_adjust* adjust, float* out,
+                               hipStream_t stream);
+
+/*
+ * Stage entry: pced_fuse with every sequence's logits adjusted (not stored). Dynamic
+ * beta, when refreshed, comes from the logits as given. A token that the mask closes,
+ * or whose score is -inf or NaN for every expert, is never chosen and is not top2
+ * either; a query without any other token gets token -1, winner 0 and scores -inf.
+ * Errors: as pced_fuse; UNSUPPORTED for aggregations other than PCED_AGG_MAX.
+ */
+pced_status pced_fuse_adjusted(pced_ctx* ctx, const float* logits, int32_t refresh_beta, const pced_adjust* adjust,
+                               int32_t* tokens_out, const pced_step_out* extra, hipStream_t stream);
+
 /* Kernel timing with HIP events attached to each kernel dispatch (start when
  * the kernel begins, stop when it completes). Classes: */
 enum {

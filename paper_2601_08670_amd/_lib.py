@@ -25,7 +25,8 @@ EXPORTED = ("pced_pool_bytes", "pced_lm_head_bytes", "pced_pack_lm_head", "pced_
             "pced_get_lengths", "pced_profile_enable", "pced_profile_read", "pced_relevance",
             "pced_model_bytes", "pced_pack_model_layer", "pced_pack_model_globals", "pced_model_prefill",
             "pced_model_step", "pced_model_generate", "pced_read_cache", "pced_lmhead_noalloc",
-            "pced_stream_read")
+            "pced_stream_read", "pced_append", "pced_advance", "pced_summary_bytes", "pced_bind_summary",
+            "pced_summarize", "pced_attend", "pced_adjust_logits", "pced_fuse_adjusted")
 
 
 class PcedError(RuntimeError):
@@ -52,6 +53,26 @@ STEP_OUT_FIELDS = tuple(n for n, _ in pced_step_out._fields_)
 
 class pced_synth(ctypes.Structure):
     _fields_ = [("seed", ctypes.c_uint64), ("first_token", ctypes.c_int32)]
+
+
+class pced_rope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("rot_dim", ctypes.c_int32), ("halves", ctypes.c_int32)]
+
+
+class pced_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_row", ctypes.c_int64), ("k_row", ctypes.c_int64), ("v_row", ctypes.c_int64)]
+
+
+class pced_select(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("n_first", ctypes.c_int32), ("n_last", ctypes.c_int32)]
+
+
+class pced_adjust(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_off", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("bias_token", ctypes.c_void_p),
+                ("bias_value", ctypes.c_void_p), ("bias_off", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_row", ctypes.c_int64), ("n_history", ctypes.c_int32), ("n_bias", ctypes.c_int32)]
 
 
 class pced_profile(ctypes.Structure):
@@ -98,6 +119,14 @@ def load_library() -> ctypes.CDLL:
         "pced_read_cache": (I, [P, I, I, I, I, P, P, V]),
         "pced_lmhead_noalloc": (I, [ctypes.POINTER(pced_config), P, I, P, P, V]),
         "pced_stream_read": (I, [P, ctypes.c_size_t, P, V]),
+        "pced_append": (I, [P, I, I, I, ctypes.POINTER(pced_rows), ctypes.POINTER(pced_rope), P, V]),
+        "pced_advance": (I, [P, I]),
+        "pced_summary_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config)]),
+        "pced_bind_summary": (I, [P, P]),
+        "pced_summarize": (I, [P, V]),
+        "pced_attend": (I, [P, I, I, I, P, ctypes.POINTER(pced_select), P, P, V]),
+        "pced_adjust_logits": (I, [P, P, ctypes.POINTER(pced_adjust), P, V]),
+        "pced_fuse_adjusted": (I, [P, P, I, ctypes.POINTER(pced_adjust), P, ctypes.POINTER(pced_step_out), V]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -151,6 +180,10 @@ def pced_lmhead_noalloc(cfg: pced_config, x, n_rows, lm_head, logits, stream=Non
 def pced_stream_read(src, nbytes, xor_out, stream=None):
     """XOR of the 32-bit words of nbytes of src (device), read with streaming loads."""
     _check(load_library().pced_stream_read(src.data_ptr(), int(nbytes), xor_out.data_ptr(), _stream(stream)))
+
+
+def pced_summary_bytes(cfg: pced_config) -> int:
+    return load_library().pced_summary_bytes(ctypes.byref(cfg))
 
 
 def pced_model_bytes(cfg: pced_config) -> int:
@@ -310,6 +343,35 @@ class Context:
     def pced_read_cache(self, seq, layer, start, count, k_out, v_out, stream=None):
         _check(self.lib.pced_read_cache(self.handle, int(seq), int(layer), int(start), int(count), k_out.data_ptr(),
                                         v_out.data_ptr(), _stream(stream)))
+
+    def pced_append(self, layer, n_layers, n_tokens, rows: pced_rows, rope: Optional[pced_rope], q_out, stream=None):
+        _check(self.lib.pced_append(self.handle, int(layer), int(n_layers), int(n_tokens), ctypes.byref(rows),
+                                    None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream)))
+
+    def pced_advance(self, n_tokens):
+        _check(self.lib.pced_advance(self.handle, int(n_tokens)))
+
+    def pced_bind_summary(self, summary):
+        _check(self.lib.pced_bind_summary(self.handle, _ptr(summary)))
+        self._summary = summary
+
+    def pced_summarize(self, stream=None):
+        _check(self.lib.pced_summarize(self.handle, _stream(stream)))
+
+    def pced_attend(self, layer, n_layers, n_tokens, q, sel: Optional[pced_select], x_out, pages_out=None, stream=None):
+        _check(self.lib.pced_attend(self.handle, int(layer), int(n_layers), int(n_tokens), _ptr(q),
+                                    None if sel is None else ctypes.byref(sel), _ptr(x_out), _ptr(pages_out),
+                                    _stream(stream)))
+
+    def pced_adjust_logits(self, logits, adjust: pced_adjust, out, stream=None):
+        _check(self.lib.pced_adjust_logits(self.handle, _ptr(logits), ctypes.byref(adjust), _ptr(out),
+                                           _stream(stream)))
+
+    def pced_fuse_adjusted(self, logits, refresh_beta, adjust: pced_adjust, tokens_out, extra: Optional[dict] = None,
+                           stream=None):
+        so = _step_out(extra)
+        _check(self.lib.pced_fuse_adjusted(self.handle, _ptr(logits), int(refresh_beta), ctypes.byref(adjust),
+                                           _ptr(tokens_out), so[0] if so else None, _stream(stream)))
 
     def pced_get_lengths(self, n_seqs):
         out = (ctypes.c_int32 * n_seqs)()

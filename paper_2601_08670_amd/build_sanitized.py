@@ -8,7 +8,7 @@ from __future__ import annotations
 import os
 import subprocess
 
-from .build import COMMON, CSRC, HIPCC, LINK, _run
+from .build import COMMON, CSRC, HIPCC, LINK, SOURCES, _run
 
 # each host-only sanitizer flag follows its own -Xarch_host (device code is not instrumented)
 SANITIZE = ("-Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined "
@@ -18,7 +18,7 @@ SANITIZE = ("-Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined "
 def build(out_dir: str, verbose: bool = False) -> str:
     os.makedirs(out_dir, exist_ok=True)
     objs = []
-    for src in ("pced_kernels.hip", "pced_api.cpp"):
+    for src in SOURCES:
         obj = os.path.join(out_dir, src.replace(".", "_") + ".san.o")
         cmd = [HIPCC, *COMMON, "-g", *SANITIZE, "-c", os.path.join(CSRC, src), "-o", obj]
         if src.endswith(".cpp"):

@@ -1,10 +1,7 @@
 // Host side of libpced: argument validation, workspace carving, the host mirror
 // of sequence lengths and page tables, and the launch sequence of a PCED decode
 // step (arXiv 2601.08670, Section 3). See include/pced.h for the contract.
-#include "pced.h"
-
-#include <hip/hip_runtime.h>
-#include <rocblas/rocblas.h>
+#include "pced_host.h"
 
 #include <algorithm>
 #include <cmath>
@@ -14,14 +11,14 @@
 #include <string>
 #include <vector>
 
-#include "pced_internal.h"
-
 using namespace pced;
 
 namespace {
 
 thread_local std::string g_err;
 
+}  // namespace
+namespace pced {
 pced_status fail(pced_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -31,17 +28,6 @@ pced_status fail(pced_status st, const char* fmt, ...) {
   g_err = buf;
   return st;
 }
-
-#define HIP_OK(expr)                                                               \
-  do {                                                                             \
-    hipError_t e_ = (expr);                                                        \
-    if (e_ != hipSuccess) return fail(PCED_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-size_t esize_of(const pced_config& c) { return c.dtype == PCED_BF16 ? 2 : 4; }
-int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
 bool cfg_valid(const pced_config* c, std::string* why) {
   auto bad = [&](const char* m) { if (why) *why = m; return false; };
@@ -74,26 +60,11 @@ bool cfg_valid(const pced_config* c, std::string* why) {
   if ((double)c->max_seqs * c->vocab > 2147483647.0) return bad("max_seqs * vocab exceeds 2^31");
   return true;
 }
+}  // namespace pced
+namespace {
 
 constexpr size_t kLoadStage = (size_t)64 << 20;  // staging of host-memory caches, at most
 constexpr size_t kPartBytes = (size_t)128 << 20;  // attention partial states of several layers, at most
-
-struct Layout {
-  size_t len0, page_table, seq_query, query_seq0, query_exp0, exp_seq, exp_query, prior, logw, beta_fixed,
-      load_items, src_k, src_v, meta_end;
-  size_t chunk_info, seg, nparts, work_pages, prev_tok, beta, part_acc, part_ml, x, logits,
-      rho, x_packed, fuse_part, lse_part, jsd_part, syn_q, syn_k, syn_v, dec_h, dec_a, dec_act, dec_ss, dec_rho, dec_part,
-      rope, pf_len0, pf_pt, pf_tok, pf_glen0, pf_gpt, pf_nparts, pf_rho, pf_h, pf_a, pf_act, pf_ss, pf_q, pf_x, pf_part_acc, pf_part_ml, pf_proj,
-      stage_bytes, total;
-  int packed_rows;      // rows x_packed holds
-  int pf_rows;          // rows of one prefill chunk (sequences x suffix tokens)
-  size_t pf_proj_cols;  // slices x columns per row of the prefill projection partials
-  size_t pf_proj_elems; // floats of that buffer
-  int rows_pad, nchunk, max_work;
-  size_t seg_slots;     // segment descriptors of the attention plan
-  size_t part_slots;
-  size_t part_cols;  // slices x columns one row of the projection partial buffer holds
-};
 
 Layout make_layout(const pced_config& c) {
   Layout L{};
@@ -145,7 +116,8 @@ Layout make_layout(const pced_config& c) {
   // least one page of one layer.
   const size_t page_bytes = (size_t)kPage * c.n_kv_heads * c.head_dim * es;
   L.stage_bytes = align_up(2 * std::max(page_bytes, std::min(kLoadStage / 2, page_bytes * c.max_pages_per_seq * c.n_layers)));
-  L.part_acc = take(std::max(L.part_slots * G * c.head_dim * 4, L.stage_bytes));
+  L.part_acc_bytes = align_up(std::max(L.part_slots * G * c.head_dim * 4, L.stage_bytes));
+  L.part_acc = take(L.part_acc_bytes);
   L.part_ml = take(2 * L.part_slots * G * 2 * 4);
   L.x = take((size_t)L.rows_pad * c.hidden * es);
   L.logits = take(S * c.vocab * 4);
@@ -208,83 +180,6 @@ Layout make_layout(const pced_config& c) {
   L.total = o;
   return L;
 }
-
-struct ProfRec {
-  int cls;
-  hipEvent_t a, b;
-  double bytes, flops;
-};
-
-}  // namespace
-
-struct pced_ctx {
-  pced_config cfg;
-  Layout lay;
-  char* ws;
-  bool bf16;
-  int G;
-  // host mirror of the loaded batch
-  bool loaded = false;
-  int B = 0, S = 0, NE = 0;
-  std::vector<int32_t> n_experts, seq_off, exp_off, len, page_table;
-  bool dynamic_beta = false, beta_frozen = false;
-  LmWidePlan head_groups;  // the fused LM head's row groups for more than 288 rows
-  int t = 0;
-  void* kpool = nullptr;
-  void* vpool = nullptr;
-  std::vector<char> staging;
-  int num_cus = 0;
-  int attn_waves_per_cu = 8;
-  // profiling
-  bool prof = false;
-  std::vector<ProfRec> recs;
-  std::vector<hipEvent_t> ev_free;
-  rocblas_handle blas = nullptr;  // created at the first many-row projection
-  pced_profile totals{};
-
-  template <class T> T* at(size_t off) { return reinterpret_cast<T*>(ws + off); }
-};
-
-namespace {
-
-// Start/stop events of one kernel class launch when profiling is on. They are
-// handed to the launcher, which attaches them to the dispatch itself
-// (hipExtLaunchKernelGGL), so they time the kernels and not the queue.
-struct ProfScope {
-  pced_ctx* c;
-  ProfRec rec;
-  Timing tm;
-  bool on;
-  ProfScope(pced_ctx* ctx, int cls, double bytes, double flops) : c(ctx), on(ctx->prof) {
-    if (!on) return;
-    rec.cls = cls;
-    rec.bytes = bytes;
-    rec.flops = flops;
-    rec.a = take();
-    rec.b = take();
-    if (!rec.a || !rec.b) {  // no events to be had: this launch goes untimed
-      if (rec.a) c->ev_free.push_back(rec.a);
-      if (rec.b) c->ev_free.push_back(rec.b);
-      on = false;
-      return;
-    }
-    tm.start = rec.a;
-    tm.stop = rec.b;
-  }
-  const Timing* timing() const { return on ? &tm : nullptr; }
-  hipEvent_t take() {
-    if (!c->ev_free.empty()) { hipEvent_t e = c->ev_free.back(); c->ev_free.pop_back(); return e; }
-    hipEvent_t e = nullptr;
-    if (hipEventCreateWithFlags(&e, hipEventDisableSystemFence) != hipSuccess) {
-      (void)hipGetLastError();
-      return nullptr;
-    }
-    return e;
-  }
-  ~ProfScope() {
-    if (on) c->recs.push_back(rec);
-  }
-};
 
 int device_cus() {
   int dev = 0, n = 0;
@@ -438,10 +333,22 @@ pced_status load_from_host(pced_ctx* c, LoadArgs a, int s, int len, const char* 
   return r;
 }
 
+}  // namespace
+namespace pced {
 pced_status check_ctx(const pced_ctx* c, bool need_loaded) {
   if (!c) return fail(PCED_ERR_INVALID_ARG, "ctx is NULL");
   if (need_loaded && !c->loaded) return fail(PCED_ERR_STATE, "no batch loaded (call pced_load_caches first)");
   return PCED_OK;
+}
+
+void advance(pced_ctx* c, int n, bool by_rows) {
+  for (int s = 0; s < c->S; ++s) c->len[s] += n;
+  c->t += n;
+  for (int l = 0; l < c->cfg.n_layers; ++l) {
+    const bool covered = by_rows && c->behind[l] == 0 && c->ahead[l] >= n;
+    if (!covered && c->behind[l] != kNotCovered) c->behind[l] += n;
+    c->ahead[l] = c->appended[l] = 0;
+  }
 }
 
 FuseArgs fuse_args(pced_ctx* c, const float* logits, int32_t* tokens_out, int tok_stride, const pced_step_out* extra,
@@ -469,6 +376,36 @@ FuseArgs fuse_args(pced_ctx* c, const float* logits, int32_t* tokens_out, int to
   f.tok_stride = tok_stride;
   return f;
 }
+}  // namespace pced
+namespace {
+
+BetaArgs beta_args(pced_ctx* c, const float* logits) {
+  BetaArgs b{};
+  b.logits = logits;
+  b.query_seq0 = c->at<int32_t>(c->lay.query_seq0);
+  b.exp_seq = c->at<int32_t>(c->lay.exp_seq);
+  b.exp_query = c->at<int32_t>(c->lay.exp_query);
+  b.lse_part = c->at<float>(c->lay.lse_part);
+  b.jsd_part = c->at<float>(c->lay.jsd_part);
+  b.beta = c->at<float>(c->lay.beta);
+  b.V = c->cfg.vocab;
+  b.nchunk = c->lay.nchunk;
+  b.query_exp0 = c->at<int32_t>(c->lay.query_exp0);
+  return b;
+}
+
+}  // namespace
+namespace pced {
+pced_status run_beta(pced_ctx* c, const float* logits, hipStream_t st) {
+  const BetaArgs b = beta_args(c, logits);
+  ProfScope ps(c, PCED_PROF_BETA, (double)(c->S + 2.0 * c->NE) * c->cfg.vocab * 4, 0);
+  HIP_OK(launch_beta(b, c->S, c->NE, true, st, ps.timing()));
+  if (c->cfg.beta_scalar) HIP_OK(launch_beta_mean(b, c->B, st));
+  c->beta_frozen = true;
+  return PCED_OK;
+}
+}  // namespace pced
+namespace {
 
 // Launch the beta (first step) and fuse kernels over `logits`.
 pced_status run_fuse(pced_ctx* c, const float* logits, bool refresh_beta, int32_t* tokens_out,
@@ -479,17 +416,7 @@ pced_status run_fuse(pced_ctx* c, const float* logits, bool refresh_beta, int32_
                                                     : fuse_slice(cfg.vocab, c->B, c->num_cus);
   FuseArgs f = fuse_args(c, logits, tokens_out, tok_stride, extra, ceil_div(cfg.vocab, slice));
   if (c->dynamic_beta && refresh_beta) {
-    BetaArgs b{};
-    b.logits = logits;
-    b.query_seq0 = c->at<int32_t>(c->lay.query_seq0);
-    b.exp_seq = c->at<int32_t>(c->lay.exp_seq);
-    b.exp_query = c->at<int32_t>(c->lay.exp_query);
-    b.lse_part = c->at<float>(c->lay.lse_part);
-    b.jsd_part = c->at<float>(c->lay.jsd_part);
-    b.beta = c->at<float>(c->lay.beta);
-    b.V = cfg.vocab;
-    b.nchunk = c->lay.nchunk;
-    b.query_exp0 = c->at<int32_t>(c->lay.query_exp0);
+    const BetaArgs b = beta_args(c, logits);
     ProfScope ps(c, PCED_PROF_BETA, (double)(c->S + 2.0 * c->NE) * cfg.vocab * 4, 0);
     // the launch that uses beta sums its partials itself, unless their mean over a query is wanted,
     // a query has more experts than the fuse holds, or the fuse's work-groups, each of which sums,
@@ -617,6 +544,8 @@ pced_status run_head(pced_ctx* c, const void* x, const float* rho_in, const void
   return run_fuse(c, logits, refresh, tokens_out, tok_stride, extra, st);
 }
 
+}  // namespace
+namespace pced {
 pced_status check_room(const pced_ctx* c, int n_tokens) {
   const int P = c->cfg.max_pages_per_seq;
   for (int s = 0; s < c->S; ++s) {
@@ -628,6 +557,8 @@ pced_status check_room(const pced_ctx* c, int n_tokens) {
   }
   return PCED_OK;
 }
+}  // namespace pced
+namespace {
 
 // Byte offsets of the decoder-stack weights inside the packed model buffer:
 // per layer the two norm weights and the packed QKV (q, k, v tiles
@@ -1102,8 +1033,7 @@ pced_status run_model_step(pced_ctx* c, const void* model, const void* w, const 
   if (extra && extra->hidden)
     HIP_OK(hipMemcpyAsync(extra->hidden, c->at<float>(c->lay.dec_h), (size_t)c->S * cfg.hidden * 4,
                           hipMemcpyDeviceToDevice, st));
-  for (int s = 0; s < c->S; ++s) c->len[s] += 1;
-  c->t += 1;
+  advance(c, 1, false);
   return PCED_OK;
 }
 
@@ -1214,8 +1144,7 @@ pced_status run_step(pced_ctx* c, const void* q, const void* k_new, const void* 
 
   const pced_status r = run_head(c, at.x_out, nullptr, w, tokens_out, tok_stride, extra, st);
   if (r != PCED_OK) return r;
-  for (int s = 0; s < c->S; ++s) c->len[s] += 1;
-  c->t += 1;
+  advance(c, 1, false);
   return PCED_OK;
 }
 
@@ -1269,6 +1198,9 @@ pced_status pced_create(const pced_config* cfg, void* d_workspace, size_t ws_byt
   c->ws = (char*)d_workspace;
   c->bf16 = cfg->dtype == PCED_BF16;
   c->G = cfg->n_q_heads / cfg->n_kv_heads;
+  c->appended.assign(cfg->n_layers, 0);
+  c->ahead.assign(cfg->n_layers, 0);
+  c->behind.assign(cfg->n_layers, kNotCovered);
   *out = c;
   return PCED_OK;
 }
@@ -1368,6 +1300,9 @@ pced_status pced_load_caches(pced_ctx* c, int32_t n_queries, const int32_t* n_ex
   }
   c->len.assign(cache_len, cache_len + S);
   c->page_table = pt;
+  std::fill(c->appended.begin(), c->appended.end(), 0);
+  std::fill(c->ahead.begin(), c->ahead.end(), 0);
+  std::fill(c->behind.begin(), c->behind.end(), kNotCovered);
   c->head_groups = c->bf16 ? lmhead_wide_plan_queries(c->seq_off.data(), n_queries, cfg.vocab, cfg.hidden,
                                                       c->lay.packed_rows)
                            : LmWidePlan{};
@@ -1600,8 +1535,7 @@ pced_status pced_model_prefill(pced_ctx* c, const void* model, int32_t n_tokens,
     const int n = std::min(T, n_tokens - i0);
     r = run_prefill_chunk(c, (const char*)model, tokens, n_tokens, i0, n, st);
     if (r != PCED_OK) return r;
-    for (int s = 0; s < c->S; ++s) c->len[s] += n;
-    c->t += n;
+    advance(c, n, false);
   }
   return PCED_OK;
 }

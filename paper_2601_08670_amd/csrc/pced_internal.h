@@ -172,8 +172,28 @@ struct FuseArgs {
   const float* jsd_part;
   float* beta_out;
   int nchunk;
+  int none_token;           // token -1 where no expert scores any token
   int32_t inl_seq0[kFuseInlineQueries + 1];  // query_seq0 / query_exp0 of the first queries
   int32_t inl_exp0[kFuseInlineQueries + 1];
+};
+
+// Per-query adjustments of logits (see pced_adjust), and the rows of k_adjust.
+struct AdjustArgs {
+  const int32_t* history;   // optional [n_history], history_off [B+1]
+  const int32_t* history_off;
+  const float* repetition;  // optional [B] each
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_token;// optional [n_bias], bias_off [B+1]
+  const float* bias_value;
+  const int32_t* bias_off;
+  const uint32_t* mask;     // optional [B] rows of mask_row words
+  int64_t mask_row;
+  int n_history, n_bias, V;
+  const float* logits;      // [S][V]
+  float* out;               // [S][V]
+  const int32_t* query_seq0;// [B+1]
+  int rows_per_block;       // (set by launch_adjust)
 };
 
 // MoE / PoE aggregation (the alternatives to Eq. 3's max): per-expert
@@ -300,6 +320,64 @@ struct ReadCacheArgs {
   int seq, layer, start, count, n_kv_heads, head_dim, max_pages, maxpps, bf16;
 };
 
+constexpr int kSumExp = 64;        // page summaries: scales are 2^-kSumExp .. 2^kSumExp
+constexpr int kScorePages = 256;   // pages per work-group of the page scores
+constexpr int kAttendTokens = 16;  // new tokens of a sequence that are scored together, at most
+inline int summary_row(int head_dim) { return (2 * head_dim + 63) / 64 * 64; }  // bytes of a page's codes
+
+// New rows of every sequence into the paged pool, K and q rotated (see pced_append).
+struct AppendRowsArgs {
+  const void* q;            // optional [S * n_tokens] rows of [n_layers][Hq][D], q_row elements apart
+  const void* k;            // [S * n_tokens] rows of [n_layers][Hkv][D]
+  const void* v;
+  void* q_out;              // [S * n_tokens][n_layers][Hq][D]
+  int64_t q_row, k_row, v_row;
+  void* kpool;
+  void* vpool;
+  const int32_t* len0;
+  const int32_t* page_table;
+  int8_t* codes;            // optional page summaries [L][Hkv][max_pages][sum_row] and their scales
+  float* scale;             // [L][Hkv][max_pages]
+  int n_seqs, n_tokens, layer0, n_layers, n_q_heads, n_kv_heads, head_dim, max_pages, maxpps, t, sum_row;
+  int slots;                // pages that a sequence's rows touch, at most
+  int rot_dim, halves;
+  double log2_theta;
+};
+// Summaries of the complete pages of every sequence from token len - behind on, all layers.
+struct SummaryArgs {
+  const void* kpool;
+  const int32_t* len0;
+  const int32_t* page_table;
+  int8_t* codes;
+  float* scale;
+  int n_seqs, n_layers, n_kv_heads, head_dim, max_pages, maxpps, t, sum_row, behind;
+  int span;                 // pages of a sequence, at most
+};
+// Attention of new tokens over chosen pages (see pced_attend). A launch takes
+// n_groups groups of gt tokens from group0 on (seq_groups of them per sequence) and
+// launch_layers layers from `layer` on, of a call for n_layers layers from layer0 on.
+struct AttendArgs {
+  const void* q;            // [S * n_tokens][n_layers][Hq][D]
+  const void* kpool;
+  const void* vpool;
+  const int8_t* codes;
+  const float* scale;
+  const int32_t* len0;
+  const int32_t* page_table;
+  float* scores;            // [item][score_row] bounds of the pages
+  int32_t* list;            // [item][n_pages] chosen pages, unless the caller wants them:
+  int32_t* pages_out;       // optional [S * n_tokens][n_layers][Hkv][n_pages]
+  float* part_acc;          // [item][parts][G][D]
+  float* part_ml;           // [item][parts][G][2]
+  void* x_out;              // [S * n_tokens][n_layers][Hq][D]
+  int t, n_tokens, gt, seq_groups, group0, n_groups, layer0, n_layers, layer, launch_layers;
+  int n_q_heads, n_kv_heads, group, head_dim, max_pages, maxpps, sum_row, bf16;
+  int n_pages, first, last;
+  int score_row, chunks;    // pages of a score row (whole 16s); blocks of kScorePages that cover them
+  int parts, part_pages;    // parts of an item's pages, and pages per part
+  float scale_log2;         // log2(e) / sqrt(D)
+};
+
 // Optional timing events attached to the first / last dispatch of a launcher.
 struct Timing {
   hipEvent_t start = nullptr;
@@ -321,6 +399,11 @@ hipError_t launch_beta(const BetaArgs& a, int n_seqs, int n_exp, bool sums, hipS
 // k_fuse (timed by tm) then the per-query merge k_fuse_final (timed by tm_merge)
 hipError_t launch_fuse(const FuseArgs& a, int n_queries, hipStream_t st, const Timing* tm = nullptr,
                        const Timing* tm_merge = nullptr);
+// k_fuse_adjusted (a.nblk = adjusted_slices(V)) then k_fuse_final
+int adjusted_slices(int V);
+hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st,
+                                const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
+hipError_t launch_adjust(const AdjustArgs& a, int n_queries, int max_rows, int num_cus, hipStream_t st);
 // vocabulary tokens per work-group of the stand-alone fuse (1024, or 512 for few queries)
 int fuse_slice(int V, int n_queries, int num_cus);
 // vocabulary tokens per work-group of the MoE / PoE aggregation (kAggSlice, or 4 kAggSlice for many
@@ -361,6 +444,11 @@ constexpr size_t kNoAllocScratchBytes = (size_t)4 << 20;
 hipError_t noalloc_scratch(void** out);
 hipError_t launch_rho(const float* ss, int parts, int ld, int M, float inv_dim, float eps, float* rho,
                       hipStream_t st);
+hipError_t launch_append_rows(const AppendRowsArgs& a, bool bf16, hipStream_t st, const Timing* tm = nullptr);
+hipError_t launch_summarize(const SummaryArgs& a, bool bf16, hipStream_t st);
+// page bounds (score) and the lists of chosen pages
+hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, const Timing* tm = nullptr);
+hipError_t launch_attend(const AttendArgs& a, hipStream_t st, const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
 // RoPE table of GemmArgs::rope for positions 0 .. positions - 1, in fp64 rounded to fp32
 hipError_t launch_rope_table(float2* out, int positions, int head_dim, double log2_theta, hipStream_t st);
 

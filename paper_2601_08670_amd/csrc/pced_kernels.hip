@@ -12,7 +12,6 @@
 //     k = tokens 4*(l/16)..+3.
 //   f32 tiles are row-major [t][d].
 // Every wave load of a page is therefore a contiguous 1 KiB.
-#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -21,49 +20,10 @@
 #include <type_traits>
 #include <utility>
 
-#include "pced_internal.h"
+#include "pced_device.h"
 
 namespace pced {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));  // at any float's address
-
-constexpr float kNegInf = -INFINITY;
-
-__device__ __forceinline__ float bf2f(uint32_t b) { return __uint_as_float(b << 16); }
-
-// round-to-nearest-even float -> bf16 bits (finite inputs)
-__device__ __forceinline__ uint32_t f2bf(float f) {
-  uint32_t u = __float_as_uint(f);
-  u += 0x7FFFu + ((u >> 16) & 1u);
-  return u >> 16;
-}
-
-__device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
-
-
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
-// 16-byte load of data a launch reads once (KV pages, LM-head and projection
-// weights in a decode step): with STREAM it carries the non-temporal hint and
-// streams through the caches without displacing what is reused (partial
-// states, outputs, q and x rows). Launches that read the same bytes several
-// times (the prefill's row groups and virtual rows, the LM head's row groups)
-// use plain loads, so that the repeats hit the caches.
-template <bool STREAM>
-__device__ __forceinline__ uint4 ld_w(const uint4* p) {
-  if constexpr (STREAM) {
-    const u32x4 v = __builtin_nontemporal_load((const u32x4*)p);
-    return make_uint4(v.x, v.y, v.z, v.w);
-  } else {
-    return *p;
-  }
-}
 
 // ------------------------------------------------------------------ utilities
 
@@ -109,9 +69,6 @@ __device__ __forceinline__ UnitPos kunit_pos(int n, int D) {
   const int upt = 2 * D, u = n % upt;
   return UnitPos{n / upt, u & 15, 32 * (u >> 6) + 8 * ((u >> 4) & 3)};
 }
-// element e (of 8) of a 16-byte row piece
-__device__ __forceinline__ uint32_t el16(const u32x4& v, int e) { return (v[e >> 1] >> (16 * (e & 1))) & 0xFFFFu; }
-
 // This wave's LDS accesses so far are complete and ordered before the next ones
 // (other lanes' data is read next).
 __device__ __forceinline__ void wave_lds_sync() {
@@ -2136,7 +2093,8 @@ __device__ __forceinline__ float4 load_tok4_any(const float* row, int v0, int V)
                      o == 0 ? t[2] : t[3], t[3]);
 }
 
-__device__ __forceinline__ void fuse_write_outputs(const FuseArgs& a, int b, const Top2& r) {
+__device__ __forceinline__ void fuse_write_outputs(const FuseArgs& a, int b, Top2 r) {
+  if (a.none_token && r.k1 == 0) r.i1 = -1;  // every token is closed
   a.tokens_out[(size_t)b * a.tok_stride] = r.i1;
   a.prev_tok[b] = r.i1;
   if (a.winner) a.winner[b] = r.k1;
@@ -2260,6 +2218,202 @@ __global__ __launch_bounds__(256) void k_fuse(FuseArgs a) {
       if (vw > v) { v = vw; k = sk[w][t]; }
     }
     if (vb + t < a.V) cand = merge(cand, Top2{v, vb + t, k, kNegInf, 0x7FFFFFFF});
+  }
+  cand = wave_top2(cand);
+  if (lane == 0) swave[wave] = cand;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    Top2 r = swave[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) r = merge(r, swave[w]);
+    float* p = a.part + ((size_t)b * a.nblk + blockIdx.x) * 5;
+    p[0] = r.v1; p[1] = __int_as_float(r.i1); p[2] = __int_as_float(r.k1);
+    p[3] = r.v2; p[4] = __int_as_float(r.i2);
+  }
+}
+
+// Adjusted logits. For a query's token v, with h = how often v occurs in the query's
+// history:  s -> s / r (s > 0) or s r (else), then (s - f h) - p, where h > 0;
+// then s + bias(v) (the last entry that names v); then -inf where the mask's bit is
+// 0. Every operation is one fp32 operation, in this order, not contracted.
+//
+// A block takes the SW tokens of a slice for its rows: it reads the query's lists
+// whole (they are short beside the rows, and cached) and keeps what falls into the
+// slice in LDS: counts by integer atomics, the last bias entry as a maximum of
+// places, so that the order of the atomics leaves no trace. A thread then holds its
+// tokens' adjustments in registers for all of its rows. Entries that name no token
+// of the vocabulary count for nothing, and list bounds are cut to the lists' sizes.
+template <int SW>
+struct AdjustLds {
+  int cnt[SW];
+  int bias[SW];
+};
+template <int SW>
+__device__ __forceinline__ void adjust_slice(const AdjustArgs& a, int b, int vb, AdjustLds<SW>& L) {
+  for (int i = threadIdx.x; i < SW; i += 256) L.cnt[i] = L.bias[i] = 0;
+  __syncthreads();
+  if (a.history) {
+    const int e1 = min(a.history_off[b + 1], a.n_history);
+    for (int e = max(a.history_off[b], 0) + threadIdx.x; e < e1; e += 256) {
+      const int v = a.history[e];
+      if (v >= vb && v < a.V && v - vb < SW) atomicAdd(&L.cnt[v - vb], 1);
+    }
+  }
+  if (a.bias_token) {
+    const int e1 = min(a.bias_off[b + 1], a.n_bias);
+    for (int e = max(a.bias_off[b], 0) + threadIdx.x; e < e1; e += 256) {
+      const int v = a.bias_token[e];
+      if (v >= vb && v < a.V && v - vb < SW) atomicMax(&L.bias[v - vb], e + 1);
+    }
+  }
+  __syncthreads();
+}
+// four tokens from vb + i on (bits of seen and open: one per token)
+struct AdjustTok4 {
+  float rep, pres, shift[4], bias[4];
+  uint32_t seen, open;
+};
+template <int SW>
+__device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, int vb, int i, const AdjustLds<SW>& L) {
+#pragma clang fp contract(off)
+  AdjustTok4 t;
+  t.rep = a.repetition ? a.repetition[b] : 1.f;
+  t.pres = a.presence ? a.presence[b] : 0.f;
+  const float freq = a.frequency ? a.frequency[b] : 0.f;
+  t.seen = 0;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int n = L.cnt[i + c], e = L.bias[i + c];
+    t.shift[c] = freq * (float)n;
+    t.bias[c] = e > 0 ? a.bias_value[e - 1] : 0.f;
+    t.seen |= (n > 0 ? 1u : 0u) << c;
+  }
+  const int v = vb + i;  // a multiple of 4
+  t.open = v >= a.V ? 0u : a.mask ? (a.mask[(size_t)b * a.mask_row + (v >> 5)] >> (v & 31)) & 15u : 15u;
+  return t;
+}
+template <bool MASK>
+__device__ __forceinline__ void adjust4(const AdjustTok4& t, float (&x)[4]) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    if (t.seen >> c & 1) {
+      x[c] = x[c] > 0.f ? x[c] / t.rep : x[c] * t.rep;
+      x[c] = (x[c] - t.shift[c]) - t.pres;
+    }
+    x[c] += t.bias[c];
+    if (MASK && !(t.open >> c & 1)) x[c] = kNegInf;
+  }
+}
+
+// Rows of adjusted logits: a block per (slice of 1024 tokens, row group of a query).
+// A thread has four neighbouring tokens of every row, a 16-byte load and store each
+// (at any 4-byte address). Bound: HBM, every logit read and written once.
+__global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
+  constexpr int SW = 1024;
+  __shared__ AdjustLds<SW> lds;
+  const int b = blockIdx.y, vb = blockIdx.x * SW, i = 4 * threadIdx.x, v = vb + i;
+  const int s0 = a.query_seq0[b], n = a.query_seq0[b + 1] - s0;
+  const int r0 = blockIdx.z * a.rows_per_block, r1 = min(n, r0 + a.rows_per_block);
+  if (r0 >= r1) return;
+  adjust_slice<SW>(a, b, vb, lds);
+  if (v >= a.V) return;
+  const AdjustTok4 t = adjust_tok4<SW>(a, b, vb, i, lds);
+  const size_t at = (size_t)(s0 + r0) * a.V + v;
+  if (v + 4 <= a.V) {
+    for (int r = r0; r < r1; ++r) {
+      const size_t o = at + (size_t)(r - r0) * a.V;
+      const f32x4 w = *(const f32x4_a4*)(a.logits + o);
+      float x[4] = {w[0], w[1], w[2], w[3]};
+      adjust4<true>(t, x);
+      *(f32x4_a4*)(a.out + o) = f32x4{x[0], x[1], x[2], x[3]};
+    }
+  } else {
+    for (int r = r0; r < r1; ++r) {
+      const size_t o = at + (size_t)(r - r0) * a.V;
+      float x[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] = a.logits[min(o + c, (size_t)(s0 + r + 1) * a.V - 1)];
+      adjust4<true>(t, x);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (v + c < a.V) a.out[o + c] = x[c];
+    }
+  }
+}
+
+// k_fuse over adjusted logits, which are not stored: Eq. 2 and the best two tokens
+// of a slice. Tokens that the mask closes, and scores that are NaN or -inf, are
+// nobody's choice: a slice without any other has no candidate (expert 0).
+template <bool VEC>
+__global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
+#pragma clang fp contract(off)
+  constexpr int SW = 256, NB = 4;
+  __shared__ AdjustLds<SW> lds;
+  __shared__ float sbest[4][SW];
+  __shared__ int sk[4][SW];
+  __shared__ Top2 swave[4];
+  const int b = blockIdx.y, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool inl = b < kFuseInlineQueries;
+  const int s0 = inl ? a.inl_seq0[b] : a.query_seq0[b];
+  const int N = (inl ? a.inl_seq0[b + 1] : a.query_seq0[b + 1]) - s0 - 1;
+  const int e0 = inl ? a.inl_exp0[b] : a.query_exp0[b];
+  const int per = (N + 3) / 4;                       // experts per wave
+  const int k_lo = 1 + wave * per, k_hi = min(N, k_lo + per - 1);
+  const int vb = blockIdx.x * SW, v = vb + 4 * lane;
+  const float* L0 = a.logits + (size_t)s0 * a.V;
+  adjust_slice<SW>(d, b, vb, lds);
+  const AdjustTok4 t = adjust_tok4<SW>(d, b, vb, 4 * lane, lds);
+  auto load = [&](const float* row, float (&x)[4]) {
+    const float4 w = load_tok4<VEC>(row, v, a.V);
+    x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+  };
+  float sa[4], best[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+  int bk[4] = {0, 0, 0, 0};
+  load(L0, sa);
+  adjust4<false>(t, sa);
+  for (int kb = k_lo; kb <= k_hi; kb += NB) {
+    float x[NB][4], cb[NB], cp[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int k = min(kb + j, k_hi);
+      load(L0 + (size_t)k * a.V, x[j]);
+      cb[j] = a.beta[e0 + k - 1];
+      cp[j] = a.prior[e0 + k - 1];
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int k = kb + j;
+      adjust4<false>(t, x[j]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float t1 = (1.0f + cb[j]) * x[j][c];
+        const float t2 = cb[j] * sa[c];
+        const float val = (t1 - t2) + cp[j];
+        const bool up = k <= k_hi && (t.open >> c & 1) && val > best[c];
+        best[c] = up ? val : best[c];
+        bk[c] = up ? k : bk[c];
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    sbest[wave][4 * lane + c] = best[c];
+    sk[wave][4 * lane + c] = bk[c];
+  }
+  __syncthreads();
+  Top2 cand{kNegInf, 0x7FFFFFFF, 0, kNegInf, 0x7FFFFFFF};
+  {
+    const int u = threadIdx.x;
+    float x = sbest[0][u];
+    int k = sk[0][u];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float y = sbest[w][u];
+      if (y > x) { x = y; k = sk[w][u]; }
+    }
+    if (vb + u < a.V && k > 0) cand = Top2{x, vb + u, k, kNegInf, 0x7FFFFFFF};
   }
   cand = wave_top2(cand);
   if (lane == 0) swave[wave] = cand;
@@ -3426,21 +3580,6 @@ __global__ __launch_bounds__(256) void k_rho(const float* ss, int parts, int ld,
 // ------------------------------------------------------------------ launchers
 
 
-namespace {
-// Launch; timing events, when given, are attached to the dispatch itself
-// (start when the kernel begins, stop when it completes), so they measure the
-// kernel and not the queue around it.
-template <typename Kern, typename... Args>
-hipError_t go(Kern kernel, dim3 grid, dim3 block, size_t shm, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1,
-              Args... args) {
-  if (ev0 || ev1) hipExtLaunchKernelGGL(kernel, grid, block, (uint32_t)shm, st, ev0, ev1, 0u, args...);
-  else hipLaunchKernelGGL(kernel, grid, block, shm, st, args...);
-  return hipGetLastError();
-}
-hipEvent_t t0(const Timing* tm) { return tm ? tm->start : nullptr; }
-hipEvent_t t1(const Timing* tm) { return tm ? tm->stop : nullptr; }
-}  // namespace
-
 hipError_t launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t st) {
   if (n == 0) return hipSuccess;
   const int blocks = (int)((n + 255) / 256 < 1024 ? (n + 255) / 256 : 1024);
@@ -3894,6 +4033,27 @@ hipError_t launch_agg(const AggArgs& a, int n_exp, int n_queries, hipStream_t st
                : go(k_agg<false, true>, g, dim3(256), 0, st, nullptr, t1(tm), a);
   return vec ? go(k_agg<true, false>, g, dim3(256), 0, st, nullptr, t1(tm), a)
              : go(k_agg<false, false>, g, dim3(256), 0, st, nullptr, t1(tm), a);
+}
+
+int adjusted_slices(int V) { return (V + 255) / 256; }
+
+hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st, const Timing* tm,
+                                const Timing* tm_merge) {
+  const dim3 g(a.nblk, n_queries);
+  const bool vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;  // (V >= 2)
+  const hipError_t e = vec ? go(k_fuse_adjusted<true>, g, dim3(256), 0, st, t0(tm), t1(tm), a, d)
+                                                : go(k_fuse_adjusted<false>, g, dim3(256), 0, st, t0(tm), t1(tm), a, d);
+  if (e != hipSuccess) return e;
+  return go(k_fuse_final, dim3(n_queries), dim3(kFuseBlock), 0, st, t0(tm_merge), t1(tm_merge), a);
+}
+
+hipError_t launch_adjust(const AdjustArgs& a0, int n_queries, int max_rows, int num_cus, hipStream_t st) {
+  AdjustArgs a = a0;
+  const int slices = (a.V + 1023) / 1024;
+  a.rows_per_block = max_rows;
+  const dim3 g(slices, n_queries, (max_rows + a.rows_per_block - 1) / a.rows_per_block);
+  (void)num_cus;
+  return go(k_adjust, g, dim3(256), 0, st, nullptr, nullptr, a);
 }
 
 hipError_t launch_fuse_final(const FuseArgs& a, int n_queries, hipStream_t st, const Timing* tm) {

@@ -17,6 +17,52 @@ def _torch():
     return torch
 
 
+class Adjust:
+    """A batch's logits adjustments (pced_adjust) with the device tensors they are in.
+
+    history [n] int32 tokens of all queries and history_off [B + 1] int32; repetition,
+    presence, frequency [B] float32; bias_token int32 and bias_value float32 [m] with
+    bias_off [B + 1] int32; mask [B][words] int32, whose rows may be wider than
+    ceil(V / 32) words or apart. All optional."""
+
+    DTYPES = dict(history="int32", history_off="int32", repetition="float32", presence="float32", frequency="float32",
+                  bias_token="int32", bias_value="float32", bias_off="int32", mask="int32")
+
+    def __init__(self, n_queries, vocab, **tensors):
+        torch = _torch()
+        unknown = set(tensors) - set(self.DTYPES)
+        if unknown:
+            raise ValueError(f"unknown adjustments {sorted(unknown)}")
+        self.n_queries, self.vocab = n_queries, vocab
+        self.tensors = {k: t for k, t in tensors.items() if t is not None}
+        for name, t in self.tensors.items():
+            if t.dtype != getattr(torch, self.DTYPES[name]):
+                raise ValueError(f"{name}: {t.dtype}, not {self.DTYPES[name]}")
+            if name == "mask":
+                if t.dim() != 2 or t.shape[0] < n_queries or t.stride(1) != 1 or t.shape[1] < -(-vocab // 32):
+                    raise ValueError("mask: [queries][>= ceil(vocab / 32)] words, a row's words next to each other")
+                continue
+            if t.dim() != 1 or not t.is_contiguous():
+                raise ValueError(f"{name}: one dimension, contiguous")
+            want = {"history_off": n_queries + 1, "bias_off": n_queries + 1, "repetition": n_queries,
+                    "presence": n_queries, "frequency": n_queries}.get(name, 0)
+            if t.numel() < want:
+                raise ValueError(f"{name}: {t.numel()} entries, not {want}")
+        for name, others in (("history", ("history_off",)), ("bias_token", ("bias_off", "bias_value"))):
+            if name in self.tensors and any(o not in self.tensors for o in others):
+                raise ValueError(f"{name} without {' or '.join(others)}")
+        size = lambda n: self.tensors[n].numel() if n in self.tensors else 0  # noqa: E731
+        if "bias_token" in self.tensors and size("bias_value") < size("bias_token"):
+            raise ValueError("bias_value is shorter than bias_token")
+        # (a list without entries has no memory to point at: it adjusts nothing)
+        ptr = {k: t.data_ptr() for k, t in self.tensors.items() if t.numel() > 0}
+        mask = self.tensors.get("mask")
+        row = 0 if mask is None else mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+        if mask is not None and row < -(-vocab // 32):
+            raise ValueError("mask: the rows overlap")
+        self.struct = _lib.pced_adjust(mask_row=row, n_history=size("history"), n_bias=size("bias_token"), **ptr)
+
+
 class PcedSession:
     """A context plus its two KV pools for one model geometry and capacity."""
 
@@ -127,6 +173,119 @@ class PcedSession:
         out = dict(extra or {})
         out["tokens"] = tokens
         return out
+
+    # ------------------------------------------------------ layer-wise calls
+    def _storage(self, t, name):
+        """A tensor of the session's storage type (bf16 values or their bits, or float32)."""
+        torch = _torch()
+        if t.dtype not in ((torch.bfloat16, torch.int16, torch.uint16) if self.dtype == "bf16" else (torch.float32,)):
+            raise ValueError(f"{name}: {t.dtype} in a session of {self.dtype}")
+        return t
+
+    def _layers(self, layer, n_layers):
+        return int(layer), self.geom["n_layers"] - int(layer) if n_layers is None else int(n_layers)
+
+    def _row_stride(self, t, name, n_tokens, n_layers, heads):
+        """Elements from one row of [S * n_tokens][n_layers][heads][D] to the next."""
+        shape = (self.S * n_tokens, n_layers, heads, self.geom["head_dim"])
+        if tuple(self._storage(t, name).shape) != shape:
+            raise ValueError(f"{name}: {tuple(t.shape)}, not {shape}")
+        inner = (heads * shape[3], shape[3], 1)
+        if any(n > 1 and st != want for n, st, want in zip(shape[1:], t.stride()[1:], inner)):
+            raise ValueError(f"{name}: a row's elements must follow each other")
+        return t.stride(0) if shape[0] > 1 else n_layers * heads * shape[3]
+
+    def append(self, q, k, v, n_tokens=1, rope=None, layer=0, n_layers=None, q_out=None):
+        """pced_append of layers [layer, layer + n_layers) (default: to the last): rows
+        [S * n_tokens][n_layers][heads][D], which may be apart (views of one projection's
+        output); q None: K / V only. ``rope``: (theta, rot_dim, halves) or None. Returns the
+        rotated q rows (``q_out`` or a new tensor)."""
+        torch = _torch()
+        layer, n_layers = self._layers(layer, n_layers)
+        g = self.geom
+        rows = _lib.pced_rows(k=k.data_ptr(), v=v.data_ptr(),
+                              k_row=self._row_stride(k, "k", n_tokens, n_layers, g["n_kv_heads"]),
+                              v_row=self._row_stride(v, "v", n_tokens, n_layers, g["n_kv_heads"]))
+        if q is not None:
+            rows.q, rows.q_row = q.data_ptr(), self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"])
+            if q_out is None:
+                q_out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+            elif tuple(self._storage(q_out, "q_out").shape) != tuple(q.shape) or not q_out.is_contiguous():
+                raise ValueError("q_out: q's shape, contiguous")
+        theta, rot, halves = rope if rope is not None else (2.0, 0, False)
+        self.ctx.pced_append(layer, n_layers, n_tokens, rows,
+                             _lib.pced_rope(theta=theta, rot_dim=rot, halves=int(bool(halves))), q_out)
+        return q_out
+
+    def advance(self, n_tokens=1):
+        self.ctx.pced_advance(n_tokens)
+
+    def bind_summary(self):
+        """A new buffer for the page summaries, bound to the context."""
+        torch = _torch()
+        self.summary = torch.empty(_lib.pced_summary_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+        self.ctx.pced_bind_summary(self.summary)
+
+    def summarize(self):
+        self.ctx.pced_summarize()
+
+    def attend(self, q, n_tokens=1, select=None, layer=0, n_layers=None, want=(), x_out=None):
+        """pced_attend: q as append returned it; ``select``: (n_pages, n_first, n_last) or None
+        for all pages. Returns {"x": [S * n_tokens][n_layers][Hq * D]}, and with "pages" in
+        ``want`` the pages [S * n_tokens][n_layers][Hkv][n_pages]."""
+        torch = _torch()
+        layer, n_layers = self._layers(layer, n_layers)
+        g = self.geom
+        if set(want) - {"pages"}:
+            raise ValueError(f"unknown outputs {sorted(set(want) - {'pages'})}")
+        rows, width = self.S * n_tokens, g["n_q_heads"] * g["head_dim"]
+        if self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"]) != n_layers * width:
+            raise ValueError("q: rows must follow each other")
+        if x_out is None:
+            x_out = torch.empty((rows, n_layers, width), dtype=q.dtype, device=q.device)
+        elif tuple(self._storage(x_out, "x_out").shape) != (rows, n_layers, width) or not x_out.is_contiguous():
+            raise ValueError("x_out: [S * n_tokens][n_layers][Hq * D], contiguous")
+        out, sel = {"x": x_out}, None
+        if select is not None:
+            sel = _lib.pced_select(*(int(x) for x in select))
+            if "pages" in want:
+                out["pages"] = torch.empty((rows, n_layers, g["n_kv_heads"], max(0, sel.n_pages)), dtype=torch.int32,
+                                           device=q.device)
+        elif want:
+            raise ValueError("pages without select")
+        self.ctx.pced_attend(layer, n_layers, n_tokens, q, sel, x_out, out.get("pages"))
+        return out
+
+    # ------------------------------------------------------- adjusted logits
+    def adjust(self, **tensors):
+        """The loaded batch's adjustments (see Adjust) for adjust_logits and fuse_adjusted."""
+        return Adjust(self.B, self.geom["vocab"], **tensors)
+
+    def _logits(self, t, name):
+        torch = _torch()
+        if t.dtype != torch.float32 or tuple(t.shape) != (self.S, self.geom["vocab"]) or not t.is_contiguous():
+            raise ValueError(f"{name}: float32 [{self.S}][{self.geom['vocab']}], contiguous")
+        return t
+
+    def _adjust(self, adjust):
+        if (adjust.n_queries, adjust.vocab) != (self.B, self.geom["vocab"]):
+            raise ValueError("the adjustments are another batch's")
+        return adjust.struct
+
+    def adjust_logits(self, logits, adjust, out=None):
+        """pced_adjust_logits of [S][V] logits; ``out`` may be logits itself."""
+        torch = _torch()
+        out = torch.empty_like(logits) if out is None else self._logits(out, "out")
+        self.ctx.pced_adjust_logits(self._logits(logits, "logits"), self._adjust(adjust), out)
+        return out
+
+    def fuse_adjusted(self, logits, adjust, refresh_beta=False, want=("winner", "top1", "top2", "beta_used")):
+        """pced_fuse_adjusted: the tokens chosen over adjusted logits, and the wanted outputs."""
+        torch = _torch()
+        tokens = torch.empty(self.B, dtype=torch.int32, device=self.device)
+        extra = self.out_buffers(want) if want else None
+        self.ctx.pced_fuse_adjusted(self._logits(logits, "logits"), refresh_beta, self._adjust(adjust), tokens, extra)
+        return dict(extra or {}, tokens=tokens)
 
     def lengths(self):
         return self.ctx.pced_get_lengths(self.S)
