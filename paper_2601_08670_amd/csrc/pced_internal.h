@@ -321,7 +321,8 @@ struct ReadCacheArgs {
 };
 
 constexpr int kSumExp = 64;        // page summaries: scales are 2^-kSumExp .. 2^kSumExp
-constexpr int kScorePages = 256;   // pages per work-group of the page scores
+constexpr int kPickPages = 512;    // pages whose bounds and choice are one launch, at most
+constexpr int kScorePages = 256;   // pages per work-group of the bounds beyond that
 constexpr int kAttendTokens = 16;  // new tokens of a sequence that are scored together, at most
 inline int summary_row(int head_dim) { return (2 * head_dim + 63) / 64 * 64; }  // bytes of a page's codes
 

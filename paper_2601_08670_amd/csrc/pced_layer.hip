@@ -337,167 +337,336 @@ __device__ __forceinline__ const int32_t* page_list(const AttendArgs& a, const A
                      : a.list + item * a.n_pages;
 }
 
-// Bounds on the scores of every page that a token may select. With the q-heads
-// of a kv-head taken together,
+// Bounds on the scores of the pages that a token may select. With the q-heads of a
+// kv-head taken together,
 //   sum_g q_g . k  <=  sum_d (w+_d max_d + w-_d min_d),
 //   w+ = sum_g max(q_g, 0),  w- = sum_g min(q_g, 0),
 // for every key k of the page. The weights go to int8 with one power of two as
 // scale (to nearest; the same for all pages, so it is left out), max and min are
 // the page's codes: a product of 2 D int8 pairs on the matrix cores, exact in
 // int32, times the page's power of two, exact in fp32 (2 * 128 * 127^2 < 2^24). So a
-// page's bound has one value however the work is split. One block per (token
-// group, layer, kv-head, kScorePages pages): 16 pages x up to 16 tokens per product,
-// pages in rows, tokens in columns. Bound: HBM, the summaries are read once.
-__global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
-  __shared__ __align__(16) int8_t w[16][256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int chunk = blockIdx.x % a.chunks;
-  size_t item = blockIdx.x / a.chunks;  // (group, layer, kv-head)
-  const int h = (int)(item % a.n_kv_heads);
-  item /= a.n_kv_heads;
-  const int l = (int)(item % a.launch_layers), gl = (int)(item / a.launch_layers), g = a.group0 + gl;
-  const int s = g / a.seq_groups, tok0 = g % a.seq_groups * a.gt, nt = min(a.gt, a.n_tokens - tok0);
-  const int len = a.len0[s] + a.t;
-  const int pages = (len + tok0 + nt - 1) / kPage + 1;   // that the group's last token sees
-  const int p0 = chunk * kScorePages, p1 = min(pages - a.last, p0 + kScorePages);
-  if (pages <= a.n_pages || p0 >= p1) return;
-  const int G = a.group, D = a.head_dim, row = a.sum_row;
-  for (int i = tid; i < 16 * 256 / 4; i += 256) ((uint32_t*)w)[i] = 0u;
-  __syncthreads();
-  for (int j = wave; j < nt; j += 4) {
-    const size_t qr = (((size_t)s * a.n_tokens + tok0 + j) * a.n_layers + a.layer - a.layer0 + l) * a.n_q_heads + (size_t)h * G;
-    double up[2] = {0., 0.}, dn[2] = {0., 0.};
-    for (int q = 0; q < G; ++q)
+// page's bound has one value however the work is split, and the choice of pages
+// is one and the same for every launch shape.
+
+// The smallest exponent whose scale keeps v, rounded, within 127 (it grows with v,
+// so the largest over a row's values is the row's). Sums are exact in fp64.
+__device__ __forceinline__ int weight_exp(double v) {
+  if (!(v > 0.)) return -kSumExp;
+  int ex = ilogb(fmin(v, 1e300)) - 6;
+  if (rint(ldexp(v, -ex)) > 127.) ++ex;
+  return min(max(ex, -kSumExp), kSumExp);
+}
+
+// The weights of one row's kv-head (q at its first head) by one wave, lane i holding
+// dims 2i and 2i + 1, to row[0 .. 2D).
+__device__ __forceinline__ void query_weights(const AttendArgs& a, const void* q, int lane, int8_t* row) {
+  const int G = a.group, D = a.head_dim, d = min(2 * lane, D - 2);
+  double up[2] = {0., 0.}, dn[2] = {0., 0.};
+  for (int g0 = 0; g0 < G; g0 += 4) {
+    float x[4][2];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int d = lane + 64 * c;
-        if (d >= D) continue;
-        const size_t o = (qr + q) * D + d;
-        const float x = a.bf16 ? bf2f(((const uint16_t*)a.q)[o]) : ((const float*)a.q)[o];
-        up[c] += (double)fmaxf(x, 0.f);
-        dn[c] += (double)fminf(x, 0.f);
+    for (int i = 0; i < 4; ++i) {
+      const size_t o = (size_t)min(g0 + i, G - 1) * D + d;
+      if (a.bf16) {
+        const uint32_t u = *(const uint32_t*)((const uint16_t*)q + o);
+        x[i][0] = bf2f(u & 0xFFFFu);
+        x[i][1] = bf2f(u >> 16);
+      } else {
+        const f32x2 u = *(const f32x2*)((const float*)q + o);
+        x[i][0] = u[0];
+        x[i][1] = u[1];
       }
-    double top = fmax(fmax(up[0], -dn[0]), fmax(up[1], -dn[1]));
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) top = fmax(top, __shfl_xor(top, o));
-    int ex = -kSumExp;
-    if (top > 0.) {
-      ex = ilogb(fmin(top, 1e300)) - 6;
-      if (rint(ldexp(top, -ex)) > 127.) ++ex;
-      ex = min(max(ex, -kSumExp), kSumExp);
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int d = lane + 64 * c;
-      if (d >= D) continue;
-      w[j][d] = (int8_t)(int)fmin(rint(ldexp(up[c], -ex)), 127.);
-      w[j][D + d] = (int8_t)(int)fmax(rint(ldexp(dn[c], -ex)), -127.);
-    }
+    for (int i = 0; i < 4; ++i)
+      if (g0 + i < G)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          up[c] += (double)fmaxf(x[i][c], 0.f);
+          dn[c] += (double)fminf(x[i][c], 0.f);
+        }
   }
-  __syncthreads();
-  const int col = lane & 15, quad = lane >> 4;
-  i32x4 b[4];
+  int ex = max(max(weight_exp(up[0]), weight_exp(up[1])), max(weight_exp(-dn[0]), weight_exp(-dn[1])));
 #pragma unroll
-  for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
-  const size_t base = ((size_t)(a.layer + l) * a.n_kv_heads + h) * a.max_pages;
-  const int32_t* pt = a.page_table + (size_t)s * a.maxpps;
-  const size_t out0 = ((size_t)gl * a.gt + col) * a.launch_layers + l;
-  float* out = a.scores + (out0 * a.n_kv_heads + h) * a.score_row;
-  for (int q = p0 + 16 * wave; q < p1; q += 64) {
-    const int phys = pt[min(q + col, p1 - 1)];  // (pages past the range repeat its last one)
-    const int8_t* code = a.codes + (base + phys) * row + 16 * quad;
-    const float sc = a.scale[base + phys];
-    i32x4 c = {0, 0, 0, 0};
+  for (int o = 32; o >= 1; o >>= 1) ex = max(ex, __shfl_xor(ex, o));
+  int8_t w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (64 * k < row) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(code + 64 * k), b[k], c, 0, 0, 0);
-    float4 o;
-    o.x = (float)c[0] * __shfl(sc, 4 * quad);
-    o.y = (float)c[1] * __shfl(sc, 4 * quad + 1);
-    o.z = (float)c[2] * __shfl(sc, 4 * quad + 2);
-    o.w = (float)c[3] * __shfl(sc, 4 * quad + 3);
-    if (col < nt) *(float4*)(out + q + 4 * quad) = o;  // (rows hold whole groups of 16 pages)
+  for (int c = 0; c < 2; ++c) {
+    w[c] = (int8_t)(int)fmin(rint(ldexp(up[c], -ex)), 127.);
+    w[2 + c] = (int8_t)(int)fmax(rint(ldexp(dn[c], -ex)), -127.);
+  }
+  if (2 * lane < D) {
+    *(uint16_t*)(row + d) = (uint16_t)((uint8_t)w[0] | (uint8_t)w[1] << 8);
+    *(uint16_t*)(row + D + d) = (uint16_t)((uint8_t)w[2] | (uint8_t)w[3] << 8);
   }
 }
 
-// fp32 order as unsigned order
+// 16 pages' codes as the rows of a product (lane: page lane % 16, bytes 16 (lane / 16)
+// of each 64), and the pages' scales.
+struct CodeTile {
+  i32x4 c[4];
+  float scale;
+};
+__device__ __forceinline__ void load_codes(const AttendArgs& a, size_t base, int phys, int quad, CodeTile& t) {
+  const int8_t* code = a.codes + (base + phys) * a.sum_row + 16 * quad;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) t.c[k] = *(const i32x4*)(code + min(64 * k, a.sum_row - 64));
+  t.scale = a.scale[base + phys];
+}
+// bounds of pages 4 (lane / 16) .. + 3 of the tile for the token of column lane % 16
+__device__ __forceinline__ float4 tile_bounds(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4], int quad) {
+  i32x4 c = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (64 * k < a.sum_row) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.c[k], w[k], c, 0, 0, 0);
+  return make_float4((float)c[0] * __shfl(t.scale, 4 * quad), (float)c[1] * __shfl(t.scale, 4 * quad + 1),
+                     (float)c[2] * __shfl(t.scale, 4 * quad + 2), (float)c[3] * __shfl(t.scale, 4 * quad + 3));
+}
+
+// fp32 order as unsigned order; 0 is below every number's key
 __device__ __forceinline__ uint32_t order_key(float f) {
   const uint32_t u = __float_as_uint(f + 0.f);  // (-0 counts as 0)
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The chosen pages of one item, ascending: the first and the last ones and, of
-// those between, the `want` highest bounds (the lower page of equal ones). The
-// want-th highest key is found by radix, 8 bits a pass; then the pages are written
-// in order, their places from prefix sums.
-__global__ __launch_bounds__(256) void k_page_select(AttendArgs a) {
-  __shared__ int hist[256];
-  __shared__ uint32_t s_key;
-  __shared__ int s_want, s_base;
-  __shared__ int wsum[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A token group's (group, layer, kv-head) of a launch
+struct GroupItem {
+  int s, l, h, gl, tok0, nt, len, pages;  // nt tokens from tok0 on; pages: that the last of them sees
+};
+__device__ __forceinline__ GroupItem group_item(const AttendArgs& a, size_t item) {
+  GroupItem r;
+  r.h = (int)(item % a.n_kv_heads);
+  item /= a.n_kv_heads;
+  r.l = (int)(item % a.launch_layers);
+  r.gl = (int)(item / a.launch_layers);
+  const int g = a.group0 + r.gl;
+  r.s = g / a.seq_groups;
+  r.tok0 = g % a.seq_groups * a.gt;
+  r.nt = min(a.gt, a.n_tokens - r.tok0);
+  r.len = a.len0[r.s] + a.t;
+  r.pages = (r.len + r.tok0 + r.nt - 1) / kPage + 1;
+  return r;
+}
+__device__ __forceinline__ const void* group_q(const AttendArgs& a, const GroupItem& it, int j) {
+  const size_t row = ((size_t)it.s * a.n_tokens + it.tok0 + j) * a.n_layers + a.layer - a.layer0 + it.l;
+  return (const char*)a.q + (row * a.n_q_heads + (size_t)it.h * a.group) * a.head_dim * (a.bf16 ? 2 : 4);
+}
+__device__ __forceinline__ size_t group_slot(const AttendArgs& a, const GroupItem& it, int j) {
+  return (((size_t)it.gl * a.gt + j) * a.launch_layers + it.l) * a.n_kv_heads + it.h;
+}
+
+// The pages of one token from the keys of its candidates, page lo + 64 i + lane at
+// key[i] (0: no candidate), by one wave: the want-th highest key bit by bit, from
+// counts over the wave, then the pages in order, each at its place. want >= 1, and
+// there are at least as many candidates. Returns nothing but the list.
+template <int R>
+__device__ __forceinline__ void pick_pages(const uint32_t (&key)[R], int lo, int want, int32_t* list, int lane) {
+  uint32_t t = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t c = t | (1u << b);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= c));
+    if (n >= want) t = c;
+  }
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) above += __popcll(__ballot(key[i] > t));
+  const int ties = want - above;  // pages equal to the key that are taken, the lowest first
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  int base = 0, eq = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint64_t mg = __ballot(key[i] > t), me = __ballot(key[i] == t);
+    const int e = eq + __popcll(me & below);
+    if (key[i] > t || (key[i] == t && e < ties))
+      list[base + __popcll(mg & below) + min(e, ties) - min(eq, ties)] = lo + 64 * i + lane;
+    const int eq1 = eq + __popcll(me);
+    base += __popcll(mg) + min(eq1, ties) - min(eq, ties);
+    eq = eq1;
+  }
+}
+
+// The pages that need no choice: all of them, or the first and the last ones.
+// Returns how many are to be chosen between.
+__device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32_t* list, int i0, int step) {
+  if (pages <= a.n_pages) {
+    for (int i = i0; i < a.n_pages; i += step) list[i] = i < pages ? i : -1;
+    return 0;
+  }
+  for (int i = i0; i < a.first; i += step) list[i] = i;
+  for (int i = i0; i < a.last; i += step) list[a.n_pages - a.last + i] = pages - a.last + i;
+  return a.n_pages - a.first - a.last;
+}
+
+// Bounds and choice in one launch, for at most 64 R pages: one block of 8 waves per
+// (token group, layer, kv-head), R/2 tiles of 16 pages per wave. The codes are on
+// their way while the weights are made; the bounds meet in LDS, from where each
+// wave chooses the pages of a token.
+template <int R>
+__global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
+  constexpr int NT = R / 2;
+  __shared__ __align__(16) int8_t w[16][256];
+  __shared__ __align__(16) float bound[16][64 * R + 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const GroupItem it = group_item(a, blockIdx.x);
+  if (it.pages > a.n_pages) {
+    const int p1 = it.pages - a.last;  // pages [first, p1) are chosen between
+    const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
+    const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
+    CodeTile t[NT];
+    int phys[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) phys[i] = pt[min(16 * (wave + 8 * i) + col, p1 - 1)];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (16 * (wave + 8 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
+    for (int j = wave; j < it.nt; j += 8) query_weights(a, group_q(a, it, j), lane, w[j]);
+    __syncthreads();
+    i32x4 b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+      if (16 * (wave + 8 * i) < p1) {
+        const float4 o = tile_bounds(a, t[i], b, quad);
+        if (col < it.nt) *(float4*)&bound[col][16 * (wave + 8 * i) + 4 * quad] = o;
+      }
+    __syncthreads();
+  }
+  for (int j = wave; j < it.nt; j += 8) {
+    const size_t slot = group_slot(a, it, j);
+    const AttendItem row = attend_item(a, slot);
+    int32_t* list = const_cast<int32_t*>(page_list(a, row, slot));
+    if (row.pages <= a.n_pages && !a.pages_out) continue;  // (all pages: nobody reads the list)
+    const int want = fixed_pages(a, row.pages, list, lane, 64);
+    if (want == 0) continue;
+    uint32_t key[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int p = 64 * i + lane;
+      key[i] = p >= a.first && p < row.pages - a.last ? order_key(bound[j][p]) : 0u;
+    }
+    pick_pages<R>(key, 0, want, list + a.first, lane);
+  }
+}
+
+// The same in two launches for long sequences, whose summaries one work-group would
+// take long to read. Bounds: a block per (token group, layer, kv-head, kScorePages
+// pages), four tiles of 16 pages per wave. Bound: HBM, the summaries are read once.
+__global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
+  constexpr int NT = kScorePages / 64;
+  __shared__ __align__(16) int8_t w[16][256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const GroupItem it = group_item(a, blockIdx.x / a.chunks);
+  const int p0 = blockIdx.x % a.chunks * kScorePages, p1 = min(it.pages - a.last, p0 + kScorePages);
+  if (it.pages <= a.n_pages || p0 >= p1) return;
+  const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
+  const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
+  CodeTile t[NT];
+  int phys[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) phys[i] = pt[min(p0 + 16 * (wave + 4 * i) + col, p1 - 1)];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+    if (p0 + 16 * (wave + 4 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
+  for (int j = wave; j < it.nt; j += 4) query_weights(a, group_q(a, it, j), lane, w[j]);
+  __syncthreads();
+  i32x4 b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
+  float* out = a.scores + group_slot(a, it, col) * a.score_row + p0 + 4 * quad;
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+    if (p0 + 16 * (wave + 4 * i) < p1) {
+      const float4 o = tile_bounds(a, t[i], b, quad);
+      if (col < it.nt) *(float4*)(out + 16 * (wave + 4 * i)) = o;  // (rows hold whole tiles)
+    }
+}
+
+// The choice from those bounds: a block of 16 waves per item, wave v's keys being the
+// v-th run of 64 R candidates. As pick_pages, with the counts of the waves added up
+// in LDS, one barrier per bit. A row of more than 1024 R candidates (MANY) goes in
+// rounds, whose keys are read again for every bit.
+template <int R, bool MANY>
+__global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
+  __shared__ int count[33];
+  __shared__ int wsum[2][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t item = blockIdx.x;
   const AttendItem it = attend_item(a, item);
-  if (it.pages == 0) return;
+  if (it.pages == 0 || (it.pages <= a.n_pages && !a.pages_out)) return;
   int32_t* list = const_cast<int32_t*>(page_list(a, it, item));
-  if (it.pages <= a.n_pages) {
-    for (int i = tid; i < a.n_pages; i += 256) list[i] = i < it.pages ? i : -1;
-    return;
-  }
-  const int lo = a.first, hi = it.pages - a.last;
-  int want = a.n_pages - a.first - a.last;
-  for (int i = tid; i < a.first; i += 256) list[i] = i;
-  for (int i = tid; i < a.last; i += 256) list[a.n_pages - a.last + i] = hi + i;
+  const int want = fixed_pages(a, it.pages, list, tid, 1024);
   if (want == 0) return;
+  list += a.first;
+  const int lo = a.first, hi = it.pages - a.last;
+  const int rounds = MANY ? (hi - lo + 1024 * R - 1) / (1024 * R) : 1;
   const float* sc = a.scores + item * a.score_row;
-  uint32_t key = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int p = lo + tid; p < hi; p += 256) {
-      const uint32_t k = order_key(sc[p]);
-      if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+  uint32_t key[R];
+  auto load = [&](int round) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int p = lo + (round * 16 + wave) * 64 * R + 64 * i + lane;
+      key[i] = p < hi ? order_key(sc[min(p, hi - 1)]) : 0u;
     }
-    __syncthreads();
-    if (wave == 0) {
-      // lane i: bins 255 - 4i .. 252 - 4i, from the highest down
-      int c[4], sum = 0;
+  };
+  if (tid < 33) count[tid] = 0;
+  load(0);
+  __syncthreads();
+  uint32_t t = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t c = t | (1u << b);
+    int n = 0;
+    for (int r = 0; r < rounds; ++r) {
+      if (MANY) load(r);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { c[j] = hist[255 - 4 * lane - j]; sum += c[j]; }
-      int before = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(before, o); if (lane >= o) before += t; }
-      before -= sum;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (before < want && want <= before + c[j]) {
-          s_key = key | ((uint32_t)(255 - 4 * lane - j) << shift);
-          s_want = want - before;
-        }
-        before += c[j];
-      }
+      for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= c));
     }
+    if (lane == 0 && n) atomicAdd(&count[b], n);
     __syncthreads();
-    key = s_key;
-    want = s_want;  // of the pages with this prefix
+    if (count[b] >= want) t = c;
   }
-  // want pages equal to the key are taken, the lowest first
-  int base = a.first, ties = 0;
-  for (int p0 = lo; p0 < hi; p0 += 256) {
-    const int p = p0 + tid;
-    const uint32_t k = p < hi ? order_key(sc[p]) : 0u;
-    const bool gt = p < hi && k > key, eq = p < hi && k == key;
-    const uint64_t mg = __ballot(gt), me = __ballot(eq);
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    if (lane == 0) wsum[wave] = (__popcll(mg) << 16) | __popcll(me);
-    __syncthreads();
-    int pre = 0, all = 0;
+  int n = 0;
+  for (int r = 0; r < rounds; ++r) {
+    if (MANY) load(r);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { if (i < wave) pre += wsum[i]; all += wsum[i]; }
-    const int g = (pre >> 16) + __popcll(mg & below), e = ties + (pre & 0xFFFF) + __popcll(me & below);
-    if (gt || (eq && e < want)) list[base + g + min(e, want) - min(ties, want)] = p;
-    base += (all >> 16) + min(ties + (all & 0xFFFF), want) - min(ties, want);
-    ties += all & 0xFFFF;
+    for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] > t));
+  }
+  if (lane == 0 && n) atomicAdd(&count[32], n);
+  __syncthreads();
+  const int ties = want - count[32];
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  int base = 0, eq = 0;  // places taken and equal keys met before the round
+  for (int r = 0; r < rounds; ++r) {
+    if (MANY) load(r);
+    int g = 0, e = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) { g += __popcll(__ballot(key[i] > t)); e += __popcll(__ballot(key[i] == t)); }
+    if (lane == 0) { wsum[0][wave] = g; wsum[1][wave] = e; }
+    __syncthreads();
+    int gb = 0, eb = 0, ga = 0, ea = 0;  // before this wave, and of all
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      if (v < wave) { gb += wsum[0][v]; eb += wsum[1][v]; }
+      ga += wsum[0][v];
+      ea += wsum[1][v];
+    }
+    int at = base + gb + min(eq + eb, ties) - min(eq, ties), seen = eq + eb;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const uint64_t mg = __ballot(key[i] > t), me = __ballot(key[i] == t);
+      const int k = seen + __popcll(me & below);
+      if (key[i] > t || (key[i] == t && k < ties))
+        list[at + __popcll(mg & below) + min(k, ties) - min(seen, ties)] = lo + (r * 16 + wave) * 64 * R + 64 * i + lane;
+      const int seen1 = seen + __popcll(me);
+      at += __popcll(mg) + min(seen1, ties) - min(seen, ties);
+      seen = seen1;
+    }
+    base += ga + min(eq + ea, ties) - min(eq, ties);
+    eq += ea;
     __syncthreads();
   }
 }
@@ -519,16 +688,33 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // One block of 4 waves per (item, part of its pages): the waves take batches of
 // pages in turn, each with an online softmax of its own, and are merged in LDS.
 // As in k_attn_bf16 the G q-heads of the kv-head are the columns of both products:
-//   S^T[16 tok x 16 heads] = K[16 x D] Q^T,   O^T[D x 16 heads] += V^T[D x 16 tok] P^T.
-// bf16: P goes into the second product as the sum of two bf16 values (what the
-// first leaves over goes into the second, a relative error of 2^-18): the products
-// are idle anyway while the pages come in. fp32: fp32 matrix cores throughout.
-// Tokens behind the row's own position get score -inf, and their V counts as 0
-// (those rows may hold anything).
+//   S^T[16 tok x 16 heads] = K[16 x D] Q^T,   O^T[D x 16 heads] += V^T[D x 32 tok] P^T,
+// and the softmax's reference moves only when a score exceeds it by 8 (weights stay
+// within 2^8), so that the common page needs no rescaling.
+// bf16: a batch is two pages, which the second product takes at once: its inner
+// dimension holds four tokens of the one and four of the other per lane, which is
+// where the scores' registers and V's 16-byte units have them. P goes in as the sum
+// of two bf16 values (what the first leaves over goes into the second, a relative
+// error of 2^-17): the matrix cores are idle anyway while the pages come in. fp32:
+// one page, fp32 matrix cores throughout.
+// A wave holds the physical ids of its pages (64 at a time) one per lane, so that no
+// batch waits for a chain of list and page table, and loads a batch while it works
+// on the one before.
+// Tokens behind the row's own position get weight 0, and their V counts as 0 (those
+// rows may hold anything).
 template <bool BF16, int NU>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) void k_attend(AttendArgs a) {
+struct PageRegs {
+  static constexpr int NB = BF16 ? 2 : 1;
+  u32x4 k[NB][NU];
+  u32x4 v[BF16 ? NB : 1][BF16 ? NU : 1];
+  float vf[BF16 ? 1 : NU][4];
+};
+
+template <bool BF16, int NU>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU > 6 ? 1 : 2, 4))) void k_attend(AttendArgs a) {
+  using Regs = PageRegs<BF16, NU>;
   constexpr int NJ = BF16 ? 2 * NU : NU;  // 16-dim output blocks
-  constexpr int NB = 2;                   // pages per batch
+  constexpr int NB = Regs::NB;            // pages per batch
   constexpr int DP = 16 * NJ + 4;
   __shared__ __align__(16) float sacc[4][kMaxGroup][DP];
   __shared__ float sm[4][kMaxGroup], sl[4][kMaxGroup];
@@ -543,6 +729,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
   const bool chosen = it.pages > a.n_pages;
   const int32_t* list = chosen ? page_list(a, it, item) : nullptr;
   const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
+  // the wave's u-th page is page (u / NB) 4 NB + NB wave + u % NB of the part
+  auto nth = [&](int u) { return u / NB * 4 * NB + NB * wave + u % NB; };
+  int my_page = 0, my_phys = 0;
+  auto ids = [&](int u0) {  // lane i: the wave's page u0 + i (past the part's end its last one)
+    const int i = c0 + min(nth(u0 + lane), cnt - 1);
+    my_page = chosen ? list[i] : i;
+    my_phys = pt[my_page];
+  };
+  ids(0);
   const int call_l = a.layer - a.layer0 + it.l;
   const size_t qrow = ((it.row * a.n_layers + call_l) * a.n_q_heads + (size_t)it.h * G + min(col, G - 1)) * D;
   u32x4 q[NU];
@@ -557,115 +752,139 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
   }
   const size_t lay = (size_t)(a.layer + it.l) * a.max_pages;
   const size_t tile = (size_t)kPage * D;
-  f32x4 acc[NJ];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = kNegInf, lsum = 0.f;
-  for (int k0 = NB * wave; k0 < cnt; k0 += 4 * NB) {
-    u32x4 kb[NB][NU], vb[NB][BF16 ? NU : 4];
-    float vf[NB][BF16 ? 1 : NU][4];
-    int lim[NB];
+  auto load = [&](int u, Regs& r) __attribute__((always_inline)) {  // pages u .. u + NB - 1 of those in the lanes
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int i = c0 + min(k0 + b, cnt - 1);
-      const int page = __builtin_amdgcn_readfirstlane(chosen ? list[i] : i);
-      const int phys = __builtin_amdgcn_readfirstlane(pt[page]);
-      // tokens of the page that count (a batch's slots past the part's pages: none)
-      lim[b] = k0 + b < cnt ? min(it.pos + 1 - kPage * page, kPage) : 0;
-      const size_t t = ((lay + phys) * a.n_kv_heads + it.h) * tile;
+      const size_t t = ((lay + __builtin_amdgcn_readlane(my_phys, u + b)) * a.n_kv_heads + it.h) * tile;
       if constexpr (BF16) {
         const u32x4* kp = (const u32x4*)((const uint16_t*)a.kpool + t) + lane;
         const u32x4* vp = (const u32x4*)((const uint16_t*)a.vpool + t) + lane;
 #pragma unroll
-        for (int i2 = 0; i2 < NU; ++i2) { kb[b][i2] = kp[64 * i2]; vb[b][i2] = vp[64 * i2]; }
+        for (int i = 0; i < NU; ++i) r.k[b][i] = kp[64 * i];
+#pragma unroll
+        for (int i = 0; i < NU; ++i) r.v[b][i] = vp[64 * i];
       } else {
         const float* kp = (const float*)a.kpool + t + (size_t)col * D;
         const float* vp = (const float*)a.vpool + t;
 #pragma unroll
-        for (int i2 = 0; i2 < NU; ++i2) {
-          kb[b][i2] = *(const u32x4*)(kp + min(16 * i2 + 4 * quad, D - 4));
+        for (int i = 0; i < NU; ++i) r.k[b][i] = *(const u32x4*)(kp + min(16 * i + 4 * quad, D - 4));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) vf[b][i2][r] = vp[(size_t)(4 * quad + r) * D + min(16 * i2 + col, D - 1)];
-        }
+        for (int i = 0; i < NU; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.vf[i][e] = vp[(size_t)(4 * quad + e) * D + min(16 * i + col, D - 1)];
       }
     }
+  };
+  f32x4 acc[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kNegInf, lsum = 0.f;
+  auto work = [&](int u, int k0, Regs& r) __attribute__((always_inline)) {
     f32x4 c[NB];
+    int lim[NB];  // tokens of the page that count (a batch's slots past the part's end: none)
     float top = kNegInf;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      const int page = __builtin_amdgcn_readlane(my_page, u + b);
+      lim[b] = k0 + b < cnt ? min(it.pos + 1 - kPage * page, kPage) : 0;
       c[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < NU; ++i) {
         if constexpr (BF16) {
-          c[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kb[b][i]),
+          c[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r.k[b][i]),
                                                          __builtin_bit_cast(bf16x8, q[i]), c[b], 0, 0, 0);
         } else {
           const bool in = 16 * i + 4 * quad < D;  // (dims past D: 0 x 0)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            c[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? __uint_as_float(kb[b][i][e]) : 0.f,
+            c[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? __uint_as_float(r.k[b][i][e]) : 0.f,
                                                         __uint_as_float(q[i][e]), c[b], 0, 0, 0);
         }
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        c[b][r] = 4 * quad + r < lim[b] ? c[b][r] * a.scale_log2 : kNegInf;
-        top = fmaxf(top, c[b][r]);
-      }
-    }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float mn = fmaxf(m, top), alpha = m == mn ? 1.f : exp2f(m - mn);
-    m = mn;
-    lsum *= alpha;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      float pr[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        pr[r] = 4 * quad + r < lim[b] ? exp2f(c[b][r] - m) : 0.f;
-        lsum += pr[r];
-      }
+      for (int e = 0; e < 4; ++e) c[b][e] *= a.scale_log2;
       if (lim[b] < kPage) {  // uniform
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (4 * quad + r >= lim[b]) {
-            if constexpr (BF16) {
-              const uint32_t keep = ~(0xFFFFu << (16 * (r & 1)));
+        for (int e = 0; e < 4; ++e) {
+          if (4 * quad + e < lim[b]) continue;
+          c[b][e] = kNegInf;
+          if constexpr (BF16) {
+            const uint32_t keep = ~(0xFFFFu << (16 * (e & 1)));
 #pragma unroll
-              for (int i = 0; i < NU; ++i) { vb[b][i][r >> 1] &= keep; vb[b][i][2 + (r >> 1)] &= keep; }
-            } else {
+            for (int i = 0; i < NU; ++i) { r.v[b][i][e >> 1] &= keep; r.v[b][i][2 + (e >> 1)] &= keep; }
+          } else {
 #pragma unroll
-              for (int i = 0; i < NU; ++i) vf[b][i][r] = 0.f;
-            }
+            for (int i = 0; i < NU; ++i) r.vf[i][e] = 0.f;
           }
+        }
       }
-      if constexpr (BF16) {
-        s16x4 ph, pl;
+      top = fmaxf(top, fmaxf(fmaxf(c[b][0], c[b][1]), fmaxf(c[b][2], c[b][3])));
+    }
+    if (__any(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      lsum *= alpha;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const __bf16 x = (__bf16)pr[r];
-          ph[r] = __builtin_bit_cast(short, x);
-          pl[r] = __builtin_bit_cast(short, (__bf16)(pr[r] - (float)x));
+      for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
+    }
+    // a column whose scores so far are all -inf keeps the reference -inf: its weights, 2^(-inf + inf), are NaN,
+    // as the softmax of nothing but -inf is; slots and tokens that do not count weigh 0 all the same
+    float p[NB][4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f(c[b][e] - m);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (lim[b] < kPage)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[b][e] = 4 * quad + e < lim[b] ? p[b][e] : 0.f;
+      lsum += (p[b][0] + p[b][1]) + (p[b][2] + p[b][3]);
+    }
+    if constexpr (BF16) {
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          hi[4 * b + e] = (__bf16)p[b][e];
+          lo[4 * b + e] = (__bf16)(p[b][e] - (float)hi[4 * b + e]);
         }
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-          const s16x4 v0 = __builtin_bit_cast(s16x4, uint2{vb[b][i][0], vb[b][i][1]});
-          const s16x4 v1 = __builtin_bit_cast(s16x4, uint2{vb[b][i][2], vb[b][i][3]});
-          acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v0, ph, acc[2 * i], 0, 0, 0);
-          acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v1, ph, acc[2 * i + 1], 0, 0, 0);
-          acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v0, pl, acc[2 * i], 0, 0, 0);
-          acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v1, pl, acc[2 * i + 1], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int i = 0; i < NU; ++i)
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[b][i][r], pr[r], acc[i], 0, 0, 0);
+      for (int i = 0; i < NU; ++i) {
+        const bf16x8 v0 = __builtin_bit_cast(bf16x8, u32x4{r.v[0][i][0], r.v[0][i][1], r.v[1][i][0], r.v[1][i][1]});
+        const bf16x8 v1 = __builtin_bit_cast(bf16x8, u32x4{r.v[0][i][2], r.v[0][i][3], r.v[1][i][2], r.v[1][i][3]});
+        acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, hi, acc[2 * i], 0, 0, 0);
+        acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, hi, acc[2 * i + 1], 0, 0, 0);
+        acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, lo, acc[2 * i], 0, 0, 0);
+        acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, lo, acc[2 * i + 1], 0, 0, 0);
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < NU; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(r.vf[i][e], p[0][e], acc[i], 0, 0, 0);
+    }
+  };
+  // two batches of registers in turn; ids are read again every 64 pages of the wave, when
+  // the next batch is the first of the new ones (64 / NB batches: an even number)
+  Regs ra, rb;
+  if (NB * wave < cnt) load(0, ra);
+  for (int v0 = 0, k0 = NB * wave; k0 < cnt; v0 += 64) {
+    for (int u = 0; u < 64 && k0 < cnt; u += 2 * NB) {
+      const int page_k1 = k0 + 4 * NB, page_k2 = k0 + 8 * NB;
+      if (page_k1 < cnt) load(u + NB, rb);
+      work(u, k0, ra);
+      const bool turn = u + 2 * NB == 64;
+      if (page_k2 < cnt && !turn) load(u + 2 * NB, ra);
+      if (page_k1 < cnt) work(u + NB, page_k1, rb);
+      if (page_k2 < cnt && turn) {
+        ids(v0 + 64);
+        load(0, ra);
+      }
+      k0 = page_k2;
     }
   }
   lsum += __shfl_xor(lsum, 16);
@@ -748,14 +967,22 @@ hipError_t launch_summarize(const SummaryArgs& a, bool bf16, hipStream_t st) {
 }
 
 hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, const Timing* tm) {
-  const size_t items = (size_t)a.n_groups * a.gt * a.launch_layers * a.n_kv_heads;
-  if (score) {
-    const size_t blocks = items / a.gt * a.chunks;
-    if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
-    const hipError_t e = go(k_page_score, dim3((unsigned)blocks), dim3(256), 0, st, t0(tm), nullptr, a);
-    if (e != hipSuccess) return e;
+  const size_t items = (size_t)a.n_groups * a.gt * a.launch_layers * a.n_kv_heads, groups = items / a.gt;
+  if (items > 0x7FFFFFFFu || groups * a.chunks > 0x7FFFFFFFu) return hipErrorInvalidValue;
+  const int pages = a.score_row;
+  if (!score || pages <= kPickPages) {
+    const dim3 grid((unsigned)groups);
+    if (!score || pages <= 128) return go(k_page_pick<2>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
+    if (pages <= 256) return go(k_page_pick<4>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
+    return go(k_page_pick<8>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
   }
-  return go(k_page_select, dim3((unsigned)items), dim3(256), 0, st, score ? nullptr : t0(tm), t1(tm), a);
+  const hipError_t e = go(k_page_score, dim3((unsigned)(groups * a.chunks)), dim3(256), 0, st, t0(tm), nullptr, a);
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)items);
+  if (pages <= 2048) return go(k_page_select<2, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
+  if (pages <= 8192) return go(k_page_select<8, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
+  if (pages <= 16384) return go(k_page_select<16, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
+  return go(k_page_select<16, true>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
 }
 
 hipError_t launch_attend(const AttendArgs& a, hipStream_t st, const Timing* tm, const Timing* tm_merge) {

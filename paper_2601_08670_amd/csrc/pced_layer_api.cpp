@@ -85,7 +85,7 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
   a.part_pages = p.part_pages;
   const double es = (double)esize_of(cfg);
   double sums = 0, kv = 0;  // pages scored and attended to, per layer and kv-head
-  for (int s = 0; s < c->S; ++s)
+  for (int s = 0; c->prof && s < c->S; ++s)
     for (int i = 0; i < a.n_tokens; ++i) {
       const int n = (c->len[s] + i) / kPage + 1;
       if (n > a.n_pages) sums += n;
