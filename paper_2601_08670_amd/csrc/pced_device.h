@@ -52,6 +52,23 @@ __device__ __forceinline__ uint4 ld_w(const uint4* p) {
 // element e (of 8) of a 16-byte row piece
 __device__ __forceinline__ uint32_t el16(const u32x4& v, int e) { return (v[e >> 1] >> (16 * (e & 1))) & 0xFFFFu; }
 
+// Run r of a bf16 V tile (see k_load): kv-head, token quad and first dim
+struct RunPos {
+  int g, q, d0;
+};
+__device__ __forceinline__ RunPos run_pos(int run, int D) {
+  const int rpt = D / 4, r = run % rpt;
+  return RunPos{run / rpt, (r >> 1) & 3, 32 * (r >> 3) + 8 * (r & 1)};
+}
+
+// This wave's LDS accesses so far are complete and ordered before the next ones
+// (other lanes' data is read next).
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Launch; timing events, when given, are attached to the dispatch itself
 // (start when the kernel begins, stop when it completes), so they measure the
 // kernel and not the queue around it.

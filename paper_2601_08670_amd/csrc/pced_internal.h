@@ -321,9 +321,9 @@ struct ReadCacheArgs {
 };
 
 constexpr int kSumExp = 64;        // page summaries: scales are 2^-kSumExp .. 2^kSumExp
+constexpr int kAttendPart = 256;   // pages of a part of an item, at most (64 per wave)
 constexpr int kPickPages = 512;    // pages whose bounds and choice are one launch, at most
-constexpr int kScorePages = 256;   // pages per work-group of the bounds beyond that
-constexpr int kAttendTokens = 16;  // new tokens of a sequence that are scored together, at most
+constexpr int kAttendTokens = 8;   // new tokens of a sequence that are scored together, at most
 inline int summary_row(int head_dim) { return (2 * head_dim + 63) / 64 * 64; }  // bytes of a page's codes
 
 // New rows of every sequence into the paged pool, K and q rotated (see pced_append).
@@ -341,6 +341,7 @@ struct AppendRowsArgs {
   float* scale;             // [L][Hkv][max_pages]
   int n_seqs, n_tokens, layer0, n_layers, n_q_heads, n_kv_heads, head_dim, max_pages, maxpps, t, sum_row;
   int slots;                // pages that a sequence's rows touch, at most
+  int q_blocks;             // work-groups of the q rows per page (set by launch_append_rows)
   int rot_dim, halves;
   double log2_theta;
 };
@@ -374,8 +375,11 @@ struct AttendArgs {
   int t, n_tokens, gt, seq_groups, group0, n_groups, layer0, n_layers, layer, launch_layers;
   int n_q_heads, n_kv_heads, group, head_dim, max_pages, maxpps, sum_row, bf16;
   int n_pages, first, last;
-  int score_row, chunks;    // pages of a score row (whole 16s); blocks of kScorePages that cover them
+  int score_row;            // pages of a score row (whole 16s)
+  int chunks, chunk_pages;  // pages per work-group of the bounds (whole 128s), work-groups that cover them
   int parts, part_pages;    // parts of an item's pages, and pages per part
+  int launch_seqs;          // sequences of the launch's groups (set by launch_attend)
+  int num_cus;
   float scale_log2;         // log2(e) / sqrt(D)
 };
 
@@ -400,8 +404,9 @@ hipError_t launch_beta(const BetaArgs& a, int n_seqs, int n_exp, bool sums, hipS
 // k_fuse (timed by tm) then the per-query merge k_fuse_final (timed by tm_merge)
 hipError_t launch_fuse(const FuseArgs& a, int n_queries, hipStream_t st, const Timing* tm = nullptr,
                        const Timing* tm_merge = nullptr);
-// k_fuse_adjusted (a.nblk = adjusted_slices(V)) then k_fuse_final
-int adjusted_slices(int V);
+// vocabulary tokens per work-group of k_fuse_adjusted
+int adjusted_slice(int V, int n_queries, int num_cus);
+// k_fuse_adjusted (a.nblk slices) then k_fuse_final
 hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st,
                                 const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
 hipError_t launch_adjust(const AdjustArgs& a, int n_queries, int max_rows, int num_cus, hipStream_t st);

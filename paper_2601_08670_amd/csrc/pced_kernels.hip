@@ -55,13 +55,6 @@ typedef unsigned u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 // K units are whole on both sides. A V run is 4 x 2 row pieces, transposed in
 // registers, and reaches (or leaves) the pool-side order through the wave's own
 // 8 KiB of LDS, units XOR-swizzled against bank conflicts.
-struct RunPos {
-  int g, q, d0;
-};
-__device__ __forceinline__ RunPos run_pos(int run, int D) {
-  const int rpt = D / 4, r = run % rpt;
-  return RunPos{run / rpt, (r >> 1) & 3, 32 * (r >> 3) + 8 * (r & 1)};
-}
 struct UnitPos {
   int g, t, d;
 };
@@ -69,14 +62,6 @@ __device__ __forceinline__ UnitPos kunit_pos(int n, int D) {
   const int upt = 2 * D, u = n % upt;
   return UnitPos{n / upt, u & 15, 32 * (u >> 6) + 8 * ((u >> 4) & 3)};
 }
-// This wave's LDS accesses so far are complete and ordered before the next ones
-// (other lanes' data is read next).
-__device__ __forceinline__ void wave_lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Loading: one wave per (item, layer, 64 runs), items being (sequence, logical
 // page) pairs, or with a.items null consecutive pages of sequence a.one_s from
 // page a.page0 on, whose rows (all layers, a.one_len tokens per layer, from token
@@ -2252,20 +2237,20 @@ template <int SW>
 __device__ __forceinline__ void adjust_slice(const AdjustArgs& a, int b, int vb, AdjustLds<SW>& L) {
   for (int i = threadIdx.x; i < SW; i += 256) L.cnt[i] = L.bias[i] = 0;
   __syncthreads();
-  if (a.history) {
-    const int e1 = min(a.history_off[b + 1], a.n_history);
-    for (int e = max(a.history_off[b], 0) + threadIdx.x; e < e1; e += 256) {
-      const int v = a.history[e];
-      if (v >= vb && v < a.V && v - vb < SW) atomicAdd(&L.cnt[v - vb], 1);
+  // (four entries of a thread at once)
+  auto scan = [&](const int32_t* list, const int32_t* off, int size, auto&& take) __attribute__((always_inline)) {
+    const int e0 = max(off[b], 0), e1 = min(off[b + 1], size);
+    for (int e = e0 + (int)threadIdx.x; e < e1; e += 1024) {
+      int v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = list[min(e + 256 * j, e1 - 1)];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e + 256 * j < e1 && v[j] >= vb && v[j] < a.V && v[j] - vb < SW) take(v[j] - vb, e + 256 * j);
     }
-  }
-  if (a.bias_token) {
-    const int e1 = min(a.bias_off[b + 1], a.n_bias);
-    for (int e = max(a.bias_off[b], 0) + threadIdx.x; e < e1; e += 256) {
-      const int v = a.bias_token[e];
-      if (v >= vb && v < a.V && v - vb < SW) atomicMax(&L.bias[v - vb], e + 1);
-    }
-  }
+  };
+  if (a.history) scan(a.history, a.history_off, a.n_history, [&](int i, int) { atomicAdd(&L.cnt[i], 1); });
+  if (a.bias_token) scan(a.bias_token, a.bias_off, a.n_bias, [&](int i, int e) { atomicMax(&L.bias[i], e + 1); });
   __syncthreads();
 }
 // four tokens from vb + i on (bits of seen and open: one per token)
@@ -2273,8 +2258,15 @@ struct AdjustTok4 {
   float rep, pres, shift[4], bias[4];
   uint32_t seen, open;
 };
+// which of the tokens v .. v + 3 (v a multiple of 4) the mask leaves open
+__device__ __forceinline__ uint32_t open_tokens(const AdjustArgs& a, int b, int v) {
+  if (v >= a.V) return 0u;
+  const uint32_t in = a.V - v >= 4 ? 15u : (1u << (a.V - v)) - 1u;
+  return a.mask ? (a.mask[(size_t)b * a.mask_row + (v >> 5)] >> (v & 31)) & in : in;
+}
 template <int SW>
-__device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, int vb, int i, const AdjustLds<SW>& L) {
+__device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, uint32_t open, int i,
+                                                  const AdjustLds<SW>& L) {
 #pragma clang fp contract(off)
   AdjustTok4 t;
   t.rep = a.repetition ? a.repetition[b] : 1.f;
@@ -2288,8 +2280,7 @@ __device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, in
     t.bias[c] = e > 0 ? a.bias_value[e - 1] : 0.f;
     t.seen |= (n > 0 ? 1u : 0u) << c;
   }
-  const int v = vb + i;  // a multiple of 4
-  t.open = v >= a.V ? 0u : a.mask ? (a.mask[(size_t)b * a.mask_row + (v >> 5)] >> (v & 31)) & 15u : 15u;
+  t.open = open;
   return t;
 }
 template <bool MASK>
@@ -2308,47 +2299,67 @@ __device__ __forceinline__ void adjust4(const AdjustTok4& t, float (&x)[4]) {
 
 // Rows of adjusted logits: a block per (slice of 1024 tokens, row group of a query).
 // A thread has four neighbouring tokens of every row, a 16-byte load and store each
-// (at any 4-byte address). Bound: HBM, every logit read and written once.
+// (at any 4-byte address), four rows at a time, the first of them on their way while
+// the lists are read. Where the mask closes all four nothing is read. Bound: HBM,
+// every logit read (if it matters) and written once.
 __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
-  constexpr int SW = 1024;
+  constexpr int SW = 1024, U = 4;
   __shared__ AdjustLds<SW> lds;
   const int b = blockIdx.y, vb = blockIdx.x * SW, i = 4 * threadIdx.x, v = vb + i;
   const int s0 = a.query_seq0[b], n = a.query_seq0[b + 1] - s0;
   const int r0 = blockIdx.z * a.rows_per_block, r1 = min(n, r0 + a.rows_per_block);
   if (r0 >= r1) return;
+  const uint32_t open = open_tokens(a, b, v);
+  const int o = v - min(v, max(a.V - 4, 0));  // a row's last load starts at V - 4 (V >= 4)
+  f32x4 w[U];
+  auto load = [&](int r) __attribute__((always_inline)) {
+    if (!open) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float* row = a.logits + (size_t)(s0 + min(r + u, r1 - 1)) * a.V;
+      if (a.V >= 4) w[u] = *(const f32x4_a4*)(row + v - o);
+      else w[u] = f32x4{row[0], row[1], row[a.V - 1], 0.f};
+    }
+  };
+  load(r0);
   adjust_slice<SW>(a, b, vb, lds);
   if (v >= a.V) return;
-  const AdjustTok4 t = adjust_tok4<SW>(a, b, vb, i, lds);
-  const size_t at = (size_t)(s0 + r0) * a.V + v;
-  if (v + 4 <= a.V) {
-    for (int r = r0; r < r1; ++r) {
-      const size_t o = at + (size_t)(r - r0) * a.V;
-      const f32x4 w = *(const f32x4_a4*)(a.logits + o);
-      float x[4] = {w[0], w[1], w[2], w[3]};
-      adjust4<true>(t, x);
-      *(f32x4_a4*)(a.out + o) = f32x4{x[0], x[1], x[2], x[3]};
-    }
-  } else {
-    for (int r = r0; r < r1; ++r) {
-      const size_t o = at + (size_t)(r - r0) * a.V;
+  const AdjustTok4 t = adjust_tok4<SW>(a, b, open, i, lds);
+  for (int r = r0; r < r1; r += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r + u >= r1) break;
       float x[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x[c] = a.logits[min(o + c, (size_t)(s0 + r + 1) * a.V - 1)];
+      for (int c = 0; c < 4; ++c) x[c] = w[u][c];
+      if (o > 0) {  // the row's last tokens: from place o of the load on
+        x[0] = o == 1 ? w[u][1] : o == 2 ? w[u][2] : w[u][3];
+        x[1] = o == 1 ? w[u][2] : w[u][3];
+        x[2] = w[u][3];
+      }
       adjust4<true>(t, x);
+      float* out = a.out + (size_t)(s0 + r + u) * a.V + v;
+      if (v + 4 <= a.V) {
+        *(f32x4_a4*)out = f32x4{x[0], x[1], x[2], x[3]};
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (v + c < a.V) a.out[o + c] = x[c];
+        for (int c = 0; c < 3; ++c)
+          if (v + c < a.V) out[c] = x[c];
+      }
     }
+    if (r + U < r1) load(r + U);
   }
 }
 
 // k_fuse over adjusted logits, which are not stored: Eq. 2 and the best two tokens
-// of a slice. Tokens that the mask closes, and scores that are NaN or -inf, are
-// nobody's choice: a slice without any other has no candidate (expert 0).
-template <bool VEC>
+// of a slice of SW tokens, a lane holding RI times four neighbouring ones. Tokens that
+// the mask closes, and scores that are NaN or -inf, are nobody's choice: a slice without
+// any other has no candidate (expert 0). Where the mask closes all four nothing is read;
+// the first rows are on their way while the lists are read.
+template <bool VEC, int SW>
 __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
 #pragma clang fp contract(off)
-  constexpr int SW = 256, NB = 4;
+  constexpr int RI = SW / 256, NB = 4;
   __shared__ AdjustLds<SW> lds;
   __shared__ float sbest[4][SW];
   __shared__ int sk[4][SW];
@@ -2361,59 +2372,88 @@ __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d)
   const int e0 = inl ? a.inl_exp0[b] : a.query_exp0[b];
   const int per = (N + 3) / 4;                       // experts per wave
   const int k_lo = 1 + wave * per, k_hi = min(N, k_lo + per - 1);
-  const int vb = blockIdx.x * SW, v = vb + 4 * lane;
+  const int vb = blockIdx.x * SW, v0 = vb + 4 * lane;
   const float* L0 = a.logits + (size_t)s0 * a.V;
-  adjust_slice<SW>(d, b, vb, lds);
-  const AdjustTok4 t = adjust_tok4<SW>(d, b, vb, 4 * lane, lds);
-  auto load = [&](const float* row, float (&x)[4]) {
-    const float4 w = load_tok4<VEC>(row, v, a.V);
-    x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+  uint32_t open[RI];
+#pragma unroll
+  for (int i = 0; i < RI; ++i) open[i] = open_tokens(d, b, v0 + 256 * i);
+  auto load = [&](const float* row, float (&x)[RI][4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < RI; ++i) {
+      if (!open[i]) continue;
+      const float4 w = load_tok4<VEC>(row, v0 + 256 * i, a.V);
+      x[i][0] = w.x; x[i][1] = w.y; x[i][2] = w.z; x[i][3] = w.w;
+    }
   };
-  float sa[4], best[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
-  int bk[4] = {0, 0, 0, 0};
-  load(L0, sa);
-  adjust4<false>(t, sa);
-  for (int kb = k_lo; kb <= k_hi; kb += NB) {
-    float x[NB][4], cb[NB], cp[NB];
+  float sa[RI][4], x[NB][RI][4], cb[NB], cp[NB];
+  auto load_batch = [&](int kb) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const int k = min(kb + j, k_hi);
+      const int k = max(min(kb + j, k_hi), 1);  // (a wave without experts: the first one's row)
       load(L0 + (size_t)k * a.V, x[j]);
       cb[j] = a.beta[e0 + k - 1];
       cp[j] = a.prior[e0 + k - 1];
     }
+  };
+  load(L0, sa);
+  load_batch(k_lo);
+  adjust_slice<SW>(d, b, vb, lds);
+  float best[RI][4];
+  int bk[RI][4];
+  bool touched[RI];  // some token of the wave's is in the lists (most slices of most vocabularies have few)
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int k = kb + j;
-      adjust4<false>(t, x[j]);
+  for (int i = 0; i < RI; ++i) {
+    const AdjustTok4 t = adjust_tok4<SW>(d, b, open[i], 256 * i + 4 * lane, lds);
+    touched[i] = __any(t.seen || t.bias[0] != 0.f || t.bias[1] != 0.f || t.bias[2] != 0.f || t.bias[3] != 0.f);
+    if (touched[i]) adjust4<false>(t, sa[i]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float t1 = (1.0f + cb[j]) * x[j][c];
-        const float t2 = cb[j] * sa[c];
-        const float val = (t1 - t2) + cp[j];
-        const bool up = k <= k_hi && (t.open >> c & 1) && val > best[c];
-        best[c] = up ? val : best[c];
-        bk[c] = up ? k : bk[c];
+    for (int c = 0; c < 4; ++c) { best[i][c] = kNegInf; bk[i][c] = 0; }
+  }
+  for (int kb = k_lo; kb <= k_hi; kb += NB) {
+#pragma unroll
+    for (int i = 0; i < RI; ++i) {
+      if (touched[i]) {
+        const AdjustTok4 t = adjust_tok4<SW>(d, b, open[i], 256 * i + 4 * lane, lds);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) adjust4<false>(t, x[j][i]);
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (kb + j > k_hi) break;  // uniform
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float t1 = (1.0f + cb[j]) * x[j][i][c];
+          const float t2 = cb[j] * sa[i][c];
+          const float val = (t1 - t2) + cp[j];
+          const bool up = val > best[i][c];
+          best[i][c] = up ? val : best[i][c];
+          bk[i][c] = up ? kb + j : bk[i][c];
+        }
       }
     }
+    if (kb + NB <= k_hi) load_batch(kb + NB);
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    sbest[wave][4 * lane + c] = best[c];
-    sk[wave][4 * lane + c] = bk[c];
-  }
+  for (int i = 0; i < RI; ++i)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool in = open[i] >> c & 1;
+      sbest[wave][256 * i + 4 * lane + c] = in ? best[i][c] : kNegInf;
+      sk[wave][256 * i + 4 * lane + c] = in ? bk[i][c] : 0;
+    }
   __syncthreads();
   Top2 cand{kNegInf, 0x7FFFFFFF, 0, kNegInf, 0x7FFFFFFF};
-  {
-    const int u = threadIdx.x;
-    float x = sbest[0][u];
+#pragma unroll
+  for (int i = 0; i < RI; ++i) {
+    const int u = threadIdx.x + 256 * i;
+    float y = sbest[0][u];
     int k = sk[0][u];
 #pragma unroll
     for (int w = 1; w < 4; ++w) {
-      const float y = sbest[w][u];
-      if (y > x) { x = y; k = sk[w][u]; }
+      const float yw = sbest[w][u];
+      if (yw > y) { y = yw; k = sk[w][u]; }
     }
-    if (vb + u < a.V && k > 0) cand = Top2{x, vb + u, k, kNegInf, 0x7FFFFFFF};
+    if (vb + u < a.V && k > 0) cand = merge(cand, Top2{y, vb + u, k, kNegInf, 0x7FFFFFFF});
   }
   cand = wave_top2(cand);
   if (lane == 0) swave[wave] = cand;
@@ -4035,14 +4075,17 @@ hipError_t launch_agg(const AggArgs& a, int n_exp, int n_queries, hipStream_t st
              : go(k_agg<false, false>, g, dim3(256), 0, st, nullptr, t1(tm), a);
 }
 
-int adjusted_slices(int V) { return (V + 255) / 256; }
+int adjusted_slice(int V, int n_queries, int num_cus) {
+  return (long)n_queries * ((V + 511) / 512) >= 2L * num_cus ? 512 : 256;
+}
 
 hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st, const Timing* tm,
                                 const Timing* tm_merge) {
-  const dim3 g(a.nblk, n_queries);
-  const bool vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;  // (V >= 2)
-  const hipError_t e = vec ? go(k_fuse_adjusted<true>, g, dim3(256), 0, st, t0(tm), t1(tm), a, d)
-                                                : go(k_fuse_adjusted<false>, g, dim3(256), 0, st, t0(tm), t1(tm), a, d);
+  // a.nblk: slices of adjusted_slice() tokens
+  const bool wide = (a.V + a.nblk - 1) / a.nblk > 256, vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;  // (V >= 2)
+  auto run = [&](auto kernel) { return go(kernel, dim3(a.nblk, n_queries), dim3(256), 0, st, t0(tm), t1(tm), a, d); };
+  const hipError_t e = wide ? (vec ? run(k_fuse_adjusted<true, 512>) : run(k_fuse_adjusted<false, 512>))
+                            : (vec ? run(k_fuse_adjusted<true, 256>) : run(k_fuse_adjusted<false, 256>));
   if (e != hipSuccess) return e;
   return go(k_fuse_final, dim3(n_queries), dim3(kFuseBlock), 0, st, t0(tm_merge), t1(tm_merge), a);
 }
@@ -4050,9 +4093,10 @@ hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_qu
 hipError_t launch_adjust(const AdjustArgs& a0, int n_queries, int max_rows, int num_cus, hipStream_t st) {
   AdjustArgs a = a0;
   const int slices = (a.V + 1023) / 1024;
-  a.rows_per_block = max_rows;
+  // rows per work-group: all of a query's, or as few as make four work-groups per compute unit
+  const long groups = (long)slices * n_queries, want = (4L * num_cus + groups - 1) / groups;
+  a.rows_per_block = (int)((max_rows + want - 1) / want);
   const dim3 g(slices, n_queries, (max_rows + a.rows_per_block - 1) / a.rows_per_block);
-  (void)num_cus;
   return go(k_adjust, g, dim3(256), 0, st, nullptr, nullptr, a);
 }
 

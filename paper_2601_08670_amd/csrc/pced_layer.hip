@@ -150,14 +150,18 @@ struct Slot {
   }
 };
 
-// A slot's unit(s) of a row, rotated: (a, b) -> (a cos - b sin, a sin + b cos) in fp32
+// A slot's unit(s) of a row
 template <bool BF16>
-__device__ __forceinline__ void turned(const char* row, const Slot<BF16>& sl, const float2* cs, int rot, bool turn,
-                                       u32x4& o1, u32x4& o2) {
-  constexpr int N = Unit<BF16>::N, es = BF16 ? 2 : 4;
+__device__ __forceinline__ void load_slot(const char* row, const Slot<BF16>& sl, u32x4& o1, u32x4& o2) {
+  constexpr int es = BF16 ? 2 : 4;
   o1 = *(const u32x4*)(row + (size_t)sl.d * es);
-  if (sl.d2 >= 0) o2 = *(const u32x4*)(row + (size_t)sl.d2 * es);
-  if (!turn || sl.d >= rot) return;
+  o2 = *(const u32x4*)(row + (size_t)(sl.d2 >= 0 ? sl.d2 : sl.d) * es);
+}
+// Rotated: (a, b) -> (a cos - b sin, a sin + b cos) in fp32, rounded once
+template <bool BF16>
+__device__ __forceinline__ void turn_slot(const Slot<BF16>& sl, const float2* cs, int rot, u32x4& o1, u32x4& o2) {
+  constexpr int N = Unit<BF16>::N;
+  if (sl.d >= rot) return;
   Unit<BF16> x;
   x.set(o1);
   if (sl.d2 >= 0) {
@@ -184,120 +188,255 @@ __device__ __forceinline__ void turned(const char* row, const Slot<BF16>& sl, co
   o1 = x.get();
 }
 
-// One block per (sequence, page that the sequence's new tokens touch, layer). The
-// page's K units are written by token pairs and its V runs by token quads, so that
-// only whole 32-byte sectors are stored (see k_append): tokens of the sector that
-// are not new keep what they hold. The angles' cos and sin, in fp64 and rounded
-// once, are made by the block for its at most 16 positions and shared by its
-// heads. A page that becomes full is summarised by the block that filled it.
+// For every (sequence, page that the sequence's new tokens touch, layer) one block for
+// K, one for V, and blocks of kAppendTasks slots for the q rows. A page that is new from
+// end to end is written in contiguous 1 KiB wave stores, V through LDS (as in k_load);
+// of other pages the K units are written by token pairs and the V runs by token quads,
+// so that only whole 32-byte sectors are stored (see k_append): tokens of the sector
+// that are not new keep what they hold. The
+// angles' cos and sin, in fp64 and rounded once, are made by the block for its at most
+// 16 positions and shared by its heads, while the rows' first loads are under way
+// (several slots of a thread at once: a store may not pass a later slot's load). A page
+// that becomes full is summarised by the block that filled it. Bound: HBM for many
+// tokens, the chain of length, rows and stores for one.
+constexpr int kAppendTasks = 1024;
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
   constexpr int N = Unit<BF16>::N, es = BF16 ? 2 : 4;
-  __shared__ float2 cs[kPage][64];
+  __shared__ union {
+    struct {
+      float2 cs[kPage][64];
+      double turn_of[64];
+    } t;
+    uint4 v[BF16 ? 4 : 1][BF16 ? 512 : 1];
+  } lds;
+  auto& cs = lds.t.cs;
+  auto& turn_of = lds.t.turn_of;
   const int tid = threadIdx.x;
-  const int l = blockIdx.x / (a.n_seqs * a.slots), rest = blockIdx.x - l * a.n_seqs * a.slots;
-  const int s = rest / a.slots;
-  const int len = a.len0[s] + a.t, p = len / kPage + rest % a.slots;
+  const uint32_t per = 2 + a.q_blocks;
+  uint32_t x = blockIdx.x / per;
+  const int z = blockIdx.x - x * per;  // 0: K, 1: V, from 2 on: q
+  const uint32_t x1 = x / (uint32_t)a.slots;
+  const int slot = x - x1 * a.slots;
+  int s = x1, l = 0;
+  if (a.n_layers > 1) {
+    l = x1 / (uint32_t)a.n_seqs;
+    s = x1 - l * a.n_seqs;
+  }
+  const int len = a.len0[s] + a.t, p = len / kPage + slot;
   const int t0 = max(len - kPage * p, 0), t1 = min(len + a.n_tokens - kPage * p, kPage);  // new tokens of the page
   if (t0 >= t1) return;
-  const int phys = a.page_table[(size_t)s * a.maxpps + p];
   const int Hq = a.n_q_heads, Hkv = a.n_kv_heads, D = a.head_dim, rot = a.rot_dim;
   const bool halves = a.halves != 0;
   const size_t row0 = (size_t)s * a.n_tokens + (kPage * p - len);  // row of the page's token 0 (as a difference)
   const int half = rot / 2, n = t1 - t0;
-  for (int e = tid; e < n * half; e += 256) {
-    const int t = t0 + e / half, i = e % half;
-    double sn, co;
-    sincos((double)(kPage * p + t) * exp2(-(2.0 * i / rot) * a.log2_theta), &sn, &co);
-    cs[t][i] = make_float2((float)co, (float)sn);
-  }
-  __syncthreads();
-  const size_t tile = (size_t)kPage * D;
-  const size_t tile0 = ((size_t)(a.layer0 + l) * a.max_pages + phys) * Hkv;
   const int nslot = Slot<BF16>::count(D, rot, halves);
+  if (z > 1 && (z - 2) * kAppendTasks >= n * Hq * nslot) return;
   auto row_of = [&](const void* base, int64_t stride, int t, int heads, int h) {
     return (const char*)base + ((size_t)(row0 + t) * stride + ((size_t)l * heads + h) * D) * es;
   };
+  // cos and sin of the block's positions; ends with a barrier
+  auto trig = [&] {
+    if (rot == 0) return;
+    if (tid < half) turn_of[tid] = exp2(-(2.0 * tid / rot) * a.log2_theta) * 0.31830988618379067154;  // over pi
+    __syncthreads();
+    for (int e = tid; e < n * half; e += 256) {
+      const int t = e / half, i = e - t * half;
+      double sn, co;
+      sincospi((double)(kPage * p + t0 + t) * turn_of[i], &sn, &co);
+      cs[t0 + t][i] = make_float2((float)co, (float)sn);
+    }
+    __syncthreads();
+  };
 
-  // q rows
-  if (a.q) {
-    for (int e = tid; e < n * Hq * nslot; e += 256) {
-      const int t = t0 + e / (Hq * nslot), h = e / nslot % Hq;
-      const Slot<BF16> sl(e % nslot, rot, halves);
-      u32x4 o1, o2;
-      turned<BF16>(row_of(a.q, a.q_row, t, Hq, h), sl, cs[t], rot, true, o1, o2);
-      char* out = (char*)a.q_out + (((row0 + t) * a.n_layers + l) * Hq + h) * D * es;
-      *(u32x4*)(out + sl.d * es) = o1;
-      if (sl.d2 >= 0) *(u32x4*)(out + sl.d2 * es) = o2;
+  if (z > 1) {
+    constexpr int U = kAppendTasks / 256;
+    const int total = n * Hq * nslot;
+    u32x4 o1[U], o2[U];
+    int tok[U], head[U], un[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int e = min((z - 2) * kAppendTasks + 256 * i + tid, total - 1);
+      const int r = e / nslot;
+      un[i] = e - r * nslot;
+      tok[i] = r / Hq;
+      head[i] = r - tok[i] * Hq;
+      load_slot<BF16>(row_of(a.q, a.q_row, t0 + tok[i], Hq, head[i]), Slot<BF16>(un[i], rot, halves), o1[i], o2[i]);
     }
+    trig();
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if ((z - 2) * kAppendTasks + 256 * i + tid >= total) break;
+      const Slot<BF16> sl(un[i], rot, halves);
+      turn_slot<BF16>(sl, cs[t0 + tok[i]], rot, o1[i], o2[i]);
+      char* out = (char*)a.q_out + (((row0 + t0 + tok[i]) * a.n_layers + l) * Hq + head[i]) * D * es;
+      *(u32x4*)(out + sl.d * es) = o1[i];
+      if (sl.d2 >= 0) *(u32x4*)(out + sl.d2 * es) = o2[i];
+    }
+    return;
   }
+
+  const int phys = a.page_table[(size_t)s * a.maxpps + p];
+  const size_t tile = (size_t)kPage * D;
+  const size_t tile0 = ((size_t)(a.layer0 + l) * a.max_pages + phys) * Hkv;
   if constexpr (BF16) {
-    // K: token pairs, a sector each
-    const int j0 = t0 >> 1, np = ((t1 - 1) >> 1) - j0 + 1;
-    for (int e = tid; e < np * nslot * Hkv; e += 256) {
-      const int j = j0 + e % np, h = e / (np * nslot);
-      const Slot<BF16> sl(e / np % nslot, rot, halves);
-      const bool na = 2 * j >= t0, nb = 2 * j + 1 < t1;  // (one of the two is new)
-      u32x4 a1{}, a2{}, b1{}, b2{};
-      if (na) turned<BF16>(row_of(a.k, a.k_row, 2 * j, Hkv, h), sl, cs[2 * j], rot, true, a1, a2);
-      if (nb) turned<BF16>(row_of(a.k, a.k_row, 2 * j + 1, Hkv, h), sl, cs[2 * j + 1], rot, true, b1, b2);
-      auto put = [&](int d, u32x4 x, u32x4 y) {
-        u32x4* sec = (u32x4*)((uint16_t*)a.kpool + (tile0 + h) * tile + kswz(2 * j, d));
-        if (!na) x = sec[0];
-        if (!nb) y = sec[1];
-        __builtin_nontemporal_store(x, sec);
-        __builtin_nontemporal_store(y, sec + 1);
-      };
-      put(sl.d, a1, b1);
-      if (sl.d2 >= 0) put(sl.d2, a2, b2);
-    }
-    // V: runs of 128 bytes, four tokens of dims d0 .. d0 + 7 and d0 + 16 .. d0 + 23
-    const int q0 = t0 >> 2, nq = ((t1 - 1) >> 2) - q0 + 1, runs = D / 16;
-    for (int e = tid; e < nq * Hkv * runs; e += 256) {
-      const int r = e % runs, h = e / runs % Hkv, q = q0 + e / (runs * Hkv);
-      const int d0 = 32 * (r >> 1) + 8 * (r & 1);
-      u32x4* run = (u32x4*)((uint16_t*)a.vpool + (tile0 + h) * tile + vswz(4 * q, d0));
-      u32x4 v[4][2] = {}, cur[8] = {};
-      const bool all = 4 * q >= t0 && 4 * q + 4 <= t1;
-      if (!all) {
+    if (z == 1) {
+      const int runs = D / 16;  // of a kv-head's token quad
+      if (n == kPage) {
+        // a wave takes 64 runs: 4 x 2 pieces of a run's rows, transposed in registers, to the wave's 8 KiB of LDS
+        // (units XOR-swizzled against bank conflicts) and out as contiguous units
+        uint4* mine = lds.v[tid >> 6];
+        const int lane = tid & 63, all = 4 * Hkv * runs;
+        for (int b = tid >> 6; 64 * b < all; b += 4) {
+          const RunPos rp = run_pos(min(64 * b + lane, all - 1), D);
+          u32x4 v[4][2];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const char* row = row_of(a.v, a.v_row, 4 * rp.q + t, Hkv, rp.g) + rp.d0 * 2;
+            v[t][0] = *(const u32x4*)row;
+            v[t][1] = *(const u32x4*)(row + 32);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            mine[lane * 8 + (i ^ (lane & 7))] =
+                make_uint4(el16(v[0][0], i) | (el16(v[1][0], i) << 16), el16(v[2][0], i) | (el16(v[3][0], i) << 16),
+                           el16(v[0][1], i) | (el16(v[1][1], i) << 16), el16(v[2][1], i) | (el16(v[3][1], i) << 16));
+          wave_lds_sync();
+          u32x4* out = (u32x4*)((uint16_t*)a.vpool + tile0 * tile) + 512 * b + lane;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int m = 64 * i + lane;
+            const uint4 w = mine[(m >> 3) * 8 + ((m & 7) ^ ((m >> 3) & 7))];
+            if (512 * b + m < 8 * all) __builtin_nontemporal_store(u32x4{w.x, w.y, w.z, w.w}, out + 64 * i);
+          }
+          wave_lds_sync();
+        }
+        return;
+      }
+      // runs of 128 bytes, four tokens of dims d0 .. d0 + 7 and d0 + 16 .. d0 + 23
+      const int q0 = t0 >> 2, nq = ((t1 - 1) >> 2) - q0 + 1;
+      for (int e = tid; e < nq * Hkv * runs; e += 256) {
+        const int r = e % runs, h = e / runs % Hkv, q = q0 + e / (runs * Hkv);
+        const int d0 = 32 * (r >> 1) + 8 * (r & 1);
+        u32x4* run = (u32x4*)((uint16_t*)a.vpool + (tile0 + h) * tile + vswz(4 * q, d0));
+        u32x4 v[4][2], cur[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) cur[i] = run[i];
-      }
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (4 * q + t < t0 || 4 * q + t >= t1) continue;
-        const char* row = row_of(a.v, a.v_row, 4 * q + t, Hkv, h) + d0 * 2;
-        v[t][0] = *(const u32x4*)row;
-        v[t][1] = *(const u32x4*)(row + 32);
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (4 * q + t < t0 || 4 * q + t >= t1) continue;
-        const uint32_t sh = 16 * (t & 1), keep = ~(0xFFFFu << sh);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          cur[i][t >> 1] = (cur[i][t >> 1] & keep) | (el16(v[t][0], i) << sh);
-          cur[i][2 + (t >> 1)] = (cur[i][2 + (t >> 1)] & keep) | (el16(v[t][1], i) << sh);
+        for (int t = 0; t < 4; ++t) {  // (tokens that are not new: a new one's row again)
+          const char* row = row_of(a.v, a.v_row, min(max(4 * q + t, t0), t1 - 1), Hkv, h) + d0 * 2;
+          v[t][0] = *(const u32x4*)row;
+          v[t][1] = *(const u32x4*)(row + 32);
         }
-      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) __builtin_nontemporal_store(cur[i], run + i);
+        for (int t = 0; t < 4; ++t) {
+          if (4 * q + t < t0 || 4 * q + t >= t1) continue;
+          const uint32_t sh = 16 * (t & 1), keep = ~(0xFFFFu << sh);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            cur[i][t >> 1] = (cur[i][t >> 1] & keep) | (el16(v[t][0], i) << sh);
+            cur[i][2 + (t >> 1)] = (cur[i][2 + (t >> 1)] & keep) | (el16(v[t][1], i) << sh);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) __builtin_nontemporal_store(cur[i], run + i);
+      }
+      return;
     }
-  } else {
+    if (n == kPage) {
+      // K: a lane per token, 16 tokens of a unit next to each other
+      constexpr int U = 4;
+      const int total = kPage * nslot * Hkv, t = tid & 15;
+      u32x4 v1[U], v2[U];
+      auto load = [&](int e0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int r = min(e0 + 256 * i + tid, total - 1) >> 4, h = r / nslot;
+          load_slot<BF16>(row_of(a.k, a.k_row, t, Hkv, h), Slot<BF16>(r - h * nslot, rot, halves), v1[i], v2[i]);
+        }
+      };
+      load(0);
+      trig();
+      for (int e0 = 0;;) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int e = e0 + 256 * i + tid, r = e >> 4, h = r / nslot;
+          if (e >= total) break;
+          const Slot<BF16> sl(r - h * nslot, rot, halves);
+          turn_slot<BF16>(sl, cs[t], rot, v1[i], v2[i]);
+          uint16_t* out = (uint16_t*)a.kpool + (tile0 + h) * tile;
+          __builtin_nontemporal_store(v1[i], (u32x4*)(out + kswz(t, sl.d)));
+          if (sl.d2 >= 0) __builtin_nontemporal_store(v2[i], (u32x4*)(out + kswz(t, sl.d2)));
+        }
+        e0 += 256 * U;
+        if (e0 >= total) break;
+        load(e0);
+      }
+    } else {
+      // K: token pairs, a sector each
+      constexpr int U = 2;
+      const int j0 = t0 >> 1, np = ((t1 - 1) >> 1) - j0 + 1, total = np * nslot * Hkv;
+      u32x4 v1[U][2], v2[U][2];
+      int pair[U], head[U], un[U];
+      auto load = [&](int e0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int e = min(e0 + 256 * i + tid, total - 1), r = e / np;
+          pair[i] = j0 + e - r * np;
+          head[i] = r / nslot;
+          un[i] = r - head[i] * nslot;
+          const Slot<BF16> sl(un[i], rot, halves);
+#pragma unroll
+          for (int c = 0; c < 2; ++c)  // (a token of the sector that is not new: its neighbour's row again)
+            load_slot<BF16>(row_of(a.k, a.k_row, min(max(2 * pair[i] + c, t0), t1 - 1), Hkv, head[i]), sl, v1[i][c],
+                            v2[i][c]);
+        }
+      };
+      load(0);
+      trig();
+      for (int e0 = 0;;) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (e0 + 256 * i + tid >= total) break;
+          const Slot<BF16> sl(un[i], rot, halves);
+          const int ta = 2 * pair[i];
+          const bool na = ta >= t0, nb = ta + 1 < t1;  // (one of the two is new)
+          if (na) turn_slot<BF16>(sl, cs[ta], rot, v1[i][0], v2[i][0]);
+          if (nb) turn_slot<BF16>(sl, cs[ta + 1], rot, v1[i][1], v2[i][1]);
+          auto put = [&](int d, u32x4 x, u32x4 y) {
+            u32x4* sec = (u32x4*)((uint16_t*)a.kpool + (tile0 + head[i]) * tile + kswz(ta, d));
+            if (!na) x = sec[0];
+            if (!nb) y = sec[1];
+            __builtin_nontemporal_store(x, sec);
+            __builtin_nontemporal_store(y, sec + 1);
+          };
+          put(sl.d, v1[i][0], v1[i][1]);
+          if (sl.d2 >= 0) put(sl.d2, v2[i][0], v2[i][1]);
+        }
+        e0 += 256 * U;
+        if (e0 >= total) break;
+        load(e0);
+      }
+    }
+  } else if (z == 1) {
     // row-major fp32 tiles: a token's row is whole lines
-    for (int e = tid; e < n * Hkv * nslot; e += 256) {
-      const int t = t0 + e / (Hkv * nslot), h = e / nslot % Hkv;
-      const Slot<BF16> sl(e % nslot, rot, halves);
-      u32x4 o1, o2;
-      turned<BF16>(row_of(a.k, a.k_row, t, Hkv, h), sl, cs[t], rot, true, o1, o2);
-      float* out = (float*)a.kpool + (tile0 + h) * tile + (size_t)t * D;
-      *(u32x4*)(out + sl.d) = o1;
-      if (sl.d2 >= 0) *(u32x4*)(out + sl.d2) = o2;
-    }
     for (int e = tid; e < n * Hkv * (D / N); e += 256) {
       const int t = t0 + e / (Hkv * (D / N)), h = e / (D / N) % Hkv, d = e % (D / N) * N;
       *(u32x4*)((float*)a.vpool + (tile0 + h) * tile + (size_t)t * D + d) =
           *(const u32x4*)(row_of(a.v, a.v_row, t, Hkv, h) + d * es);
+    }
+    return;
+  } else {
+    trig();
+    for (int e = tid; e < n * Hkv * nslot; e += 256) {
+      const int t = t0 + e / (Hkv * nslot), h = e / nslot % Hkv;
+      const Slot<BF16> sl(e % nslot, rot, halves);
+      u32x4 o1, o2;
+      load_slot<BF16>(row_of(a.k, a.k_row, t, Hkv, h), sl, o1, o2);
+      turn_slot<BF16>(sl, cs[t], rot, o1, o2);
+      float* out = (float*)a.kpool + (tile0 + h) * tile + (size_t)t * D;
+      *(u32x4*)(out + sl.d) = o1;
+      if (sl.d2 >= 0) *(u32x4*)(out + sl.d2) = o2;
     }
   }
   if (a.codes && t1 == kPage) {
@@ -313,28 +452,40 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
 // ------------------------------------------------------------- page selection
 
 // A launch's items: (token group, token of the group, layer, kv-head), the groups
-// being gt consecutive new tokens of one sequence.
+// being gt consecutive new tokens of one sequence. (Fewer than 2^31 of them.)
 struct AttendItem {
   int s, tok, l, h, pos, pages;  // pos: the token's position; pages: how many it sees (0: no such token)
   size_t row;                    // (sequence, token) row of q, x and the page lists
 };
-__device__ __forceinline__ AttendItem attend_item(const AttendArgs& a, size_t item) {
+__device__ __forceinline__ AttendItem attend_item(const AttendArgs& a, uint32_t item) {
   AttendItem r;
-  r.h = (int)(item % a.n_kv_heads);
-  item /= a.n_kv_heads;
-  r.l = (int)(item % a.launch_layers);
-  item /= a.launch_layers;
-  const int j = (int)(item % a.gt), g = a.group0 + (int)(item / a.gt);
-  r.s = g / a.seq_groups;
-  r.tok = g % a.seq_groups * a.gt + j;
+  r.h = item % (uint32_t)a.n_kv_heads;
+  item /= (uint32_t)a.n_kv_heads;
+  r.l = 0;
+  if (a.launch_layers > 1) {
+    r.l = item % (uint32_t)a.launch_layers;
+    item /= (uint32_t)a.launch_layers;
+  }
+  uint32_t j = 0, g = item;
+  if (a.gt > 1) {
+    j = item % (uint32_t)a.gt;
+    g = item / (uint32_t)a.gt;
+  }
+  g += a.group0;
+  r.s = g;
+  r.tok = j;
+  if (a.seq_groups > 1) {
+    r.s = g / (uint32_t)a.seq_groups;
+    r.tok = (g - r.s * a.seq_groups) * a.gt + j;
+  }
   r.pos = a.len0[r.s] + a.t + r.tok;
   r.pages = r.tok < a.n_tokens ? r.pos / kPage + 1 : 0;
   r.row = (size_t)r.s * a.n_tokens + r.tok;
   return r;
 }
-__device__ __forceinline__ const int32_t* page_list(const AttendArgs& a, const AttendItem& it, size_t item) {
+__device__ __forceinline__ const int32_t* page_list(const AttendArgs& a, const AttendItem& it, uint32_t item) {
   return a.pages_out ? a.pages_out + ((it.row * a.n_layers + a.layer - a.layer0 + it.l) * a.n_kv_heads + it.h) * a.n_pages
-                     : a.list + item * a.n_pages;
+                     : a.list + (size_t)item * a.n_pages;
 }
 
 // Bounds on the scores of the pages that a token may select. With the q-heads of a
@@ -433,15 +584,23 @@ __device__ __forceinline__ uint32_t order_key(float f) {
 struct GroupItem {
   int s, l, h, gl, tok0, nt, len, pages;  // nt tokens from tok0 on; pages: that the last of them sees
 };
-__device__ __forceinline__ GroupItem group_item(const AttendArgs& a, size_t item) {
+__device__ __forceinline__ GroupItem group_item(const AttendArgs& a, uint32_t item) {
   GroupItem r;
-  r.h = (int)(item % a.n_kv_heads);
-  item /= a.n_kv_heads;
-  r.l = (int)(item % a.launch_layers);
-  r.gl = (int)(item / a.launch_layers);
-  const int g = a.group0 + r.gl;
-  r.s = g / a.seq_groups;
-  r.tok0 = g % a.seq_groups * a.gt;
+  r.h = item % (uint32_t)a.n_kv_heads;
+  item /= (uint32_t)a.n_kv_heads;
+  r.l = 0;
+  r.gl = item;
+  if (a.launch_layers > 1) {
+    r.l = item % (uint32_t)a.launch_layers;
+    r.gl = item / (uint32_t)a.launch_layers;
+  }
+  const uint32_t g = a.group0 + r.gl;
+  r.s = g;
+  r.tok0 = 0;
+  if (a.seq_groups > 1) {
+    r.s = g / (uint32_t)a.seq_groups;
+    r.tok0 = (g - r.s * a.seq_groups) * a.gt;
+  }
   r.nt = min(a.gt, a.n_tokens - r.tok0);
   r.len = a.len0[r.s] + a.t;
   r.pages = (r.len + r.tok0 + r.nt - 1) / kPage + 1;
@@ -451,14 +610,27 @@ __device__ __forceinline__ const void* group_q(const AttendArgs& a, const GroupI
   const size_t row = ((size_t)it.s * a.n_tokens + it.tok0 + j) * a.n_layers + a.layer - a.layer0 + it.l;
   return (const char*)a.q + (row * a.n_q_heads + (size_t)it.h * a.group) * a.head_dim * (a.bf16 ? 2 : 4);
 }
-__device__ __forceinline__ size_t group_slot(const AttendArgs& a, const GroupItem& it, int j) {
-  return (((size_t)it.gl * a.gt + j) * a.launch_layers + it.l) * a.n_kv_heads + it.h;
+__device__ __forceinline__ uint32_t group_slot(const AttendArgs& a, const GroupItem& it, int j) {
+  return (((uint32_t)it.gl * a.gt + j) * a.launch_layers + it.l) * a.n_kv_heads + it.h;
+}
+// the token's item
+__device__ __forceinline__ AttendItem group_row(const AttendArgs& a, const GroupItem& it, int j) {
+  AttendItem r;
+  r.s = it.s;
+  r.tok = it.tok0 + j;
+  r.l = it.l;
+  r.h = it.h;
+  r.pos = it.len + r.tok;
+  r.pages = r.pos / kPage + 1;
+  r.row = (size_t)it.s * a.n_tokens + r.tok;
+  return r;
 }
 
 // The pages of one token from the keys of its candidates, page lo + 64 i + lane at
 // key[i] (0: no candidate), by one wave: the want-th highest key bit by bit, from
-// counts over the wave, then the pages in order, each at its place. want >= 1, and
-// there are at least as many candidates. Returns nothing but the list.
+// counts over the wave (done as soon as a bound has just `want` keys above it, which
+// takes about as many bits as tell neighbours apart), then the pages in order, each
+// at its place. want >= 1, and there are at least as many candidates.
 template <int R>
 __device__ __forceinline__ void pick_pages(const uint32_t (&key)[R], int lo, int want, int32_t* list, int lane) {
   uint32_t t = 0;
@@ -468,6 +640,10 @@ __device__ __forceinline__ void pick_pages(const uint32_t (&key)[R], int lo, int
 #pragma unroll
     for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= c));
     if (n >= want) t = c;
+    if (n == want) {
+      t = c - 1;  // exactly the keys above this
+      break;
+    }
   }
   int above = 0;
 #pragma unroll
@@ -499,15 +675,15 @@ __device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32
   return a.n_pages - a.first - a.last;
 }
 
-// Bounds and choice in one launch, for at most 64 R pages: one block of 8 waves per
-// (token group, layer, kv-head), R/2 tiles of 16 pages per wave. The codes are on
+// Bounds and choice in one launch, for at most 64 R pages: one block of W waves per
+// (token group, layer, kv-head), 4 R / W tiles of 16 pages per wave. The codes are on
 // their way while the weights are made; the bounds meet in LDS, from where each
 // wave chooses the pages of a token.
-template <int R>
-__global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
-  constexpr int NT = R / 2;
-  __shared__ __align__(16) int8_t w[16][256];
-  __shared__ __align__(16) float bound[16][64 * R + 4];
+template <int R, int W>
+__global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
+  constexpr int NT = 4 * R / W, T = kAttendTokens;
+  __shared__ __align__(16) int8_t w[16][256];  // (columns past the tokens' count for nothing)
+  __shared__ __align__(16) float bound[T][64 * R + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const GroupItem it = group_item(a, blockIdx.x);
@@ -518,26 +694,26 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
     CodeTile t[NT];
     int phys[NT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) phys[i] = pt[min(16 * (wave + 8 * i) + col, p1 - 1)];
+    for (int i = 0; i < NT; ++i) phys[i] = pt[min(16 * (wave + W * i) + col, p1 - 1)];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
-      if (16 * (wave + 8 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
-    for (int j = wave; j < it.nt; j += 8) query_weights(a, group_q(a, it, j), lane, w[j]);
+      if (16 * (wave + W * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
+    for (int j = wave; j < it.nt; j += W) query_weights(a, group_q(a, it, j), lane, w[j]);
     __syncthreads();
     i32x4 b[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
-      if (16 * (wave + 8 * i) < p1) {
+      if (16 * (wave + W * i) < p1) {
         const float4 o = tile_bounds(a, t[i], b, quad);
-        if (col < it.nt) *(float4*)&bound[col][16 * (wave + 8 * i) + 4 * quad] = o;
+        if (col < it.nt) *(float4*)&bound[col][16 * (wave + W * i) + 4 * quad] = o;
       }
     __syncthreads();
   }
-  for (int j = wave; j < it.nt; j += 8) {
-    const size_t slot = group_slot(a, it, j);
-    const AttendItem row = attend_item(a, slot);
+  for (int j = wave; j < it.nt; j += W) {
+    const uint32_t slot = group_slot(a, it, j);
+    const AttendItem row = group_row(a, it, j);
     int32_t* list = const_cast<int32_t*>(page_list(a, row, slot));
     if (row.pages <= a.n_pages && !a.pages_out) continue;  // (all pages: nobody reads the list)
     const int want = fixed_pages(a, row.pages, list, lane, 64);
@@ -553,49 +729,74 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
 }
 
 // The same in two launches for long sequences, whose summaries one work-group would
-// take long to read. Bounds: a block per (token group, layer, kv-head, kScorePages
-// pages), four tiles of 16 pages per wave. Bound: HBM, the summaries are read once.
+// take long to read. Bounds: a block per (token group, layer, kv-head, chunk_pages
+// pages), each wave 32 of every 128 pages at a time; their ids are two rounds ahead and
+// their codes one. Bound: HBM, the summaries are read once.
 __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
-  constexpr int NT = kScorePages / 64;
   __shared__ __align__(16) int8_t w[16][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const GroupItem it = group_item(a, blockIdx.x / a.chunks);
-  const int p0 = blockIdx.x % a.chunks * kScorePages, p1 = min(it.pages - a.last, p0 + kScorePages);
+  const GroupItem it = group_item(a, blockIdx.x / (uint32_t)a.chunks);
+  const int p0 = blockIdx.x % (uint32_t)a.chunks * a.chunk_pages, p1 = min(it.pages - a.last, p0 + a.chunk_pages);
   if (it.pages <= a.n_pages || p0 >= p1) return;
   const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
   const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
-  CodeTile t[NT];
-  int phys[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) phys[i] = pt[min(p0 + 16 * (wave + 4 * i) + col, p1 - 1)];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    if (p0 + 16 * (wave + 4 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
+  struct Ids {
+    int a, b;
+  };
+  struct Tiles {
+    CodeTile a, b;
+  };
+  const int q0 = p0 + 32 * wave;  // the wave's first pages
+  // (past the range its last page)
+  auto ids = [&](int q) { return Ids{pt[min(q + col, p1 - 1)], pt[min(q + 16 + col, p1 - 1)]}; };
+  auto load = [&](const Ids& p, Tiles& t) __attribute__((always_inline)) {
+    load_codes(a, base, p.a, quad, t.a);
+    load_codes(a, base, p.b, quad, t.b);
+  };
+  Ids ia = ids(q0), ib = ids(q0 + 128);
+  Tiles ta, tb;
+  load(ia, ta);
   for (int j = wave; j < it.nt; j += 4) query_weights(a, group_q(a, it, j), lane, w[j]);
   __syncthreads();
   i32x4 b[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
-  float* out = a.scores + group_slot(a, it, col) * a.score_row + p0 + 4 * quad;
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    if (p0 + 16 * (wave + 4 * i) < p1) {
-      const float4 o = tile_bounds(a, t[i], b, quad);
-      if (col < it.nt) *(float4*)(out + 16 * (wave + 4 * i)) = o;  // (rows hold whole tiles)
-    }
+  float* out = a.scores + (size_t)group_slot(a, it, min(col, it.nt - 1)) * a.score_row + 4 * quad;
+  auto put = [&](int q, const Tiles& t) __attribute__((always_inline)) {
+    const float4 x = tile_bounds(a, t.a, b, quad), y = tile_bounds(a, t.b, b, quad);
+    if (col < it.nt && q < p1) *(float4*)(out + q) = x;  // (rows hold whole tiles)
+    if (col < it.nt && q + 16 < p1) *(float4*)(out + q + 16) = y;
+  };
+  for (int q = q0; q < p1; q += 256) {
+    ia = ids(q + 256);
+    load(ib, tb);
+    put(q, ta);
+    ib = ids(q + 384);
+    load(ia, ta);
+    put(q + 128, tb);
+  }
 }
 
 // The choice from those bounds: a block of 16 waves per item, wave v's keys being the
-// v-th run of 64 R candidates. As pick_pages, with the counts of the waves added up
-// in LDS, one barrier per bit. A row of more than 1024 R candidates (MANY) goes in
-// rounds, whose keys are read again for every bit.
+// v-th run of 64 R candidates. The candidates are counted in kBins equal steps of
+// their range (which spreads them, so that the LDS atomics rarely meet), the step that
+// holds the want-th highest bound is found from the counts, and its candidates, a few,
+// are ranked one by one. Where they are more than kNear (bounds far from the rest
+// squeeze it into few steps), the bound is searched bit by bit as in pick_pages, with the
+// counts of the waves added up in LDS and two bits per barrier. A row of more than
+// 1024 R candidates (MANY) goes in rounds, whose keys are read again for every pass.
+constexpr int kBins = 2048, kNear = 512;
+__device__ __forceinline__ float order_value(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
 template <int R, bool MANY>
 __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
-  __shared__ int count[33];
-  __shared__ int wsum[2][16];
+  __shared__ int count[52], hist[kBins], near_page[kNear];
+  __shared__ uint32_t near_key[kNear], wmin[16], wmax[16], s_key;
+  __shared__ int wsum[2][16], s_bin, s_need, s_near, s_page;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const size_t item = blockIdx.x;
+  const uint32_t item = blockIdx.x;
   const AttendItem it = attend_item(a, item);
   if (it.pages == 0 || (it.pages <= a.n_pages && !a.pages_out)) return;
   int32_t* list = const_cast<int32_t*>(page_list(a, it, item));
@@ -604,7 +805,7 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
   list += a.first;
   const int lo = a.first, hi = it.pages - a.last;
   const int rounds = MANY ? (hi - lo + 1024 * R - 1) / (1024 * R) : 1;
-  const float* sc = a.scores + item * a.score_row;
+  const float* sc = a.scores + (size_t)item * a.score_row;
   uint32_t key[R];
   auto load = [&](int round) __attribute__((always_inline)) {
 #pragma unroll
@@ -613,38 +814,125 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
       key[i] = p < hi ? order_key(sc[min(p, hi - 1)]) : 0u;
     }
   };
-  if (tid < 33) count[tid] = 0;
+  for (int i = tid; i < kBins; i += 1024) hist[i] = 0;
+  if (tid < 52) count[tid] = 0;
   load(0);
+  // the range of the bounds
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+  for (int r = 0; r < rounds; ++r) {
+    if (MANY) load(r);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      kmin = min(kmin, key[i] ? key[i] : 0xFFFFFFFFu);
+      kmax = max(kmax, key[i]);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    kmin = min(kmin, (uint32_t)__shfl_xor((int)kmin, o));
+    kmax = max(kmax, (uint32_t)__shfl_xor((int)kmax, o));
+  }
+  if (lane == 0) { wmin[wave] = kmin; wmax[wave] = kmax; }
   __syncthreads();
+#pragma unroll
+  for (int v = 0; v < 16; ++v) { kmin = min(kmin, wmin[v]); kmax = max(kmax, wmax[v]); }
+  const float low = order_value(kmin), span = order_value(kmax) - low;
+  const float inv = span > 0.f ? (float)(kBins - 1) / span : 0.f;
+  auto bin_of = [&](uint32_t k) { return min((int)((order_value(k) - low) * inv), kBins - 1); };  // (grows with k)
+  for (int r = 0; r < rounds; ++r) {
+    if (MANY) load(r);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (key[i]) atomicAdd(&hist[bin_of(key[i])], 1);
+  }
+  __syncthreads();
+  {  // thread i: bins kBins - 1 - 2i and the one below it
+    const int hi2 = hist[kBins - 1 - 2 * tid], lo2 = hist[kBins - 2 - 2 * tid];
+    int sum = hi2 + lo2, run = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(run, o); if (lane >= o) run += x; }
+    if (lane == 63) wsum[0][wave] = run;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 16; ++v) if (v < wave) run += wsum[0][v];
+    const int before = run - sum;
+    if (before < want && want <= before + sum) {
+      const bool first = want <= before + hi2;
+      s_bin = kBins - 1 - 2 * tid - (first ? 0 : 1);
+      s_need = want - before - (first ? 0 : hi2);
+      s_near = first ? hi2 : lo2;
+    }
+  }
+  __syncthreads();
+  const int bin = s_bin, need = s_need;  // the best `need` of this bin's, and all above it
   uint32_t t = 0;
-  for (int b = 31; b >= 0; --b) {
-    const uint32_t c = t | (1u << b);
+  int ties = 0x7FFFFFFF, last_tie = 0x7FFFFFFF;  // equal keys that are taken: so many, and up to this page
+  if (s_near <= kNear) {
+    for (int r = 0; r < rounds; ++r) {
+      if (MANY) load(r);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (key[i] && bin_of(key[i]) == bin) {
+          const int at = atomicAdd(&count[0], 1);
+          near_key[at] = key[i];
+          near_page[at] = lo + (r * 16 + wave) * 64 * R + 64 * i + lane;
+        }
+    }
+    __syncthreads();
+    const int n = s_near;
+    if (tid < n) {
+      const uint32_t k = near_key[tid];
+      const int p = near_page[tid];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += near_key[j] > k || (near_key[j] == k && near_page[j] < p);
+      if (rank == need - 1) { s_key = k; s_page = p; }
+    }
+    __syncthreads();
+    t = s_key;
+    last_tie = s_page;
+  } else {
+    bool exact = false;
+    for (int b = 30; b >= 0 && !exact; b -= 2) {  // two bits: keys from t + 2^b, 2 * 2^b and 3 * 2^b on
+      const uint32_t c = 1u << b;
+      int n[3] = {0, 0, 0};
+      for (int r = 0; r < rounds; ++r) {
+        if (MANY) load(r);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int j = 0; j < 3; ++j) n[j] += __popcll(__ballot(key[i] >= t + (j + 1) * c));
+      }
+      int* at = count + 3 * (b >> 1);
+      if (lane < 3) {
+        const int mine = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
+        if (mine) atomicAdd(&at[lane], mine);
+      }
+      __syncthreads();
+      const int n1 = at[0], n2 = at[1], n3 = at[2];
+      const int k = n3 >= want ? 3 : n2 >= want ? 2 : n1 >= want ? 1 : 0;
+      exact = (k == 3 ? n3 : k == 2 ? n2 : k == 1 ? n1 : 0) == want;
+      t += k * c - (exact ? 1u : 0u);  // (exactly the keys above it)
+    }
+    // the pages equal to the key: as many as there is room for, from the first on
     int n = 0;
     for (int r = 0; r < rounds; ++r) {
       if (MANY) load(r);
 #pragma unroll
-      for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= c));
+      for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] > t));
     }
-    if (lane == 0 && n) atomicAdd(&count[b], n);
+    if (lane == 0 && n) atomicAdd(&count[51], n);
     __syncthreads();
-    if (count[b] >= want) t = c;
+    ties = want - count[51];
   }
-  int n = 0;
-  for (int r = 0; r < rounds; ++r) {
-    if (MANY) load(r);
-#pragma unroll
-    for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] > t));
-  }
-  if (lane == 0 && n) atomicAdd(&count[32], n);
-  __syncthreads();
-  const int ties = want - count[32];
+  auto page_at = [&](int r, int i) { return lo + (r * 16 + wave) * 64 * R + 64 * i + lane; };
+  auto tie = [&](int r, int i) { return key[i] == t && page_at(r, i) <= last_tie; };
   const uint64_t below = ((uint64_t)1 << lane) - 1;
   int base = 0, eq = 0;  // places taken and equal keys met before the round
   for (int r = 0; r < rounds; ++r) {
     if (MANY) load(r);
     int g = 0, e = 0;
 #pragma unroll
-    for (int i = 0; i < R; ++i) { g += __popcll(__ballot(key[i] > t)); e += __popcll(__ballot(key[i] == t)); }
+    for (int i = 0; i < R; ++i) { g += __popcll(__ballot(key[i] > t)); e += __popcll(__ballot(tie(r, i))); }
     if (lane == 0) { wsum[0][wave] = g; wsum[1][wave] = e; }
     __syncthreads();
     int gb = 0, eb = 0, ga = 0, ea = 0;  // before this wave, and of all
@@ -657,10 +945,10 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
     int at = base + gb + min(eq + eb, ties) - min(eq, ties), seen = eq + eb;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const uint64_t mg = __ballot(key[i] > t), me = __ballot(key[i] == t);
+      const uint64_t mg = __ballot(key[i] > t), me = __ballot(tie(r, i));
       const int k = seen + __popcll(me & below);
-      if (key[i] > t || (key[i] == t && k < ties))
-        list[at + __popcll(mg & below) + min(k, ties) - min(seen, ties)] = lo + (r * 16 + wave) * 64 * R + 64 * i + lane;
+      if (key[i] > t || (tie(r, i) && k < ties))
+        list[at + __popcll(mg & below) + min(k, ties) - min(seen, ties)] = page_at(r, i);
       const int seen1 = seen + __popcll(me);
       at += __popcll(mg) + min(seen1, ties) - min(seen, ties);
       seen = seen1;
@@ -697,9 +985,10 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // of two bf16 values (what the first leaves over goes into the second, a relative
 // error of 2^-17): the matrix cores are idle anyway while the pages come in. fp32:
 // one page, fp32 matrix cores throughout.
-// A wave holds the physical ids of its pages (64 at a time) one per lane, so that no
-// batch waits for a chain of list and page table, and loads a batch while it works
-// on the one before.
+// A wave holds the ids of its pages (a part has at most 64 per wave) one per lane, so
+// that no batch waits for a chain of list and page table, and loads a batch while it
+// works on the one before (no load is conditional: the wait for a batch must leave
+// the next one in flight on every path).
 // Tokens behind the row's own position get weight 0, and their V counts as 0 (those
 // rows may hold anything).
 template <bool BF16, int NU>
@@ -720,8 +1009,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   __shared__ float sm[4][kMaxGroup], sl[4][kMaxGroup];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const int part = blockIdx.x % a.parts;
-  const size_t item = blockIdx.x / a.parts;
+  // Work-groups go to the eight dies in turn. With several new tokens, all those of one
+  // (sequence, layer, kv-head) go to one die and follow each other there, so that pages
+  // which several of them chose are in its L2.
+  uint32_t item, part;
+  if (a.n_tokens == 1) {
+    item = blockIdx.x / (uint32_t)a.parts;
+    part = blockIdx.x - item * a.parts;
+  } else {
+    const uint32_t s0 = (uint32_t)a.group0 / a.seq_groups, tok = (uint32_t)a.seq_groups * a.gt, per = tok * a.parts;
+    const uint32_t r = blockIdx.x >> 3, k = r / per, rest = r - k * per;
+    const uint32_t pair = (blockIdx.x & 7) + 8 * k;  // (layer, kv-head, sequence)
+    const uint32_t heads = (uint32_t)a.launch_layers * a.n_kv_heads;
+    const uint32_t lh = pair / a.launch_seqs, s = pair - lh * a.launch_seqs;
+    const uint32_t i = rest / a.parts, g = (s0 + s) * a.seq_groups + i / a.gt - a.group0;  // the token's group
+    if (lh >= heads || g >= (uint32_t)a.n_groups) return;
+    part = rest - i * a.parts;
+    item = (g * a.gt + i % a.gt) * heads + lh;
+  }
   const AttendItem it = attend_item(a, item);
   const int total = min(it.pages, a.n_pages), c0 = part * a.part_pages, cnt = min(total - c0, a.part_pages);
   if (cnt <= 0) return;
@@ -731,13 +1036,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
   // the wave's u-th page is page (u / NB) 4 NB + NB wave + u % NB of the part
   auto nth = [&](int u) { return u / NB * 4 * NB + NB * wave + u % NB; };
-  int my_page = 0, my_phys = 0;
-  auto ids = [&](int u0) {  // lane i: the wave's page u0 + i (past the part's end its last one)
-    const int i = c0 + min(nth(u0 + lane), cnt - 1);
-    my_page = chosen ? list[i] : i;
-    my_phys = pt[my_page];
-  };
-  ids(0);
+  const int mine = c0 + min(nth(lane), cnt - 1);  // (past the part's end its last page)
+  const int my_page = chosen ? list[mine] : mine, my_phys = pt[my_page];
   const int call_l = a.layer - a.layer0 + it.l;
   const size_t qrow = ((it.row * a.n_layers + call_l) * a.n_q_heads + (size_t)it.h * G + min(col, G - 1)) * D;
   u32x4 q[NU];
@@ -868,23 +1168,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
         for (int i = 0; i < NU; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(r.vf[i][e], p[0][e], acc[i], 0, 0, 0);
     }
   };
-  // two batches of registers in turn; ids are read again every 64 pages of the wave, when
-  // the next batch is the first of the new ones (64 / NB batches: an even number)
-  Regs ra, rb;
-  if (NB * wave < cnt) load(0, ra);
-  for (int v0 = 0, k0 = NB * wave; k0 < cnt; v0 += 64) {
-    for (int u = 0; u < 64 && k0 < cnt; u += 2 * NB) {
-      const int page_k1 = k0 + 4 * NB, page_k2 = k0 + 8 * NB;
-      if (page_k1 < cnt) load(u + NB, rb);
-      work(u, k0, ra);
-      const bool turn = u + 2 * NB == 64;
-      if (page_k2 < cnt && !turn) load(u + 2 * NB, ra);
-      if (page_k1 < cnt) work(u + NB, page_k1, rb);
-      if (page_k2 < cnt && turn) {
-        ids(v0 + 64);
-        load(0, ra);
-      }
-      k0 = page_k2;
+  const int nb = (cnt - NB * wave + 4 * NB - 1) / (4 * NB);  // the wave's batches
+  auto step = [&](int i, Regs& r) __attribute__((always_inline)) { work(NB * i, NB * wave + 4 * NB * i, r); };
+  if (cnt > NB * wave) {
+    Regs ra, rb;
+    load(0, ra);
+    int i = 0;
+    for (; i + 2 < nb; i += 2) {
+      load(NB * (i + 1), rb);
+      step(i, ra);
+      load(NB * (i + 2), ra);
+      step(i + 1, rb);
+    }
+    if (nb - i == 2) {
+      load(NB * (i + 1), rb);
+      step(i, ra);
+      step(i + 1, rb);
+    } else {
+      step(i, ra);
     }
   }
   lsum += __shfl_xor(lsum, 16);
@@ -912,7 +1213,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
     if (a.parts == 1) {
       store_x4<BF16>(a, it, g, d, D, o * (1.f / den));
     } else {
-      const size_t w = (item * a.parts + part) * G + g;
+      const size_t w = ((size_t)item * a.parts + part) * G + g;
       *(f32x4*)(a.part_acc + w * D + d) = o;
       if (d == 0) *(float2*)(a.part_ml + 2 * w) = make_float2(mm, den);
     }
@@ -922,24 +1223,40 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
 // The merge of an item's parts: o = sum_j acc_j 2^(m_j - m*) / sum_j l_j 2^(m_j - m*).
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
-  const size_t item = blockIdx.x;
+  const uint32_t item = blockIdx.x;
   const AttendItem it = attend_item(a, item);
   if (it.pages == 0) return;
   const int G = a.group, D = a.head_dim;
   const int n = (min(it.pages, a.n_pages) + a.part_pages - 1) / a.part_pages;
   for (int e = threadIdx.x; e < G * (D / 4); e += 256) {
     const int g = e / (D / 4), d = e % (D / 4) * 4;
-    const size_t w0 = item * a.parts * G + g;
-    float mm = kNegInf;
-    for (int j = 0; j < n; ++j) mm = fmaxf(mm, a.part_ml[2 * (w0 + (size_t)j * G)]);
+    const size_t w0 = (size_t)item * a.parts * G + g;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f;
-    for (int j = 0; j < n; ++j) {
-      const size_t w = w0 + (size_t)j * G;
-      const float2 ml = *(const float2*)(a.part_ml + 2 * w);
-      const float f = exp2f(ml.x - mm);
-      den += f * ml.y;
-      o += f * *(const f32x4*)(a.part_acc + w * D + d);
+    float mm = kNegInf, den = 0.f;
+    for (int j0 = 0; j0 < n; j0 += 8) {  // (slots past the last part read it again and weigh nothing)
+      f32x4 v[8];
+      float2 ml[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const size_t w = w0 + (size_t)min(j0 + j, n - 1) * G;
+        v[j] = *(const f32x4*)(a.part_acc + w * D + d);
+        ml[j] = *(const float2*)(a.part_ml + 2 * w);
+      }
+      float top = mm;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+      const float r = mm == top ? 1.f : exp2f(mm - top);
+      mm = top;
+      den *= r;
+      o *= r;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float f = j0 + j < n ? exp2f(ml[j].x - mm) : 0.f;
+        if (j0 + j < n) {
+          den += f * ml[j].y;
+          o += f * v[j];
+        }
+      }
     }
     store_x4<BF16>(a, it, g, d, D, o * (1.f / den));
   }
@@ -949,8 +1266,12 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
 
 // ------------------------------------------------------------------ launchers
 
-hipError_t launch_append_rows(const AppendRowsArgs& a, bool bf16, hipStream_t st, const Timing* tm) {
-  const size_t blocks = (size_t)a.n_seqs * a.slots * a.n_layers;
+hipError_t launch_append_rows(const AppendRowsArgs& a0, bool bf16, hipStream_t st, const Timing* tm) {
+  AppendRowsArgs a = a0;
+  const int unit = bf16 ? 8 : 4, nslot = (a.head_dim - (a.halves ? a.rot_dim / 2 : 0)) / unit;
+  const int tasks = (a.n_tokens < kPage ? a.n_tokens : kPage) * a.n_q_heads * nslot;  // of a page, at most
+  a.q_blocks = a.q ? (tasks + kAppendTasks - 1) / kAppendTasks : 0;
+  const size_t blocks = (size_t)a.n_seqs * a.slots * a.n_layers * (2 + a.q_blocks);
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   if (bf16) return go(k_append_rows<true>, grid, dim3(256), 0, st, t0(tm), t1(tm), a);
@@ -971,10 +1292,14 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
   if (items > 0x7FFFFFFFu || groups * a.chunks > 0x7FFFFFFFu) return hipErrorInvalidValue;
   const int pages = a.score_row;
   if (!score || pages <= kPickPages) {
-    const dim3 grid((unsigned)groups);
-    if (!score || pages <= 128) return go(k_page_pick<2>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
-    if (pages <= 256) return go(k_page_pick<4>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
-    return go(k_page_pick<8>, grid, dim3(512), 0, st, t0(tm), t1(tm), a);
+    // Many work-groups: four tiles per wave, so that more of them are resident (16 of 2 waves
+    // per compute unit); else 8 waves, which read the summaries sooner. 4224 work-groups of
+    // up to 129 pages: see the launch's figures in k_page_pick.
+    const bool many = groups > 4 * (size_t)a.num_cus && a.gt == 1;
+    auto run = [&](auto kernel, int waves) { return go(kernel, dim3((unsigned)groups), dim3(64 * waves), 0, st, t0(tm), t1(tm), a); };
+    if (!score || pages <= 128) return many ? run(k_page_pick<2, 2>, 2) : run(k_page_pick<2, 8>, 8);
+    if (pages <= 256) return many ? run(k_page_pick<4, 4>, 4) : run(k_page_pick<4, 8>, 8);
+    return run(k_page_pick<8, 8>, 8);
   }
   const hipError_t e = go(k_page_score, dim3((unsigned)(groups * a.chunks)), dim3(256), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;
@@ -985,10 +1310,14 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
   return go(k_page_select<16, true>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
 }
 
-hipError_t launch_attend(const AttendArgs& a, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
-  const size_t items = (size_t)a.n_groups * a.gt * a.launch_layers * a.n_kv_heads;
-  if (items * a.parts > 0x7FFFFFFFu) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(items * a.parts));
+hipError_t launch_attend(const AttendArgs& a0, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
+  const size_t items = (size_t)a0.n_groups * a0.gt * a0.launch_layers * a0.n_kv_heads;
+  AttendArgs a = a0;
+  a.launch_seqs = (a.group0 + a.n_groups - 1) / a.seq_groups - a.group0 / a.seq_groups + 1;
+  const size_t pairs = (size_t)a.launch_seqs * a.launch_layers * a.n_kv_heads;
+  const size_t blocks = (a.n_tokens == 1 ? items : (pairs + 7) / 8 * 8 * a.seq_groups * a.gt) * a.parts;
+  if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
   hipError_t e = hipErrorInvalidValue;
   auto run = [&](auto kernel) { e = go(kernel, grid, dim3(256), 0, st, t0(tm), t1(tm), a); };
   if (a.bf16) {

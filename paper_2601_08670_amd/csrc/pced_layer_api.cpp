@@ -46,7 +46,7 @@ AttendPlan attend_plan(const pced_ctx* c, const AttendArgs& a, int max_pages, bo
   const int cnt = std::min(max_pages, a.n_pages);
   // two work-groups per compute unit, as far as a part keeps two batches of pages per wave
   const size_t want = std::max<size_t>(1, 2 * (size_t)c->num_cus / items);
-  p.part_pages = std::max<int>({min_part, ceil_div(ceil_div(cnt, (long)want), 8) * 8, 8});
+  p.part_pages = std::min(std::max<int>({min_part, ceil_div(ceil_div(cnt, (long)want), 8) * 8, 8}), kAttendPart);
   p.parts = ceil_div(cnt, p.part_pages);
   size_t o = 0;
   auto take = [&](size_t n) { const size_t at = o; o = align_up(o + n); return at; };
@@ -64,7 +64,6 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
   int max_pages = 0;
   for (int s = 0; s < c->S; ++s) max_pages = std::max(max_pages, (c->len[s] + a.n_tokens - 1) / kPage + 1);
   a.score_row = ceil_div(max_pages, 16) * 16;
-  a.chunks = ceil_div(max_pages, kScorePages);
   const int all = c->S * a.seq_groups;
   // as many layers and groups per launch as the workspace takes
   int groups = all, layers = a.n_layers, min_part = 8;
@@ -72,7 +71,7 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
   while (p.bytes > room) {
     if (layers > 1) layers = (layers + 1) / 2;
     else if (groups > 1) groups = (groups + 1) / 2;
-    else if (p.parts > 1) min_part = 2 * p.part_pages;
+    else if (p.parts > 1 && p.part_pages < kAttendPart) min_part = 2 * p.part_pages;
     else return fail(PCED_ERR_CAPACITY, "a row's page lists exceed the workspace");
     p = attend_plan(c, a, max_pages, select, groups, layers, min_part);
   }
@@ -100,6 +99,11 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
       a.n_groups = std::min(groups, all - g);
       const double part = share * a.n_groups * a.launch_layers * a.n_layers * cfg.n_kv_heads;
       if (select || a.pages_out) {
+        // the bounds of long sequences: six work-groups per compute unit, each at least 128 pages (9 books
+        // of up to 131072 tokens, us at 4 / 6 / 12 / 24: scattered pages 33 / 29 / 28 / 33, in order 23 / 20 / 20 / 25)
+        const long blocks = std::max<long>(1, 6L * c->num_cus / ((long)a.n_groups * a.launch_layers * a.n_kv_heads));
+        a.chunk_pages = ceil_div(ceil_div(max_pages, blocks), 128) * 128;
+        a.chunks = ceil_div(max_pages, a.chunk_pages);
         ProfScope ps(c, PCED_PROF_ATTN, select ? part * sums * (2.0 * cfg.head_dim + 4) : 0,
                      select ? part * sums * 4.0 * cfg.head_dim : 0);
         HIP_OK(launch_page_select(a, select, st, ps.timing()));
@@ -327,6 +331,7 @@ pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   a.maxpps = cfg.max_pages_per_seq;
   a.sum_row = summary_row(cfg.head_dim);
   a.bf16 = c->bf16;
+  a.num_cus = c->num_cus;
   a.n_pages = sel ? sel->n_pages : max_pages;
   a.first = sel ? sel->n_first : 0;
   a.last = sel ? sel->n_last : 1;
@@ -369,7 +374,8 @@ pced_status pced_fuse_adjusted(pced_ctx* c, const float* logits, int32_t refresh
     r = run_beta(c, logits, st);
     if (r != PCED_OK) return r;
   }
-  FuseArgs f = fuse_args(c, logits, tokens_out, 1, extra, adjusted_slices(c->cfg.vocab));
+  FuseArgs f = fuse_args(c, logits, tokens_out, 1, extra,
+                         ceil_div(c->cfg.vocab, adjusted_slice(c->cfg.vocab, c->B, c->num_cus)));
   f.none_token = 1;
   ProfScope ps(c, PCED_PROF_FUSE, (double)c->S * c->cfg.vocab * 4, 0);
   ProfScope pm(c, PCED_PROF_FUSE_MERGE, (double)c->B * f.nblk * 5 * 4, 0);

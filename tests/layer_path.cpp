@@ -16,7 +16,7 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t, const Timing*, const 
   return note("attend", a.layer, a.launch_layers, a.group0, a.n_groups, a.parts, a.part_pages, (long)end, (long)(uintptr_t)a.scores);
 }
 hipError_t launch_adjust(const AdjustArgs& a, int, int max_rows, int, hipStream_t) { return note("adjust", max_rows, (long)a.mask_row); }
-int adjusted_slices(int V) { return (V + 255) / 256; }
+int adjusted_slice(int, int, int) { return 256; }
 hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs&, int, hipStream_t, const Timing*, const Timing*) {
   return note("fuse_adjusted", a.none_token);
 }

@@ -168,7 +168,6 @@ def test_launches_cover_every_row_once_within_the_workspace(layer_host, lens, n,
     assert b.status == OK and b.bind() == OK and b.summarize() == OK and b.append(n, rope=None) == OK
     assert b.attend(n, sel) == OK, b.error()
     layers = b.layers
-    groups = len(lens) * -(-n // 16)
     seen = set()
     start = DEVICE
     end = DEVICE + layer_host.pced_workspace_bytes(ctypes.byref(b.cfg))
@@ -180,7 +179,9 @@ def test_launches_cover_every_row_once_within_the_workspace(layer_host, lens, n,
         assert start <= first <= last <= end
         want = -(-(max(lens) + n) // 16)
         assert parts * part_pages >= min(want, sel[0] if sel else want)
+    groups = len({j for _, j in seen})   # of up to some number of tokens of a sequence
     assert seen == {(i, j) for i in range(layers) for j in range(groups)}
+    assert groups % len(lens) == 0 and groups // len(lens) <= n
 
 
 def test_adjust_refusals(layer_host):
