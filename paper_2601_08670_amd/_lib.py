@@ -226,10 +226,20 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_torch_c = None
+
+
 def _stream(stream) -> int:
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    """The handle of `stream`, or of the current device's current stream (asked for directly: the
+    Stream object around it costs a short call more than its launch)."""
+    global _torch_c
+    if stream is not None:
+        return stream.cuda_stream
+    if _torch_c is None:
+        import torch
+        torch.cuda.current_stream()  # (initialises the device)
+        _torch_c = torch._C
+    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
 
 
 def _i32_array(values):
@@ -345,11 +355,13 @@ class Context:
                                         v_out.data_ptr(), _stream(stream)))
 
     def pced_append(self, layer, n_layers, n_tokens, rows: pced_rows, rope: Optional[pced_rope], q_out, stream=None):
-        _check(self.lib.pced_append(self.handle, int(layer), int(n_layers), int(n_tokens), ctypes.byref(rows),
-                                    None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream)))
+        status = self.lib.pced_append(self.handle, layer, n_layers, n_tokens, ctypes.byref(rows),
+                                      None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream))
+        if status:
+            _check(status)
 
     def pced_advance(self, n_tokens):
-        _check(self.lib.pced_advance(self.handle, int(n_tokens)))
+        _check(self.lib.pced_advance(self.handle, n_tokens))
 
     def pced_bind_summary(self, summary):
         _check(self.lib.pced_bind_summary(self.handle, _ptr(summary)))
@@ -359,9 +371,11 @@ class Context:
         _check(self.lib.pced_summarize(self.handle, _stream(stream)))
 
     def pced_attend(self, layer, n_layers, n_tokens, q, sel: Optional[pced_select], x_out, pages_out=None, stream=None):
-        _check(self.lib.pced_attend(self.handle, int(layer), int(n_layers), int(n_tokens), _ptr(q),
-                                    None if sel is None else ctypes.byref(sel), _ptr(x_out), _ptr(pages_out),
-                                    _stream(stream)))
+        status = self.lib.pced_attend(self.handle, layer, n_layers, n_tokens, _ptr(q),
+                                      None if sel is None else ctypes.byref(sel), _ptr(x_out), _ptr(pages_out),
+                                      _stream(stream))
+        if status:
+            _check(status)
 
     def pced_adjust_logits(self, logits, adjust: pced_adjust, out, stream=None):
         _check(self.lib.pced_adjust_logits(self.handle, _ptr(logits), ctypes.byref(adjust), _ptr(out),
@@ -369,9 +383,14 @@ class Context:
 
     def pced_fuse_adjusted(self, logits, refresh_beta, adjust: pced_adjust, tokens_out, extra: Optional[dict] = None,
                            stream=None):
-        so = _step_out(extra)
+        """extra: step outputs (winner, top1, top2, beta_used)."""
+        so = pced_step_out()
+        for name in ("winner", "top1", "top2", "beta_used"):
+            t = extra.get(name) if extra else None
+            if t is not None:
+                setattr(so, name, t.data_ptr())
         _check(self.lib.pced_fuse_adjusted(self.handle, _ptr(logits), int(refresh_beta), ctypes.byref(adjust),
-                                           _ptr(tokens_out), so[0] if so else None, _stream(stream)))
+                                           _ptr(tokens_out), ctypes.byref(so), _stream(stream)))
 
     def pced_get_lengths(self, n_seqs):
         out = (ctypes.c_int32 * n_seqs)()

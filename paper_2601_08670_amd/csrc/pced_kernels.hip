@@ -2229,34 +2229,64 @@ __global__ __launch_bounds__(256) void k_fuse(FuseArgs a) {
 // tokens' adjustments in registers for all of its rows. Entries that name no token
 // of the vocabulary count for nothing, and list bounds are cut to the lists' sizes.
 template <int SW>
-struct AdjustLds {
+struct alignas(16) AdjustLds {
   int cnt[SW];
   int bias[SW];
 };
-template <int SW>
-__device__ __forceinline__ void adjust_slice(const AdjustArgs& a, int b, int vb, AdjustLds<SW>& L) {
-  for (int i = threadIdx.x; i < SW; i += 256) L.cnt[i] = L.bias[i] = 0;
-  __syncthreads();
-  // (four entries of a thread at once)
-  auto scan = [&](const int32_t* list, const int32_t* off, int size, auto&& take) __attribute__((always_inline)) {
-    const int e0 = max(off[b], 0), e1 = min(off[b + 1], size);
-    for (int e = e0 + (int)threadIdx.x; e < e1; e += 1024) {
-      int v[4];
+// A query's part of a list, of which a thread has the entries e0 + thread + 256 j; the
+// first four are loaded ahead of the block's rows (loads return in order: behind the
+// rows' they would come last, and the block would wait for both in turn).
+struct AdjustScan {
+  const int32_t* list;
+  int e0, e1, v[4];
+  __device__ __forceinline__ void begin(const int32_t* l, const int32_t* off, int b, int size) {
+    list = l;
+    e0 = e1 = 0;
+    if (!l) return;
+    e0 = max(off[b], 0);
+    e1 = min(off[b + 1], size);
+    load(e0);
+  }
+  __device__ __forceinline__ void load(int e) {
+    if (e >= e1) return;  // uniform
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = list[min(e + 256 * j, e1 - 1)];
+    for (int j = 0; j < 4; ++j) v[j] = list[min(e + (int)threadIdx.x + 256 * j, e1 - 1)];
+  }
+  // take(token - vb, place) for every entry that names a token of the slice
+  template <class F>
+  __device__ __forceinline__ void each(int vb, int n, F&& take) {
+    for (int e = e0; e < e1; e += 1024) {
+      if (e > e0) load(e);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (e + 256 * j < e1 && v[j] >= vb && v[j] < a.V && v[j] - vb < SW) take(v[j] - vb, e + 256 * j);
+      for (int j = 0; j < 4; ++j) {
+        const int at = e + (int)threadIdx.x + 256 * j;
+        if (at < e1 && v[j] >= vb && v[j] - vb < n) take(v[j] - vb, at);
+      }
     }
-  };
-  if (a.history) scan(a.history, a.history_off, a.n_history, [&](int i, int) { atomicAdd(&L.cnt[i], 1); });
-  if (a.bias_token) scan(a.bias_token, a.bias_off, a.n_bias, [&](int i, int e) { atomicMax(&L.bias[i], e + 1); });
-  __syncthreads();
-}
-// four tokens from vb + i on (bits of seen and open: one per token)
+  }
+};
+template <int SW>
+struct AdjustSlice {
+  AdjustScan history, bias;
+  __device__ __forceinline__ void begin(const AdjustArgs& a, int b, AdjustLds<SW>& L) {
+    history.begin(a.history, a.history_off, b, a.n_history);
+    bias.begin(a.bias_token, a.bias_off, b, a.n_bias);
+    for (int i = threadIdx.x; i < SW / 2; i += 256) ((int4*)&L)[i] = make_int4(0, 0, 0, 0);
+  }
+  // listed(token - vb): once or more for every token that the lists name
+  template <class F>
+  __device__ __forceinline__ void end(const AdjustArgs& a, int vb, AdjustLds<SW>& L, F&& listed) {
+    const int n = min(SW, a.V - vb);
+    __syncthreads();
+    history.each(vb, n, [&](int i, int) { atomicAdd(&L.cnt[i], 1); listed(i); });
+    bias.each(vb, n, [&](int i, int e) { atomicMax(&L.bias[i], e + 1); listed(i); });
+    __syncthreads();
+  }
+};
+// the adjustments of four tokens from vb + i on (shift: f h; a bit of seen per token)
 struct AdjustTok4 {
   float rep, pres, shift[4], bias[4];
-  uint32_t seen, open;
+  uint32_t seen;
 };
 // which of the tokens v .. v + 3 (v a multiple of 4) the mask leaves open
 __device__ __forceinline__ uint32_t open_tokens(const AdjustArgs& a, int b, int v) {
@@ -2264,9 +2294,15 @@ __device__ __forceinline__ uint32_t open_tokens(const AdjustArgs& a, int b, int 
   const uint32_t in = a.V - v >= 4 ? 15u : (1u << (a.V - v)) - 1u;
   return a.mask ? (a.mask[(size_t)b * a.mask_row + (v >> 5)] >> (v & 31)) & in : in;
 }
+// whether some token of the wave's lanes, four from place i on each, is in the lists: most
+// slices of most vocabularies have few, and the rest needs no adjustment but the mask
 template <int SW>
-__device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, uint32_t open, int i,
-                                                  const AdjustLds<SW>& L) {
+__device__ __forceinline__ bool listed(const AdjustLds<SW>& L, int i) {
+  const int4 n = *(const int4*)&L.cnt[i], e = *(const int4*)&L.bias[i];
+  return __any((n.x | n.y | n.z | n.w | e.x | e.y | e.z | e.w) != 0);
+}
+template <int SW>
+__device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, int i, const AdjustLds<SW>& L) {
 #pragma clang fp contract(off)
   AdjustTok4 t;
   t.rep = a.repetition ? a.repetition[b] : 1.f;
@@ -2280,21 +2316,15 @@ __device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, ui
     t.bias[c] = e > 0 ? a.bias_value[e - 1] : 0.f;
     t.seen |= (n > 0 ? 1u : 0u) << c;
   }
-  t.open = open;
   return t;
 }
-template <bool MASK>
-__device__ __forceinline__ void adjust4(const AdjustTok4& t, float (&x)[4]) {
+__device__ __forceinline__ float adjust1(float x, bool seen, float rep, float shift, float pres, float bias) {
 #pragma clang fp contract(off)
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (t.seen >> c & 1) {
-      x[c] = x[c] > 0.f ? x[c] / t.rep : x[c] * t.rep;
-      x[c] = (x[c] - t.shift[c]) - t.pres;
-    }
-    x[c] += t.bias[c];
-    if (MASK && !(t.open >> c & 1)) x[c] = kNegInf;
+  if (seen) {
+    x = x > 0.f ? x / rep : x * rep;
+    x = (x - shift) - pres;
   }
+  return x + bias;
 }
 
 // Rows of adjusted logits: a block per (slice of 1024 tokens, row group of a query).
@@ -2310,6 +2340,8 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
   const int r0 = blockIdx.z * a.rows_per_block, r1 = min(n, r0 + a.rows_per_block);
   if (r0 >= r1) return;
   const uint32_t open = open_tokens(a, b, v);
+  AdjustSlice<SW> lists;
+  lists.begin(a, b, lds);
   const int o = v - min(v, max(a.V - 4, 0));  // a row's last load starts at V - 4 (V >= 4)
   f32x4 w[U];
   auto load = [&](int r) __attribute__((always_inline)) {
@@ -2322,9 +2354,11 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
     }
   };
   load(r0);
-  adjust_slice<SW>(a, b, vb, lds);
+  lists.end(a, vb, lds, [](int) {});
+  const bool some = listed<SW>(lds, i);
+  AdjustTok4 t{};
+  if (some) t = adjust_tok4<SW>(a, b, i, lds);
   if (v >= a.V) return;
-  const AdjustTok4 t = adjust_tok4<SW>(a, b, open, i, lds);
   for (int r = r0; r < r1; r += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -2337,7 +2371,11 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
         x[1] = o == 1 ? w[u][2] : w[u][3];
         x[2] = w[u][3];
       }
-      adjust4<true>(t, x);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (some) x[c] = adjust1(x[c], t.seen >> c & 1, t.rep, t.shift[c], t.pres, t.bias[c]);
+        if (!(open >> c & 1)) x[c] = kNegInf;
+      }
       float* out = a.out + (size_t)(s0 + r + u) * a.V + v;
       if (v + 4 <= a.V) {
         *(f32x4_a4*)out = f32x4{x[0], x[1], x[2], x[3]};
@@ -2356,15 +2394,25 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
 // the mask closes, and scores that are NaN or -inf, are nobody's choice: a slice without
 // any other has no candidate (expert 0). Where the mask closes all four nothing is read;
 // the first rows are on their way while the lists are read.
+// The lists name few of a slice's tokens, but some of most waves' 256, and their
+// adjustment costs several times what Eq. 2 does. So the sweep over the rows leaves
+// them out, and the block then takes them one by one, a thread per token and a few
+// experts, whose logits are in the caches by then; the best expert is a maximum over
+// (score, lower expert) keys, in whatever order it is taken. The slices of low tokens,
+// of which a history names most, start first.
 template <bool VEC, int SW>
-__global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 ? (VEC ? 3 : 2) : 4))) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
 #pragma clang fp contract(off)
   constexpr int RI = SW / 256, NB = 4;
   __shared__ AdjustLds<SW> lds;
+  __shared__ unsigned long long tbest[SW];  // of the listed tokens
+  __shared__ uint16_t tlist[SW];
+  __shared__ uint32_t tbits[SW / 32];
+  __shared__ int tcount;
   __shared__ float sbest[4][SW];
   __shared__ int sk[4][SW];
   __shared__ Top2 swave[4];
-  const int b = blockIdx.y, lane = threadIdx.x & 63;
+  const int b = blockIdx.x, slice = blockIdx.y, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool inl = b < kFuseInlineQueries;
   const int s0 = inl ? a.inl_seq0[b] : a.query_seq0[b];
@@ -2372,11 +2420,13 @@ __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d)
   const int e0 = inl ? a.inl_exp0[b] : a.query_exp0[b];
   const int per = (N + 3) / 4;                       // experts per wave
   const int k_lo = 1 + wave * per, k_hi = min(N, k_lo + per - 1);
-  const int vb = blockIdx.x * SW, v0 = vb + 4 * lane;
+  const int vb = slice * SW, v0 = vb + 4 * lane;
   const float* L0 = a.logits + (size_t)s0 * a.V;
   uint32_t open[RI];
 #pragma unroll
   for (int i = 0; i < RI; ++i) open[i] = open_tokens(d, b, v0 + 256 * i);
+  AdjustSlice<SW> lists;
+  lists.begin(d, b, lds);
   auto load = [&](const float* row, float (&x)[RI][4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
@@ -2397,50 +2447,100 @@ __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d)
   };
   load(L0, sa);
   load_batch(k_lo);
-  adjust_slice<SW>(d, b, vb, lds);
+  if (threadIdx.x == 0) tcount = 0;
+  if (threadIdx.x < SW / 32) tbits[threadIdx.x] = 0;
+  lists.end(d, vb, lds, [&](int u) {
+    const uint32_t bit = 1u << (u & 31);
+    if (atomicOr(&tbits[u >> 5], bit) & bit) return;  // (listed before)
+    if (!(open_tokens(d, b, (vb + u) & ~3) >> (u & 3) & 1)) return;
+    tlist[atomicAdd(&tcount, 1)] = (uint16_t)u;
+    tbest[u] = 0;
+  });
+  // the listed tokens, a thread per (token, KB experts): the first of them are on their way during the sweep
+  constexpr int KB = SW == 1024 ? 2 : SW == 512 ? 4 : 8;
+  const int groups = (N + KB - 1) / KB, tasks = tcount * groups;
+  int tu, tk;
+  float p0, pk[KB], pb[KB], pp[KB];
+  auto load_task = [&](int e) __attribute__((always_inline)) {  // (past the last one, or without any, some other's values)
+    const int at = max(min(e + (int)threadIdx.x, tasks - 1), 0), ti = (uint32_t)at / (uint32_t)groups;
+    tu = tasks > 0 ? tlist[ti] : 0;
+    tk = (at - ti * groups) * KB + 1;
+    p0 = L0[vb + tu];
+#pragma unroll
+    for (int j = 0; j < KB; ++j) {
+      const int k = min(tk + j, N);
+      pk[j] = L0[(size_t)k * a.V + vb + tu];
+      pb[j] = a.beta[e0 + k - 1];
+      pp[j] = a.prior[e0 + k - 1];
+    }
+  };
+  load_task(0);
   float best[RI][4];
   int bk[RI][4];
-  bool touched[RI];  // some token of the wave's is in the lists (most slices of most vocabularies have few)
 #pragma unroll
   for (int i = 0; i < RI; ++i) {
-    const AdjustTok4 t = adjust_tok4<SW>(d, b, open[i], 256 * i + 4 * lane, lds);
-    touched[i] = __any(t.seen || t.bias[0] != 0.f || t.bias[1] != 0.f || t.bias[2] != 0.f || t.bias[3] != 0.f);
-    if (touched[i]) adjust4<false>(t, sa[i]);
+    open[i] &= ~(tbits[8 * i + (lane >> 3)] >> (4 * (lane & 7)));
 #pragma unroll
     for (int c = 0; c < 4; ++c) { best[i][c] = kNegInf; bk[i][c] = 0; }
   }
   for (int kb = k_lo; kb <= k_hi; kb += NB) {
 #pragma unroll
-    for (int i = 0; i < RI; ++i) {
-      if (touched[i]) {
-        const AdjustTok4 t = adjust_tok4<SW>(d, b, open[i], 256 * i + 4 * lane, lds);
+    for (int j = 0; j < NB; ++j) {
+      if (kb + j > k_hi) break;  // uniform
+      const float coef = 1.0f + cb[j];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) adjust4<false>(t, x[j][i]);
-      }
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        if (kb + j > k_hi) break;  // uniform
+      for (int i = 0; i < RI; ++i)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float t1 = (1.0f + cb[j]) * x[j][i][c];
+          const float t1 = coef * x[j][i][c];
           const float t2 = cb[j] * sa[i][c];
           const float val = (t1 - t2) + cp[j];
           const bool up = val > best[i][c];
           best[i][c] = up ? val : best[i][c];
           bk[i][c] = up ? kb + j : bk[i][c];
         }
-      }
     }
     if (kb + NB <= k_hi) load_batch(kb + NB);
   }
 #pragma unroll
-  for (int i = 0; i < RI; ++i)
+  for (int i = 0; i < RI; ++i) {
+    float o[4];
+    int ok[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const bool in = open[i] >> c & 1;
-      sbest[wave][256 * i + 4 * lane + c] = in ? best[i][c] : kNegInf;
-      sk[wave][256 * i + 4 * lane + c] = in ? bk[i][c] : 0;
+      o[c] = in ? best[i][c] : kNegInf;
+      ok[c] = in ? bk[i][c] : 0;
     }
+    *(f32x4*)&sbest[wave][256 * i + 4 * lane] = f32x4{o[0], o[1], o[2], o[3]};
+    *(int4*)&sk[wave][256 * i + 4 * lane] = make_int4(ok[0], ok[1], ok[2], ok[3]);
+  }
+  __syncthreads();
+  for (int e = 0; e < tasks; e += 256) {
+    if (e > 0) load_task(e);
+    if (e + (int)threadIdx.x >= tasks) break;
+    const int c = tu & 3;
+    const AdjustTok4 t = adjust_tok4<SW>(d, b, tu & ~3, lds);
+    const float sh = c == 0 ? t.shift[0] : c == 1 ? t.shift[1] : c == 2 ? t.shift[2] : t.shift[3];
+    const float bi = c == 0 ? t.bias[0] : c == 1 ? t.bias[1] : c == 2 ? t.bias[2] : t.bias[3];
+    const bool seen = t.seen >> c & 1;
+    const float y0 = adjust1(p0, seen, t.rep, sh, t.pres, bi);
+    float top = kNegInf;
+    int who = 0;
+#pragma unroll
+    for (int j = 0; j < KB; ++j) {  // (experts past the last repeat it: no higher)
+      const float yk = adjust1(pk[j], seen, t.rep, sh, t.pres, bi);
+      const float t1 = (1.0f + pb[j]) * yk;
+      const float t2 = pb[j] * y0;
+      const float val = (t1 - t2) + pp[j];
+      who = val > top ? tk + j : who;
+      top = val > top ? val : top;
+    }
+    if (who > 0) {
+      const uint32_t f = __float_as_uint(top + 0.f), key = f & 0x80000000u ? ~f : f | 0x80000000u;  // fp32 order
+      atomicMax(&tbest[tu], (unsigned long long)key << 32 | (uint32_t)~who);
+    }
+  }
   __syncthreads();
   Top2 cand{kNegInf, 0x7FFFFFFF, 0, kNegInf, 0x7FFFFFFF};
 #pragma unroll
@@ -2455,6 +2555,14 @@ __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d)
     }
     if (vb + u < a.V && k > 0) cand = merge(cand, Top2{y, vb + u, k, kNegInf, 0x7FFFFFFF});
   }
+  for (int i = threadIdx.x; i < tcount; i += 256) {
+    const int u = tlist[i];
+    const unsigned long long w = tbest[u];
+    if (w == 0) continue;
+    const uint32_t key = (uint32_t)(w >> 32);
+    const float y = __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+    cand = merge(cand, Top2{y, vb + u, (int)~(uint32_t)w, kNegInf, 0x7FFFFFFF});
+  }
   cand = wave_top2(cand);
   if (lane == 0) swave[wave] = cand;
   __syncthreads();
@@ -2462,7 +2570,7 @@ __global__ __launch_bounds__(256) void k_fuse_adjusted(FuseArgs a, AdjustArgs d)
     Top2 r = swave[0];
 #pragma unroll
     for (int w = 1; w < 4; ++w) r = merge(r, swave[w]);
-    float* p = a.part + ((size_t)b * a.nblk + blockIdx.x) * 5;
+    float* p = a.part + ((size_t)b * a.nblk + slice) * 5;
     p[0] = r.v1; p[1] = __int_as_float(r.i1); p[2] = __int_as_float(r.k1);
     p[3] = r.v2; p[4] = __int_as_float(r.i2);
   }
@@ -4076,16 +4184,21 @@ hipError_t launch_agg(const AggArgs& a, int n_exp, int n_queries, hipStream_t st
 }
 
 int adjusted_slice(int V, int n_queries, int num_cus) {
-  return (long)n_queries * ((V + 511) / 512) >= 2L * num_cus ? 512 : 256;
+  for (int sw = 1024; sw > 256; sw /= 2)
+    if ((long)n_queries * ((V + sw - 1) / sw) >= 2L * num_cus) return sw;
+  return 256;
 }
 
 hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st, const Timing* tm,
                                 const Timing* tm_merge) {
   // a.nblk: slices of adjusted_slice() tokens
-  const bool wide = (a.V + a.nblk - 1) / a.nblk > 256, vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;  // (V >= 2)
-  auto run = [&](auto kernel) { return go(kernel, dim3(a.nblk, n_queries), dim3(256), 0, st, t0(tm), t1(tm), a, d); };
-  const hipError_t e = wide ? (vec ? run(k_fuse_adjusted<true, 512>) : run(k_fuse_adjusted<false, 512>))
-                            : (vec ? run(k_fuse_adjusted<true, 256>) : run(k_fuse_adjusted<false, 256>));
+  const int per = (a.V + a.nblk - 1) / a.nblk;
+  const bool vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;  // (V >= 2)
+  auto run = [&](auto kernel) { return go(kernel, dim3(n_queries, a.nblk), dim3(256), 0, st, t0(tm), t1(tm), a, d); };
+  const hipError_t e =
+      per > 512   ? (vec ? run(k_fuse_adjusted<true, 1024>) : run(k_fuse_adjusted<false, 1024>))
+      : per > 256 ? (vec ? run(k_fuse_adjusted<true, 512>) : run(k_fuse_adjusted<false, 512>))
+                  : (vec ? run(k_fuse_adjusted<true, 256>) : run(k_fuse_adjusted<false, 256>));
   if (e != hipSuccess) return e;
   return go(k_fuse_final, dim3(n_queries), dim3(kFuseBlock), 0, st, t0(tm_merge), t1(tm_merge), a);
 }

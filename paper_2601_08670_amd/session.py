@@ -12,9 +12,15 @@ import numpy as np
 from . import _lib
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 class Adjust:
@@ -88,6 +94,8 @@ class PcedSession:
         if poison:  # all-ones bytes: NaN in bf16 and f32, to expose reads of unwritten memory
             for t in (self.k_pool, self.v_pool, self.ctx.workspace):
                 t.fill_(255)
+        self._dtypes = (torch.bfloat16, torch.int16, torch.uint16) if dtype == "bf16" else (torch.float32,)
+        self._rows, self._ropes, self._out_like = _lib.pced_rows(), {}, {}
         self.n_experts: list = []
         self.S = 0
         self.B = 0
@@ -133,6 +141,8 @@ class PcedSession:
         self.ctx.pced_load_caches(n_experts, cache_len, src_k, src_v, self.k_pool, self.v_pool, relevance,
                                   gamma=gamma, beta=beta, page_table=page_table,
                                   reserve_tokens=reserve_tokens)
+        # (shapes of fuse_adjusted's outputs: empty_like takes a third less time than a shape and a type)
+        self._out_like = self.out_buffers(("winner", "top1", "top2", "beta_used"))
 
     # ----------------------------------------------------------------- steps
     def out_buffers(self, want=("logits", "winner", "top1", "top2", "beta_used")):
@@ -177,44 +187,55 @@ class PcedSession:
     # ------------------------------------------------------ layer-wise calls
     def _storage(self, t, name):
         """A tensor of the session's storage type (bf16 values or their bits, or float32)."""
-        torch = _torch()
-        if t.dtype not in ((torch.bfloat16, torch.int16, torch.uint16) if self.dtype == "bf16" else (torch.float32,)):
+        if t.dtype not in self._dtypes:
             raise ValueError(f"{name}: {t.dtype} in a session of {self.dtype}")
         return t
 
-    def _layers(self, layer, n_layers):
-        return int(layer), self.geom["n_layers"] - int(layer) if n_layers is None else int(n_layers)
-
     def _row_stride(self, t, name, n_tokens, n_layers, heads):
         """Elements from one row of [S * n_tokens][n_layers][heads][D] to the next."""
-        shape = (self.S * n_tokens, n_layers, heads, self.geom["head_dim"])
-        if tuple(self._storage(t, name).shape) != shape:
+        d = self.geom["head_dim"]
+        shape = (self.S * n_tokens, n_layers, heads, d)
+        if t.shape != shape:
             raise ValueError(f"{name}: {tuple(t.shape)}, not {shape}")
-        inner = (heads * shape[3], shape[3], 1)
-        if any(n > 1 and st != want for n, st, want in zip(shape[1:], t.stride()[1:], inner)):
+        self._storage(t, name)
+        if t.is_contiguous():
+            return n_layers * heads * d
+        st = t.stride()
+        if (d > 1 and st[3] != 1) or (heads > 1 and st[2] != d) or (n_layers > 1 and st[1] != heads * d):
             raise ValueError(f"{name}: a row's elements must follow each other")
-        return t.stride(0) if shape[0] > 1 else n_layers * heads * shape[3]
+        return st[0] if shape[0] > 1 else n_layers * heads * d
+
+    def _rope(self, rope):
+        """(theta, rot_dim, halves) as the library takes it."""
+        if rope is None:
+            return None
+        r = self._ropes.get(rope)
+        if r is None:
+            theta, rot, halves = rope
+            r = self._ropes[rope] = _lib.pced_rope(theta=theta, rot_dim=rot, halves=int(bool(halves)))
+        return r
 
     def append(self, q, k, v, n_tokens=1, rope=None, layer=0, n_layers=None, q_out=None):
         """pced_append of layers [layer, layer + n_layers) (default: to the last): rows
         [S * n_tokens][n_layers][heads][D], which may be apart (views of one projection's
         output); q None: K / V only. ``rope``: (theta, rot_dim, halves) or None. Returns the
         rotated q rows (``q_out`` or a new tensor)."""
-        torch = _torch()
-        layer, n_layers = self._layers(layer, n_layers)
         g = self.geom
-        rows = _lib.pced_rows(k=k.data_ptr(), v=v.data_ptr(),
-                              k_row=self._row_stride(k, "k", n_tokens, n_layers, g["n_kv_heads"]),
-                              v_row=self._row_stride(v, "v", n_tokens, n_layers, g["n_kv_heads"]))
+        if n_layers is None:
+            n_layers = g["n_layers"] - layer
+        rows = self._rows
+        rows.k_row = self._row_stride(k, "k", n_tokens, n_layers, g["n_kv_heads"])
+        rows.v_row = self._row_stride(v, "v", n_tokens, n_layers, g["n_kv_heads"])
+        rows.k, rows.v, rows.q, rows.q_row = k.data_ptr(), v.data_ptr(), None, 0
         if q is not None:
-            rows.q, rows.q_row = q.data_ptr(), self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"])
+            rows.q_row = self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"])
+            rows.q = q.data_ptr()
             if q_out is None:
-                q_out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
-            elif tuple(self._storage(q_out, "q_out").shape) != tuple(q.shape) or not q_out.is_contiguous():
+                torch = _torch()
+                q_out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            elif self._storage(q_out, "q_out").shape != q.shape or not q_out.is_contiguous():
                 raise ValueError("q_out: q's shape, contiguous")
-        theta, rot, halves = rope if rope is not None else (2.0, 0, False)
-        self.ctx.pced_append(layer, n_layers, n_tokens, rows,
-                             _lib.pced_rope(theta=theta, rot_dim=rot, halves=int(bool(halves))), q_out)
+        self.ctx.pced_append(layer, n_layers, n_tokens, rows, self._rope(rope), q_out)
         return q_out
 
     def advance(self, n_tokens=1):
@@ -233,27 +254,28 @@ class PcedSession:
         """pced_attend: q as append returned it; ``select``: (n_pages, n_first, n_last) or None
         for all pages. Returns {"x": [S * n_tokens][n_layers][Hq * D]}, and with "pages" in
         ``want`` the pages [S * n_tokens][n_layers][Hkv][n_pages]."""
-        torch = _torch()
-        layer, n_layers = self._layers(layer, n_layers)
-        g = self.geom
-        if set(want) - {"pages"}:
-            raise ValueError(f"unknown outputs {sorted(set(want) - {'pages'})}")
+        torch, g = _torch(), self.geom
+        if n_layers is None:
+            n_layers = g["n_layers"] - layer
+        for name in want:
+            if name != "pages":
+                raise ValueError(f"unknown output {name}")
         rows, width = self.S * n_tokens, g["n_q_heads"] * g["head_dim"]
         if self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"]) != n_layers * width:
             raise ValueError("q: rows must follow each other")
         if x_out is None:
             x_out = torch.empty((rows, n_layers, width), dtype=q.dtype, device=q.device)
-        elif tuple(self._storage(x_out, "x_out").shape) != (rows, n_layers, width) or not x_out.is_contiguous():
+        elif self._storage(x_out, "x_out").shape != (rows, n_layers, width) or not x_out.is_contiguous():
             raise ValueError("x_out: [S * n_tokens][n_layers][Hq * D], contiguous")
-        out, sel = {"x": x_out}, None
+        out, sel, pages = {"x": x_out}, None, None
         if select is not None:
-            sel = _lib.pced_select(*(int(x) for x in select))
-            if "pages" in want:
-                out["pages"] = torch.empty((rows, n_layers, g["n_kv_heads"], max(0, sel.n_pages)), dtype=torch.int32,
-                                           device=q.device)
+            sel = _lib.pced_select(*select)
+            if want:
+                out["pages"] = pages = torch.empty((rows, n_layers, g["n_kv_heads"], max(0, sel.n_pages)),
+                                                   dtype=torch.int32, device=q.device)
         elif want:
             raise ValueError("pages without select")
-        self.ctx.pced_attend(layer, n_layers, n_tokens, q, sel, x_out, out.get("pages"))
+        self.ctx.pced_attend(layer, n_layers, n_tokens, q, sel, x_out, pages)
         return out
 
     # ------------------------------------------------------- adjusted logits
@@ -262,30 +284,33 @@ class PcedSession:
         return Adjust(self.B, self.geom["vocab"], **tensors)
 
     def _logits(self, t, name):
-        torch = _torch()
-        if t.dtype != torch.float32 or tuple(t.shape) != (self.S, self.geom["vocab"]) or not t.is_contiguous():
+        if t.dtype != _torch().float32 or t.shape != (self.S, self.geom["vocab"]) or not t.is_contiguous():
             raise ValueError(f"{name}: float32 [{self.S}][{self.geom['vocab']}], contiguous")
         return t
 
     def _adjust(self, adjust):
-        if (adjust.n_queries, adjust.vocab) != (self.B, self.geom["vocab"]):
+        if adjust.n_queries != self.B or adjust.vocab != self.geom["vocab"]:
             raise ValueError("the adjustments are another batch's")
         return adjust.struct
 
     def adjust_logits(self, logits, adjust, out=None):
         """pced_adjust_logits of [S][V] logits; ``out`` may be logits itself."""
-        torch = _torch()
-        out = torch.empty_like(logits) if out is None else self._logits(out, "out")
-        self.ctx.pced_adjust_logits(self._logits(logits, "logits"), self._adjust(adjust), out)
+        self._logits(logits, "logits")
+        out = _torch().empty_like(logits) if out is None else self._logits(out, "out")
+        self.ctx.pced_adjust_logits(logits, self._adjust(adjust), out)
         return out
 
     def fuse_adjusted(self, logits, adjust, refresh_beta=False, want=("winner", "top1", "top2", "beta_used")):
         """pced_fuse_adjusted: the tokens chosen over adjusted logits, and the wanted outputs."""
-        torch = _torch()
-        tokens = torch.empty(self.B, dtype=torch.int32, device=self.device)
-        extra = self.out_buffers(want) if want else None
-        self.ctx.pced_fuse_adjusted(self._logits(logits, "logits"), refresh_beta, self._adjust(adjust), tokens, extra)
-        return dict(extra or {}, tokens=tokens)
+        like = _torch().empty_like
+        self._logits(logits, "logits")
+        out = {"tokens": like(self._out_like["winner"])}
+        for name in want:
+            if name not in self._out_like:
+                raise ValueError(f"unknown output {name}")
+            out[name] = like(self._out_like[name])
+        self.ctx.pced_fuse_adjusted(logits, refresh_beta, self._adjust(adjust), out["tokens"], out)
+        return out
 
     def lengths(self):
         return self.ctx.pced_get_lengths(self.S)

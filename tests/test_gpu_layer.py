@@ -300,6 +300,45 @@ def test_attend(dtype, heads, layers, lens, T, sel):
     _check_attend(m, q, out, T, sel)
 
 
+@pytest.mark.parametrize("dtype,lens,T,sel", [
+    ("f32", [9000, 100], 1, (40, 2, 3)),        # bounds and choice in two launches, from here on
+    ("bf16", [20000, 8300], 2, (600, 1, 1)),
+    ("f32", [131500, 40], 1, (300, 0, 1)),
+    ("f32", [270000, 500], 1, (100, 1, 1)),     # keys in rounds
+])
+def test_attend_over_long_caches(dtype, lens, T, sel):
+    m = Model(lens, T, dtype, (4, 2, 64) if dtype == "bf16" else (2, 1, 8), seed=30)
+    m.sess.bind_summary()
+    m.sess.summarize()
+    q, out = _run_attend(m, T, sel)
+    _check_attend(m, q, out, T, sel)
+
+
+@pytest.mark.parametrize("kind", ["equal", "outlier", "steps", "many_steps"])
+def test_long_choices_among_crowded_bounds(kind):
+    """Bounds that fall into few places of their range: all equal, all but one close together, a few values."""
+    m = Model([300000 if kind == "many_steps" else 12000, 20], 1, "f32", (2, 1, 8), seed=31)
+    k, n = m.k[0], m.lens[0]
+    if kind == "equal":
+        k[:] = 0.5
+    elif kind == "outlier":
+        k *= 1e-4
+        k[:, 5000] = 1e4
+    else:
+        k[:] = torch.arange(n, device=DEV).div(16, rounding_mode="floor").remainder(5).float().view(1, -1, 1, 1) + 1
+    m.load()
+    m.sess.bind_summary()
+    m.sess.summarize()
+    for sel in ((100, 1, 1), (3, 1, 1), (700, 0, 2)):
+        q = m.rows(1)[0].abs()
+        kn, vn = m.rows(1)[1:]
+        m.sess.append(None, kn, vn)
+        out = m.sess.attend(q, select=sel, want=("pages",))
+        torch.cuda.synchronize()
+        pages = L.chosen_pages(_f64(q[0, 0]), np.concatenate([_f64(m.k[0][0, :, 0]), _f64(kn[0, 0])]), *sel)
+        assert out["pages"][0, 0, 0].tolist() == pages
+
+
 def test_attend_sharp_and_equal_scores():
     """Scores far apart (one token takes it all), and pages that measure the same: the lower ones are chosen."""
     m = Model([400, 333], 1, "bf16", (8, 2, 64), seed=8)
