@@ -454,7 +454,8 @@ hipError_t launch_append_rows(const AppendRowsArgs& a, bool bf16, hipStream_t st
 hipError_t launch_summarize(const SummaryArgs& a, bool bf16, hipStream_t st);
 // page bounds (score) and the lists of chosen pages
 hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, const Timing* tm = nullptr);
-hipError_t launch_attend(const AttendArgs& a, hipStream_t st, const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
+// pick: the lists are chosen by the same launch (n_tokens and parts 1, at most kPickPages pages)
+hipError_t launch_attend(const AttendArgs& a, bool pick, hipStream_t st, const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
 // RoPE table of GemmArgs::rope for positions 0 .. positions - 1, in fp64 rounded to fp32
 hipError_t launch_rope_table(float2* out, int positions, int head_dim, double log2_theta, hipStream_t st);
 

@@ -499,13 +499,25 @@ __device__ __forceinline__ const int32_t* page_list(const AttendArgs& a, const A
 // page's bound has one value however the work is split, and the choice of pages
 // is one and the same for every launch shape.
 
-// The smallest exponent whose scale keeps v, rounded, within 127 (it grows with v,
-// so the largest over a row's values is the row's). Sums are exact in fp64.
+// The smallest exponent whose scale keeps v >= 0, rounded to nearest, within 127 (it
+// grows with v, so the largest over a row's values is the row's): v's own exponent less
+// 6, and one more where v 2^-e would be 127.5 or more, which is where the fraction's
+// first 7 bits are all ones. Sums are exact in fp64.
 __device__ __forceinline__ int weight_exp(double v) {
-  if (!(v > 0.)) return -kSumExp;
-  int ex = ilogb(fmin(v, 1e300)) - 6;
-  if (rint(ldexp(v, -ex)) > 127.) ++ex;
-  return min(max(ex, -kSumExp), kSumExp);
+  return min(max((__double2hiint(v) + (1 << 13) >> 20) - 1023 - 6, -kSumExp), kSumExp);
+}
+
+// The largest of the lanes' values, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  auto step = [&](uint32_t y) { x = max(x, y); };
+  // (row shifts by 1, 2, 4, 8, then the rows' last lanes to the rows behind; lanes without a source keep their own)
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x111, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x112, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x114, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x118, 0xF, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x142, 0xA, 0xF, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x143, 0xC, 0xF, false));
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // The weights of one row's kv-head (q at its first head) by one wave, lane i holding
@@ -537,9 +549,8 @@ __device__ __forceinline__ void query_weights(const AttendArgs& a, const void* q
           dn[c] += (double)fminf(x[i][c], 0.f);
         }
   }
-  int ex = max(max(weight_exp(up[0]), weight_exp(up[1])), max(weight_exp(-dn[0]), weight_exp(-dn[1])));
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) ex = max(ex, __shfl_xor(ex, o));
+  const int mine = max(max(weight_exp(up[0]), weight_exp(up[1])), max(weight_exp(-dn[0]), weight_exp(-dn[1])));
+  const int ex = (int)wave_max((uint32_t)(mine + kSumExp)) - kSumExp;
   int8_t w[4];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -564,14 +575,19 @@ __device__ __forceinline__ void load_codes(const AttendArgs& a, size_t base, int
   for (int k = 0; k < 4; ++k) t.c[k] = *(const i32x4*)(code + min(64 * k, a.sum_row - 64));
   t.scale = a.scale[base + phys];
 }
-// bounds of pages 4 (lane / 16) .. + 3 of the tile for the token of column lane % 16
-__device__ __forceinline__ float4 tile_bounds(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4], int quad) {
+// the sums of pages 4 (lane / 16) .. + 3 of the tile for the token of column lane % 16
+__device__ __forceinline__ float4 tile_sums(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4]) {
   i32x4 c = {0, 0, 0, 0};
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (64 * k < a.sum_row) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.c[k], w[k], c, 0, 0, 0);
-  return make_float4((float)c[0] * __shfl(t.scale, 4 * quad), (float)c[1] * __shfl(t.scale, 4 * quad + 1),
-                     (float)c[2] * __shfl(t.scale, 4 * quad + 2), (float)c[3] * __shfl(t.scale, 4 * quad + 3));
+  return make_float4((float)c[0], (float)c[1], (float)c[2], (float)c[3]);
+}
+// the pages' bounds: sums times scales
+__device__ __forceinline__ float4 tile_bounds(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4], int quad) {
+  const float4 c = tile_sums(a, t, w);
+  return make_float4(c.x * __shfl(t.scale, 4 * quad), c.y * __shfl(t.scale, 4 * quad + 1), c.z * __shfl(t.scale, 4 * quad + 2),
+                     c.w * __shfl(t.scale, 4 * quad + 3));
 }
 
 // fp32 order as unsigned order; 0 is below every number's key
@@ -627,14 +643,24 @@ __device__ __forceinline__ AttendItem group_row(const AttendArgs& a, const Group
 }
 
 // The pages of one token from the keys of its candidates, page lo + 64 i + lane at
-// key[i] (0: no candidate), by one wave: the want-th highest key bit by bit, from
-// counts over the wave (done as soon as a bound has just `want` keys above it, which
-// takes about as many bits as tell neighbours apart), then the pages in order, each
-// at its place. want >= 1, and there are at least as many candidates.
+// key[i] (0: no candidate), by one wave: the want-th highest key bit by bit below the
+// bits that all keys share, from counts over the wave (done as soon as a bound has just
+// `want` keys above it, which takes about as many bits as tell neighbours apart), then
+// the pages in order, each at its place. want >= 1, and there are at least as many
+// candidates.
 template <int R>
 __device__ __forceinline__ void pick_pages(const uint32_t (&key)[R], int lo, int want, int32_t* list, int lane) {
-  uint32_t t = 0;
-  for (int b = 31; b >= 0; --b) {
+  uint32_t kmax = 0, kmin = 0;  // (kmin: of the complements)
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    kmax = max(kmax, key[i]);
+    kmin = max(kmin, key[i] ? ~key[i] : 0u);
+  }
+  kmax = wave_max(kmax);
+  kmin = ~wave_max(kmin);
+  int b = kmax == kmin ? -1 : 31 - __clz(kmax ^ kmin);
+  uint32_t t = b < 0 ? kmin : kmax >> b >> 1 << b << 1;
+  for (; b >= 0; --b) {
     const uint32_t c = t | (1u << b);
     int n = 0;
 #pragma unroll
@@ -663,6 +689,21 @@ __device__ __forceinline__ void pick_pages(const uint32_t (&key)[R], int lo, int
   }
 }
 
+// Keys of pages [lo, hi), page 64 i + lane at key[i], from their sums and scales in LDS (which hold 64 R)
+template <int R>
+__device__ __forceinline__ void page_keys(const float* sums, const float* scale, int lo, int hi, int lane,
+                                          uint32_t (&key)[R]) {
+  float x[R], y[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) { x[i] = sums[64 * i + lane]; y[i] = scale[64 * i + lane]; }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int p = 64 * i + lane;
+    const uint32_t k = order_key(x[i] * y[i]);
+    key[i] = p >= lo && p < hi ? k : 0u;
+  }
+}
+
 // The pages that need no choice: all of them, or the first and the last ones.
 // Returns how many are to be chosen between.
 __device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32_t* list, int i0, int step) {
@@ -683,7 +724,8 @@ template <int R, int W>
 __global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
   constexpr int NT = 4 * R / W, T = kAttendTokens;
   __shared__ __align__(16) int8_t w[16][256];  // (columns past the tokens' count for nothing)
-  __shared__ __align__(16) float bound[T][64 * R + 4];
+  __shared__ __align__(16) float bound[T][64 * R + 4];  // (sums, to be scaled)
+  __shared__ float scale[64 * R];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const GroupItem it = group_item(a, blockIdx.x);
@@ -706,8 +748,9 @@ __global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
       if (16 * (wave + W * i) < p1) {
-        const float4 o = tile_bounds(a, t[i], b, quad);
+        const float4 o = tile_sums(a, t[i], b);
         if (col < it.nt) *(float4*)&bound[col][16 * (wave + W * i) + 4 * quad] = o;
+        if (quad == 0) scale[16 * (wave + W * i) + col] = t[i].scale;
       }
     __syncthreads();
   }
@@ -719,11 +762,7 @@ __global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
     const int want = fixed_pages(a, row.pages, list, lane, 64);
     if (want == 0) continue;
     uint32_t key[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int p = 64 * i + lane;
-      key[i] = p >= a.first && p < row.pages - a.last ? order_key(bound[j][p]) : 0u;
-    }
+    page_keys<R>(bound[j], scale, a.first, row.pages - a.last, lane, key);
     pick_pages<R>(key, 0, want, list + a.first, lane);
   }
 }
@@ -999,7 +1038,10 @@ struct PageRegs {
   float vf[BF16 ? 1 : NU][4];
 };
 
-template <bool BF16, int NU>
+// PICK: the block chooses its item's pages itself, as k_page_pick does: one new token,
+// at most kPickPages pages, one part. The launch that this saves, and the list's way
+// through memory, cost more than the pages that wait behind the choice: see launch_attend.
+template <bool BF16, int NU, bool PICK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU > 6 ? 1 : 2, 4))) void k_attend(AttendArgs a) {
   using Regs = PageRegs<BF16, NU>;
   constexpr int NJ = BF16 ? 2 * NU : NU;  // 16-dim output blocks
@@ -1007,6 +1049,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   constexpr int DP = 16 * NJ + 4;
   __shared__ __align__(16) float sacc[4][kMaxGroup][DP];
   __shared__ float sm[4][kMaxGroup], sl[4][kMaxGroup];
+  __shared__ __align__(16) int8_t s_w[PICK ? 256 : 16];
+  __shared__ __align__(16) float s_bound[PICK ? kPickPages : 4];  // (sums, to be scaled)
+  __shared__ float s_scale[PICK ? kPickPages : 1];
+  __shared__ int32_t s_list[PICK ? kAttendPart : 1], s_phys[PICK ? kPickPages : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
   // Work-groups go to the eight dies in turn. With several new tokens, all those of one
@@ -1032,12 +1078,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   if (cnt <= 0) return;
   const int G = a.group, D = BF16 ? 32 * NU : a.head_dim;
   const bool chosen = it.pages > a.n_pages;
-  const int32_t* list = chosen ? page_list(a, it, item) : nullptr;
+  const int32_t* list = chosen && !PICK ? page_list(a, it, item) : nullptr;
   const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
-  // the wave's u-th page is page (u / NB) 4 NB + NB wave + u % NB of the part
-  auto nth = [&](int u) { return u / NB * 4 * NB + NB * wave + u % NB; };
-  const int mine = c0 + min(nth(lane), cnt - 1);  // (past the part's end its last page)
-  const int my_page = chosen ? list[mine] : mine, my_phys = pt[my_page];
   const int call_l = a.layer - a.layer0 + it.l;
   const size_t qrow = ((it.row * a.n_layers + call_l) * a.n_q_heads + (size_t)it.h * G + min(col, G - 1)) * D;
   u32x4 q[NU];
@@ -1050,6 +1092,59 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
       if (d >= D) q[i] = u32x4{0u, 0u, 0u, 0u};
     }
   }
+  if constexpr (PICK) {
+    // (the page ids do not wait for the length: pages that the sequence does not have get some id)
+    constexpr int R = kPickPages / 64;
+    int phys[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      phys[i] = 0;
+      if (16 * (wave + 4 * i) < a.score_row) phys[i] = max(pt[min(16 * (wave + 4 * i) + col, a.maxpps - 1)], 0);
+    }
+    int32_t* out = a.pages_out ? const_cast<int32_t*>(page_list(a, it, item)) : nullptr;
+    if (!chosen) {
+      if (out) fixed_pages(a, it.pages, out, tid, 256);
+    } else {
+      const int p1 = it.pages - a.last;
+      const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
+      CodeTile t[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (16 * (wave + 4 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (quad == 0) s_phys[16 * (wave + 4 * i) + col] = phys[i];
+      if (wave == 0)
+        query_weights(a, (const char*)a.q + (qrow - (size_t)min(col, G - 1) * D) * (BF16 ? 2 : 4), lane, s_w);
+      __syncthreads();
+      i32x4 w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = *(const i32x4*)&s_w[64 * k + 16 * quad];  // (every column the token's)
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (16 * (wave + 4 * i) < p1) {
+          const float4 o = tile_sums(a, t[i], w);
+          if (col == 0) *(float4*)&s_bound[16 * (wave + 4 * i) + 4 * quad] = o;
+          if (quad == 0) s_scale[16 * (wave + 4 * i) + col] = t[i].scale;
+        }
+      __syncthreads();
+      if (wave == 0) {
+        const int want = fixed_pages(a, it.pages, s_list, lane, 64);
+        if (want > 0) {
+          uint32_t key[R];
+          page_keys<R>(s_bound, s_scale, a.first, p1, lane, key);
+          pick_pages<R>(key, 0, want, s_list + a.first, lane);
+        }
+      }
+      __syncthreads();
+      if (out && tid < a.n_pages) out[tid] = s_list[tid];  // (n_pages <= kAttendPart)
+    }
+  }
+  // the wave's u-th page is page (u / NB) 4 NB + NB wave + u % NB of the part
+  auto nth = [&](int u) { return u / NB * 4 * NB + NB * wave + u % NB; };
+  const int mine = c0 + min(nth(lane), cnt - 1);  // (past the part's end its last page)
+  const int my_page = !chosen ? mine : PICK ? s_list[mine] : list[mine];
+  const int my_phys = PICK && chosen ? s_phys[my_page] : pt[my_page];
   const size_t lay = (size_t)(a.layer + it.l) * a.max_pages;
   const size_t tile = (size_t)kPage * D;
   auto load = [&](int u, Regs& r) __attribute__((always_inline)) {  // pages u .. u + NB - 1 of those in the lanes
@@ -1310,7 +1405,7 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
   return go(k_page_select<16, true>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
 }
 
-hipError_t launch_attend(const AttendArgs& a0, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
+hipError_t launch_attend(const AttendArgs& a0, bool pick, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
   const size_t items = (size_t)a0.n_groups * a0.gt * a0.launch_layers * a0.n_kv_heads;
   AttendArgs a = a0;
   a.launch_seqs = (a.group0 + a.n_groups - 1) / a.seq_groups - a.group0 / a.seq_groups + 1;
@@ -1320,19 +1415,20 @@ hipError_t launch_attend(const AttendArgs& a0, hipStream_t st, const Timing* tm,
   const dim3 grid((unsigned)blocks);
   hipError_t e = hipErrorInvalidValue;
   auto run = [&](auto kernel) { e = go(kernel, grid, dim3(256), 0, st, t0(tm), t1(tm), a); };
+  auto pick_or_not = [&](auto yes, auto no) { pick ? run(yes) : run(no); };
   if (a.bf16) {
-    if (a.head_dim == 128) run(k_attend<true, 4>);
-    else if (a.head_dim == 64) run(k_attend<true, 2>);
+    if (a.head_dim == 128) pick_or_not(k_attend<true, 4, true>, k_attend<true, 4, false>);
+    else if (a.head_dim == 64) pick_or_not(k_attend<true, 2, true>, k_attend<true, 2, false>);
   } else {
     switch ((a.head_dim + 15) / 16) {  // (head_dim <= 128)
-      case 1: run(k_attend<false, 1>); break;
-      case 2: run(k_attend<false, 2>); break;
-      case 3: run(k_attend<false, 3>); break;
-      case 4: run(k_attend<false, 4>); break;
-      case 5: run(k_attend<false, 5>); break;
-      case 6: run(k_attend<false, 6>); break;
-      case 7: run(k_attend<false, 7>); break;
-      case 8: run(k_attend<false, 8>); break;
+      case 1: pick_or_not(k_attend<false, 1, true>, k_attend<false, 1, false>); break;
+      case 2: pick_or_not(k_attend<false, 2, true>, k_attend<false, 2, false>); break;
+      case 3: pick_or_not(k_attend<false, 3, true>, k_attend<false, 3, false>); break;
+      case 4: pick_or_not(k_attend<false, 4, true>, k_attend<false, 4, false>); break;
+      case 5: pick_or_not(k_attend<false, 5, true>, k_attend<false, 5, false>); break;
+      case 6: pick_or_not(k_attend<false, 6, true>, k_attend<false, 6, false>); break;
+      case 7: pick_or_not(k_attend<false, 7, true>, k_attend<false, 7, false>); break;
+      case 8: pick_or_not(k_attend<false, 8, true>, k_attend<false, 8, false>); break;
     }
   }
   if (e != hipSuccess || a.parts == 1) return e;

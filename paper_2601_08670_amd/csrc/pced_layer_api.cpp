@@ -66,7 +66,12 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
   a.score_row = ceil_div(max_pages, 16) * 16;
   const int all = c->S * a.seq_groups;
   // as many layers and groups per launch as the workspace takes
-  int groups = all, layers = a.n_layers, min_part = 8;
+  int groups = all, layers = a.n_layers;
+  // One new token and few pages: one launch chooses them and attends to them, each item in one part. bf16, 5
+  // sequences of 4000 to 6000 tokens, us in one launch / in three (choice, parts, merge): 16 pages 14 / 20, 64 pages
+  // 19 / 22, 128 pages 24 / 25; 2 sequences: 64 pages 17 / 20, 128 pages 22 / 20.
+  const bool pick = select && a.n_tokens == 1 && max_pages <= kPickPages;
+  int min_part = pick && a.n_pages <= 64 ? kAttendPart : 8;
   AttendPlan p = attend_plan(c, a, max_pages, select, groups, layers, min_part);
   while (p.bytes > room) {
     if (layers > 1) layers = (layers + 1) / 2;
@@ -75,6 +80,7 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
     else return fail(PCED_ERR_CAPACITY, "a row's page lists exceed the workspace");
     p = attend_plan(c, a, max_pages, select, groups, layers, min_part);
   }
+  const bool fused = pick && p.parts == 1;
   char* ws = c->at<char>(c->lay.part_acc);
   a.scores = (float*)(ws + p.scores);
   a.list = (int32_t*)(ws + p.list);
@@ -98,7 +104,7 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
       a.group0 = g;
       a.n_groups = std::min(groups, all - g);
       const double part = share * a.n_groups * a.launch_layers * a.n_layers * cfg.n_kv_heads;
-      if (select || a.pages_out) {
+      if (!fused && (select || a.pages_out)) {
         // the bounds of long sequences: six work-groups per compute unit, each at least 128 pages (9 books
         // of up to 131072 tokens, us at 4 / 6 / 12 / 24: scattered pages 33 / 29 / 28 / 33, in order 23 / 20 / 20 / 25)
         const long blocks = std::max<long>(1, 6L * c->num_cus / ((long)a.n_groups * a.launch_layers * a.n_kv_heads));
@@ -111,7 +117,7 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
       ProfScope ps(c, PCED_PROF_ATTN, part * kv * 2 * kPage * cfg.head_dim * es, part * kv * 4 * kPage * cfg.head_dim * c->G);
       ProfScope pm(c, PCED_PROF_COMBINE, 0, 0);
       if (p.parts == 1) pm.drop();
-      HIP_OK(launch_attend(a, st, ps.timing(), pm.timing()));
+      HIP_OK(launch_attend(a, fused, st, ps.timing(), pm.timing()));
     }
   }
   return PCED_OK;

@@ -10,7 +10,8 @@ hipError_t launch_summarize(const SummaryArgs& a, bool, hipStream_t) { return no
 hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t, const Timing*) {
   return note("select", a.layer, a.launch_layers, a.group0, a.n_groups, score, a.gt);
 }
-hipError_t launch_attend(const AttendArgs& a, hipStream_t, const Timing*, const Timing*) {
+hipError_t launch_attend(const AttendArgs& a, bool pick, hipStream_t, const Timing*, const Timing*) {
+  if (pick) note("select", a.layer, a.launch_layers, a.group0, a.n_groups, 1, a.gt);
   const size_t items = (size_t)a.n_groups * a.gt * a.launch_layers * a.n_kv_heads;
   const size_t end = a.parts > 1 ? (uintptr_t)(a.part_ml + items * a.parts * a.group * 2) : (uintptr_t)(a.list + 1);
   return note("attend", a.layer, a.launch_layers, a.group0, a.n_groups, a.parts, a.part_pages, (long)end, (long)(uintptr_t)a.scores);
