@@ -502,7 +502,8 @@ pced_status pced_advance(pced_ctx* ctx, int32_t n_tokens);
  * Page summaries, for attention that reads part of a cache: per complete page,
  * layer and kv-head the largest and the smallest value of each key dimension over
  * the page's 16 keys, in int8 with a power of two as scale, rounded outward (1/32 of
- * the bf16 cache). pced_summary_bytes: size of the buffer for cfg (0 if invalid).
+ * the bf16 cache). NaN keys are left out, and keys beyond 127 * 2^64 count as that.
+ * pced_summary_bytes: size of the buffer for cfg (0 if invalid).
  * pced_bind_summary (host-only) gives the context a caller-owned device buffer of
  * that size, 256-byte aligned, without contents (NULL: none). pced_summarize brings
  * it up to date with the loaded caches and all appended tokens: call it after
@@ -532,7 +533,9 @@ typedef struct pced_select {
 /*
  * Attention of the new tokens, after pced_append of the same layers: row (s, i)
  * attends to tokens 0 .. len_s + i of its sequence, as far as they are in its pages
- * (grouped-query attention, scale 1/sqrt(head_dim)); sums and softmax in fp32.
+ * (grouped-query attention, scale 1/sqrt(head_dim)); sums and softmax in fp32. The
+ * work goes into the context's workspace in as many launches as that takes;
+ * pced_config.max_attn_chunks does not bound them.
  *   q          device [S * n_tokens][n_layers][Hq][D], storage type, 16-byte aligned
  *   sel        pages to attend to, or NULL: all
  *   x_out      device [S * n_tokens][n_layers][Hq * D], storage type, 16-byte aligned;
@@ -569,7 +572,7 @@ typedef struct pced_adjust {
   const int32_t* bias_off;     /* [B + 1]                                             */
   const uint32_t* mask;        /* [B] rows of mask_row words: bit v % 32 of word v / 32 */
   int64_t mask_row;            /* 0: ceil(V / 32)                                     */
-  int32_t n_history, n_bias;
+  int32_t n_history, n_bias;   /* 0 .. 2^30                                           */
 } pced_adjust;
 
 /*
@@ -594,10 +597,11 @@ pced_status pced_fuse_adjusted(pced_ctx* ctx, const float* logits, int32_t refre
 /* Kernel timing with HIP events attached to each kernel dispatch (start when
  * the kernel begins, stop when it completes). Classes: */
 enum {
-  PCED_PROF_APPEND = 0,  /* shared-history append and work planning */
+  PCED_PROF_APPEND = 0,  /* shared-history append and work planning; pced_append */
   PCED_PROF_ATTN = 1,    /* decode attention (pced_step, pced_generate: a
                             launch takes as many layers as the partial
-                            states leave room for; decoder stack: one) */
+                            states leave room for; decoder stack: one);
+                            pced_attend: choice of pages, attention */
   PCED_PROF_LMHEAD = 2,  /* LM head                                */
   PCED_PROF_BETA = 3,    /* dynamic beta (first step only)         */
   PCED_PROF_FUSE = 4,    /* Eq. 2 + Eq. 3 over materialised logits:

@@ -126,7 +126,9 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
 // The device form of a caller's adjustments
 pced_status adjust_args(const pced_ctx* c, const pced_adjust* d, AdjustArgs* out) {
   if (!d) return fail(PCED_ERR_INVALID_ARG, "adjust is NULL");
-  if (d->n_history < 0 || d->n_bias < 0) return fail(PCED_ERR_INVALID_ARG, "n_history and n_bias must be >= 0");
+  constexpr int kMaxList = 1 << 30;  // (the kernels' places in a list are 32-bit)
+  if (d->n_history < 0 || d->n_history > kMaxList || d->n_bias < 0 || d->n_bias > kMaxList)
+    return fail(PCED_ERR_INVALID_ARG, "n_history %d, n_bias %d: 0 .. 2^30", d->n_history, d->n_bias);
   if (d->history && !d->history_off) return fail(PCED_ERR_INVALID_ARG, "history without history_off");
   if (d->bias_token && (!d->bias_value || !d->bias_off))
     return fail(PCED_ERR_INVALID_ARG, "bias_token without bias_value or bias_off");
@@ -169,7 +171,7 @@ pced_status pced_append(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   a.k = rows->k;
   a.v = rows->v;
   a.q_out = q_out;
-  a.q_row = rows->q_row ? rows->q_row : qd;
+  a.q_row = rows->q && rows->q_row ? rows->q_row : qd;
   a.k_row = rows->k_row ? rows->k_row : kd;
   a.v_row = rows->v_row ? rows->v_row : kd;
   if (a.q_row < qd || a.k_row < kd || a.v_row < kd)
@@ -177,7 +179,7 @@ pced_status pced_append(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
                 (long long)a.v_row);
   // the kernel moves rows in 16-byte units
   if (((uintptr_t)rows->q | (uintptr_t)rows->k | (uintptr_t)rows->v | (uintptr_t)q_out) % 16 ||
-      (size_t)(rows->q ? a.q_row : 0) * es % 16 || (size_t)a.k_row * es % 16 || (size_t)a.v_row * es % 16)
+      (size_t)a.q_row * es % 16 || (size_t)a.k_row * es % 16 || (size_t)a.v_row * es % 16)
     return fail(PCED_ERR_INVALID_ARG, "rows and q_out must be 16-byte aligned, and the rows' distances too");
   if (q_out) {
     const size_t nq = ((R - 1) * a.q_row + qd) * es, nk = ((R - 1) * a.k_row + kd) * es, nv = ((R - 1) * a.v_row + kd) * es;

@@ -34,7 +34,7 @@ class Adjust:
     DTYPES = dict(history="int32", history_off="int32", repetition="float32", presence="float32", frequency="float32",
                   bias_token="int32", bias_value="float32", bias_off="int32", mask="int32")
 
-    def __init__(self, n_queries, vocab, **tensors):
+    def __init__(self, n_queries, vocab, device, **tensors):
         torch = _torch()
         unknown = set(tensors) - set(self.DTYPES)
         if unknown:
@@ -44,6 +44,8 @@ class Adjust:
         for name, t in self.tensors.items():
             if t.dtype != getattr(torch, self.DTYPES[name]):
                 raise ValueError(f"{name}: {t.dtype}, not {self.DTYPES[name]}")
+            if t.device != device:
+                raise ValueError(f"{name}: on {t.device}, the session is on {device}")
             if name == "mask":
                 if t.dim() != 2 or t.shape[0] < n_queries or t.stride(1) != 1 or t.shape[1] < -(-vocab // 32):
                     raise ValueError("mask: [queries][>= ceil(vocab / 32)] words, a row's words next to each other")
@@ -94,6 +96,7 @@ class PcedSession:
         if poison:  # all-ones bytes: NaN in bf16 and f32, to expose reads of unwritten memory
             for t in (self.k_pool, self.v_pool, self.ctx.workspace):
                 t.fill_(255)
+        self._device_index = self.k_pool.get_device()
         self._dtypes = (torch.bfloat16, torch.int16, torch.uint16) if dtype == "bf16" else (torch.float32,)
         self._rows, self._ropes, self._out_like = _lib.pced_rows(), {}, {}
         self.n_experts: list = []
@@ -189,6 +192,11 @@ class PcedSession:
         """A tensor of the session's storage type (bf16 values or their bits, or float32)."""
         if t.dtype not in self._dtypes:
             raise ValueError(f"{name}: {t.dtype} in a session of {self.dtype}")
+        return self._here(t, name)
+
+    def _here(self, t, name):
+        if t.get_device() != self._device_index:
+            raise ValueError(f"{name}: on {t.device}, the session is on {self.k_pool.device}")
         return t
 
     def _row_stride(self, t, name, n_tokens, n_layers, heads):
@@ -281,12 +289,12 @@ class PcedSession:
     # ------------------------------------------------------- adjusted logits
     def adjust(self, **tensors):
         """The loaded batch's adjustments (see Adjust) for adjust_logits and fuse_adjusted."""
-        return Adjust(self.B, self.geom["vocab"], **tensors)
+        return Adjust(self.B, self.geom["vocab"], self.k_pool.device, **tensors)
 
     def _logits(self, t, name):
         if t.dtype != _torch().float32 or t.shape != (self.S, self.geom["vocab"]) or not t.is_contiguous():
             raise ValueError(f"{name}: float32 [{self.S}][{self.geom['vocab']}], contiguous")
-        return t
+        return self._here(t, name)
 
     def _adjust(self, adjust):
         if adjust.n_queries != self.B or adjust.vocab != self.geom["vocab"]:

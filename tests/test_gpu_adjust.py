@@ -264,13 +264,15 @@ def test_session_refusals():
                 dict(presence=torch.zeros(1, device=DEV)), dict(presence=torch.zeros((2, 2), device=DEV)),
                 dict(bias_token=z, bias_off=z), dict(bias_token=z, bias_off=z, bias_value=torch.zeros(2, device=DEV)),
                 dict(mask=torch.zeros((2, 15), **i32)), dict(mask=torch.zeros((1, 16), **i32)),
-                dict(mask=torch.zeros((16, 2), **i32).t()), dict(mask=torch.zeros((1, 16), **i32).expand(2, 16)), dict(temperature=z)):
+                dict(mask=torch.zeros((16, 2), **i32).t()), dict(mask=torch.zeros((1, 16), **i32).expand(2, 16)), dict(temperature=z),
+                dict(presence=torch.zeros(2)), dict(mask=torch.zeros((2, 16), dtype=torch.int32))):
         with pytest.raises(ValueError):
             s.adjust(**bad)
     adj, t = s.adjust(), torch.zeros((6, 500), device=DEV)
     for bad in (lambda: s.adjust_logits(t[:5], adj), lambda: s.adjust_logits(t.double(), adj),
                 lambda: s.adjust_logits(t, adj, out=torch.zeros((6, 501), device=DEV)),
-                lambda: s.fuse_adjusted(torch.zeros((500, 6), device=DEV).t(), adj)):
+                lambda: s.fuse_adjusted(torch.zeros((500, 6), device=DEV).t(), adj), lambda: s.adjust_logits(t.cpu(), adj),
+                lambda: s.adjust_logits(t, adj, out=t.cpu()), lambda: s.fuse_adjusted(t, adj, want=("logits",))):
         with pytest.raises(ValueError):
             bad()
     other, _, _ = _session(400, [2, 2])

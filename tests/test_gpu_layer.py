@@ -524,7 +524,9 @@ def test_session_refusals():
                 lambda: s.append(q, k[..., ::2], v, n_tokens=2), lambda: s.attend(q, n_tokens=1),
                 lambda: s.attend(q[:, :1], n_tokens=2, n_layers=1), lambda: s.attend(q, n_tokens=2, want=("pages",)),
                 lambda: s.attend(q, n_tokens=2, want=("scores",), select=(2, 0, 1)),
-                lambda: s.attend(q, n_tokens=2, x_out=q)):
+                lambda: s.attend(q, n_tokens=2, x_out=q), lambda: s.append(q.cpu(), k, v, n_tokens=2),
+                lambda: s.append(None, k, v.cpu(), n_tokens=2), lambda: s.attend(q.cpu(), n_tokens=2),
+                lambda: s.append(q, k, v, n_tokens=2, q_out=q.cpu())):
         with pytest.raises(ValueError):
             bad()
     assert s.lengths() == [40, 20]

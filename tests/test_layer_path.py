@@ -103,6 +103,7 @@ def test_append_takes(layer_host):
     assert b.append() == OK and b.calls("append_rows")[0][:7] == [0, 2, 1, 1, 0, 0, 2 * 32 * 128]
     assert b.append(q_out=Q) == OK                                   # in place
     assert b.append(rope=None) == OK and b.append(rope=(1e4, 0, 1)) == OK and b.append(rope=(1e4, 22, 0)) == OK
+    assert b.append(rows=dict(k=K, v=V, q_row=-5), q_out=None) == OK  # (no q rows: no distance)
     assert b.append(rows=dict(k=K, v=V), q_out=None, n=40) == OK and b.calls("append_rows")[0][3] == 3  # tokens 16 .. 55 and 40 .. 79
     fused = dict(q=Q, k=Q + 4096 * 2, v=Q + 5120 * 2, q_row=6144, k_row=6144, v_row=6144)
     assert b.append(layers=1, rows=fused) == OK
@@ -195,7 +196,8 @@ def test_adjust_refusals(layer_host):
     good = _lib.pced_adjust()
     for call in (run, fuse):
         assert call(None) == INVALID and call(good, None) == INVALID and call(good, logits, None) == INVALID
-        for bad in (dict(n_history=-1), dict(n_bias=-1), dict(history=dev, n_history=3), dict(mask=dev, mask_row=31),
+        for bad in (dict(n_history=-1), dict(n_bias=-1), dict(history=dev, history_off=dev, n_history=2 ** 31 - 1),
+                    dict(n_bias=2 ** 30 + 1), dict(history=dev, n_history=3), dict(mask=dev, mask_row=31),
                     dict(bias_token=dev, bias_value=dev), dict(bias_token=dev, bias_off=dev), dict(mask=dev, mask_row=-32)):
             assert call(_lib.pced_adjust(**bad)) == INVALID, bad
     assert run(good, logits, P(Q + 4000)) == INVALID           # partly itself
