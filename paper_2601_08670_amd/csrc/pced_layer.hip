@@ -198,7 +198,9 @@ __device__ __forceinline__ void turn_slot(const Slot<BF16>& sl, const float2* cs
 // 16 positions and shared by its heads, while the rows' first loads are under way
 // (several slots of a thread at once: a store may not pass a later slot's load). A page
 // that becomes full is summarised by the block that filled it. Bound: HBM for many
-// tokens, the chain of length, rows and stores for one.
+// tokens (64 of 33 sequences, 32/8 heads of 128: 15.8 us for 52 MB, 3.3 TB/s; reads and
+// writes in turn reach 5.1), the chain of length, rows and stores for one (eight layers
+// of 33 sequences 6.8 us, one of five 3.6).
 constexpr int kAppendTasks = 1024;
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
@@ -716,13 +718,15 @@ __device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32
   return a.n_pages - a.first - a.last;
 }
 
-// Bounds and choice in one launch, for at most 64 R pages: one block of W waves per
-// (token group, layer, kv-head), 4 R / W tiles of 16 pages per wave. The codes are on
+// Bounds and choice in one launch, for at most 64 R pages: one block of 8 waves per
+// (token group, layer, kv-head), R / 2 tiles of 16 pages per wave. The codes are on
 // their way while the weights are made; the bounds meet in LDS, from where each
-// wave chooses the pages of a token.
-template <int R, int W>
-__global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
-  constexpr int NT = 4 * R / W, T = kAttendTokens;
+// wave chooses the pages of a token. Bound: latency (lengths, ids, codes, weights and
+// the choice one after the other): 24 new tokens of 17 sequences of up to 8192
+// tokens, 4 kv-heads, 204 blocks, 15.2 us.
+template <int R>
+__global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
+  constexpr int W = 8, NT = 4 * R / W, T = kAttendTokens;
   __shared__ __align__(16) int8_t w[16][256];  // (columns past the tokens' count for nothing)
   __shared__ __align__(16) float bound[T][64 * R + 4];  // (sums, to be scaled)
   __shared__ float scale[64 * R];
@@ -770,7 +774,10 @@ __global__ __launch_bounds__(64 * W) void k_page_pick(AttendArgs a) {
 // The same in two launches for long sequences, whose summaries one work-group would
 // take long to read. Bounds: a block per (token group, layer, kv-head, chunk_pages
 // pages), each wave 32 of every 128 pages at a time; their ids are two rounds ahead and
-// their codes one. Bound: HBM, the summaries are read once.
+// their codes one. Bound: HBM, the summaries are read once, in pieces of 256 bytes: 9
+// sequences of up to 8192 pages, 8 kv-heads, 101 MB in 28 us (3.6 TB/s) where the pages
+// lie scattered, 20 us (5.0) in order. (Blocks of all kv-heads, a page's codes of all of
+// them next to each other: 31 and 26 us.)
 __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
   __shared__ __align__(16) int8_t w[16][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -825,6 +832,8 @@ __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
 // squeeze it into few steps), the bound is searched bit by bit as in pick_pages, with the
 // counts of the waves added up in LDS and two bits per barrier. A row of more than
 // 1024 R candidates (MANY) goes in rounds, whose keys are read again for every pass.
+// Bound: latency, some ten passes between barriers: 11 us for 72 rows of up to 8192
+// pages at R = 8 (15.4 at 16), 6 us for up to 1024 at R = 2 (9.4 at 8, 14.5 at 16).
 constexpr int kBins = 2048, kNear = 512;
 __device__ __forceinline__ float order_value(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
@@ -1030,6 +1039,11 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // the next one in flight on every path).
 // Tokens behind the row's own position get weight 0, and their V counts as 0 (those
 // rows may hold anything).
+// Bound: HBM where items abound (16 layers of 33 sequences, 32 of up to 128 pages, 8
+// kv-heads, PICK: 1.18 GB in 208 us, 5.7 TB/s); start and drain of short streams at one
+// layer (18 us for 74 MB; 256 pages of 9 sequences in 504 work-groups, 29 us for 134 MB);
+// with many tokens the way from the L2, which has most of their pages (24 tokens of 17
+// sequences, 64 pages each, 53 us for 0.8 GB of which HBM gives a sixth).
 template <bool BF16, int NU>
 struct PageRegs {
   static constexpr int NB = BF16 ? 2 : 1;
@@ -1040,7 +1054,7 @@ struct PageRegs {
 
 // PICK: the block chooses its item's pages itself, as k_page_pick does: one new token,
 // at most kPickPages pages, one part. The launch that this saves, and the list's way
-// through memory, cost more than the pages that wait behind the choice: see launch_attend.
+// through memory, cost more than the pages that wait behind the choice: see run_attend.
 template <bool BF16, int NU, bool PICK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU > 6 ? 1 : 2, 4))) void k_attend(AttendArgs a) {
   using Regs = PageRegs<BF16, NU>;
@@ -1387,14 +1401,10 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
   if (items > 0x7FFFFFFFu || groups * a.chunks > 0x7FFFFFFFu) return hipErrorInvalidValue;
   const int pages = a.score_row;
   if (!score || pages <= kPickPages) {
-    // Many work-groups: four tiles per wave, so that more of them are resident (16 of 2 waves
-    // per compute unit); else 8 waves, which read the summaries sooner. 4224 work-groups of
-    // up to 129 pages: see the launch's figures in k_page_pick.
-    const bool many = groups > 4 * (size_t)a.num_cus && a.gt == 1;
-    auto run = [&](auto kernel, int waves) { return go(kernel, dim3((unsigned)groups), dim3(64 * waves), 0, st, t0(tm), t1(tm), a); };
-    if (!score || pages <= 128) return many ? run(k_page_pick<2, 2>, 2) : run(k_page_pick<2, 8>, 8);
-    if (pages <= 256) return many ? run(k_page_pick<4, 4>, 4) : run(k_page_pick<4, 8>, 8);
-    return run(k_page_pick<8, 8>, 8);
+    auto run = [&](auto kernel) { return go(kernel, dim3((unsigned)groups), dim3(512), 0, st, t0(tm), t1(tm), a); };
+    if (!score || pages <= 128) return run(k_page_pick<2>);
+    if (pages <= 256) return run(k_page_pick<4>);
+    return run(k_page_pick<8>);
   }
   const hipError_t e = go(k_page_score, dim3((unsigned)(groups * a.chunks)), dim3(256), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;

@@ -44,7 +44,9 @@ AttendPlan attend_plan(const pced_ctx* c, const AttendArgs& a, int max_pages, bo
   p.layers = layers;
   const size_t items = (size_t)groups * a.gt * layers * a.n_kv_heads;
   const int cnt = std::min(max_pages, a.n_pages);
-  // two work-groups per compute unit, as far as a part keeps two batches of pages per wave
+  // two work-groups per compute unit, as far as a part keeps a batch of pages per wave (9 sequences, 256 pages each,
+  // 8 kv-heads, attention and merge in us at 1 / 2 / 4 / 8 per unit: 33 / 34 / 34 / 35; 3 sequences, 128 pages: 9.9 /
+  // 10.6 / 10.7 / 11; rounded down, one per unit would leave half of them idle at some counts)
   const size_t want = std::max<size_t>(1, 2 * (size_t)c->num_cus / items);
   p.part_pages = std::min(std::max<int>({min_part, ceil_div(ceil_div(cnt, (long)want), 8) * 8, 8}), kAttendPart);
   p.parts = ceil_div(cnt, p.part_pages);
@@ -339,7 +341,6 @@ pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   a.maxpps = cfg.max_pages_per_seq;
   a.sum_row = summary_row(cfg.head_dim);
   a.bf16 = c->bf16;
-  a.num_cus = c->num_cus;
   a.n_pages = sel ? sel->n_pages : max_pages;
   a.first = sel ? sel->n_first : 0;
   a.last = sel ? sel->n_last : 1;
