@@ -2332,8 +2332,8 @@ __device__ __forceinline__ float adjust1(float x, bool seen, float rep, float sh
 // (at any 4-byte address), four rows at a time, the first of them on their way while
 // the lists are read. Where the mask closes all four nothing is read. Bound: HBM,
 // every logit read (if it matters) and written once: 16 queries of 17 rows of 50257
-// tokens, one in a hundred open, 17 us for 110 MB (6.4 TB/s; some of it stays in the
-// caches); 9 rows of 128256, all open, 5.2 us for 9.2 MB (the way through the lists).
+// tokens, one in a hundred open, 16.5 us for 18 MB read and 55 written (4.4 TB/s); 9
+// rows of 128256, all open, 5.3 us for 9.2 MB (the way through the lists).
 __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
   constexpr int SW = 1024, U = 4;
   __shared__ AdjustLds<SW> lds;
