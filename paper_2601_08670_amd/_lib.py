@@ -229,17 +229,22 @@ def _ptr(t) -> Optional[int]:
 _torch_c = None
 
 
-def _stream(stream) -> int:
-    """The handle of `stream`, or of the current device's current stream (asked for directly: the
-    Stream object around it costs a short call more than its launch)."""
+def current_device() -> int:
     global _torch_c
-    if stream is not None:
-        return stream.cuda_stream
     if _torch_c is None:
         import torch
         torch.cuda.current_stream()  # (initialises the device)
         _torch_c = torch._C
-    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
+    return _torch_c._cuda_getDevice()
+
+
+def _stream(stream) -> int:
+    """The handle of `stream`, or of the current device's current stream (asked for directly: the
+    Stream object around it costs a short call more than its launch)."""
+    if stream is not None:
+        return stream.cuda_stream
+    device = current_device()
+    return _torch_c._cuda_getCurrentRawStream(device)
 
 
 def _i32_array(values):

@@ -194,6 +194,11 @@ class PcedSession:
             raise ValueError(f"{name}: {t.dtype} in a session of {self.dtype}")
         return self._here(t, name)
 
+    def _on_device(self):
+        """The calls go to the current device's stream, which has to be the session's."""
+        if _lib.current_device() != self._device_index:
+            raise ValueError(f"the session is on {self.k_pool.device}, which is not the current device")
+
     def _here(self, t, name):
         if t.get_device() != self._device_index:
             raise ValueError(f"{name}: on {t.device}, the session is on {self.k_pool.device}")
@@ -228,6 +233,7 @@ class PcedSession:
         [S * n_tokens][n_layers][heads][D], which may be apart (views of one projection's
         output); q None: K / V only. ``rope``: (theta, rot_dim, halves) or None. Returns the
         rotated q rows (``q_out`` or a new tensor)."""
+        self._on_device()
         g = self.geom
         if n_layers is None:
             n_layers = g["n_layers"] - layer
@@ -256,12 +262,14 @@ class PcedSession:
         self.ctx.pced_bind_summary(self.summary)
 
     def summarize(self):
+        self._on_device()
         self.ctx.pced_summarize()
 
     def attend(self, q, n_tokens=1, select=None, layer=0, n_layers=None, want=(), x_out=None):
         """pced_attend: q as append returned it; ``select``: (n_pages, n_first, n_last) or None
         for all pages. Returns {"x": [S * n_tokens][n_layers][Hq * D]}, and with "pages" in
         ``want`` the pages [S * n_tokens][n_layers][Hkv][n_pages]."""
+        self._on_device()
         torch, g = _torch(), self.geom
         if n_layers is None:
             n_layers = g["n_layers"] - layer
@@ -303,6 +311,7 @@ class PcedSession:
 
     def adjust_logits(self, logits, adjust, out=None):
         """pced_adjust_logits of [S][V] logits; ``out`` may be logits itself."""
+        self._on_device()
         self._logits(logits, "logits")
         out = _torch().empty_like(logits) if out is None else self._logits(out, "out")
         self.ctx.pced_adjust_logits(logits, self._adjust(adjust), out)
@@ -310,6 +319,7 @@ class PcedSession:
 
     def fuse_adjusted(self, logits, adjust, refresh_beta=False, want=("winner", "top1", "top2", "beta_used")):
         """pced_fuse_adjusted: the tokens chosen over adjusted logits, and the wanted outputs."""
+        self._on_device()
         like = _torch().empty_like
         self._logits(logits, "logits")
         out = {"tokens": like(self._out_like["winner"])}

@@ -243,3 +243,16 @@ def test_structs_match_the_header(tmp_path, struct, names):
                     "-o", exe], check=True)
     got = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()]
     assert got == [ctypes.sizeof(struct)] + [getattr(struct, n).offset for n in names]
+
+
+def test_calls_from_another_device_are_refused(monkeypatch):
+    import torch
+
+    from paper_2601_08670_amd.session import PcedSession
+    s = object.__new__(PcedSession)
+    s._device_index, s.k_pool = 0, torch.empty(0)
+    monkeypatch.setattr(_lib, "current_device", lambda: 1)
+    for call in (lambda: s.append(None, None, None), lambda: s.attend(None), lambda: s.summarize(),
+                 lambda: s.adjust_logits(None, None), lambda: s.fuse_adjusted(None, None)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
