@@ -381,6 +381,7 @@ struct AttendArgs {
   int chunks, chunk_pages;  // pages per work-group of the bounds (whole 128s), work-groups that cover them
   int parts, part_pages;    // parts of an item's pages, and pages per part
   int launch_seqs;          // sequences of the launch's groups (set by launch_attend)
+  int num_cus;
   float scale_log2;         // log2(e) / sqrt(D)
 };
 

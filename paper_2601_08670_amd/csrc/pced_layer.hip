@@ -567,27 +567,31 @@ __device__ __forceinline__ void query_weights(const AttendArgs& a, const void* q
 
 // 16 pages' codes as the rows of a product (lane: page lane % 16, bytes 16 (lane / 16)
 // of each 64), and the pages' scales.
+template <int K>
 struct CodeTile {
-  i32x4 c[4];
+  i32x4 c[K];
   float scale;
 };
-__device__ __forceinline__ void load_codes(const AttendArgs& a, size_t base, int phys, int quad, CodeTile& t) {
+template <int K>
+__device__ __forceinline__ void load_codes(const AttendArgs& a, size_t base, int phys, int quad, CodeTile<K>& t) {
   const int8_t* code = a.codes + (base + phys) * a.sum_row + 16 * quad;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) t.c[k] = *(const i32x4*)(code + min(64 * k, a.sum_row - 64));
+  for (int k = 0; k < K; ++k) t.c[k] = *(const i32x4*)(code + min(64 * k, a.sum_row - 64));
   t.scale = a.scale[base + phys];
 }
 // the sums of pages 4 (lane / 16) .. + 3 of the tile for the token of column lane % 16
-__device__ __forceinline__ float4 tile_sums(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4]) {
+template <int K>
+__device__ __forceinline__ float4 tile_sums(const AttendArgs& a, const CodeTile<K>& t, const i32x4 (&w)[K]) {
   i32x4 c = {0, 0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < K; ++k)
     if (64 * k < a.sum_row) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.c[k], w[k], c, 0, 0, 0);
   return make_float4((float)c[0], (float)c[1], (float)c[2], (float)c[3]);
 }
 // the pages' bounds: sums times scales
-__device__ __forceinline__ float4 tile_bounds(const AttendArgs& a, const CodeTile& t, const i32x4 (&w)[4], int quad) {
-  const float4 c = tile_sums(a, t, w);
+template <int K>
+__device__ __forceinline__ float4 tile_bounds(const AttendArgs& a, const CodeTile<K>& t, const i32x4 (&w)[K], int quad) {
+  const float4 c = tile_sums<K>(a, t, w);
   return make_float4(c.x * __shfl(t.scale, 4 * quad), c.y * __shfl(t.scale, 4 * quad + 1), c.z * __shfl(t.scale, 4 * quad + 2),
                      c.w * __shfl(t.scale, 4 * quad + 3));
 }
@@ -737,7 +741,7 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
     const int p1 = it.pages - a.last;  // pages [first, p1) are chosen between
     const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
     const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
-    CodeTile t[NT];
+    CodeTile<4> t[NT];
     int phys[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) phys[i] = pt[min(16 * (wave + W * i) + col, p1 - 1)];
@@ -752,7 +756,7 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
       if (16 * (wave + W * i) < p1) {
-        const float4 o = tile_sums(a, t[i], b);
+        const float4 o = tile_sums<4>(a, t[i], b);
         if (col < it.nt) *(float4*)&bound[col][16 * (wave + W * i) + 4 * quad] = o;
         if (quad == 0) scale[16 * (wave + W * i) + col] = t[i].scale;
       }
@@ -778,6 +782,7 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
 // sequences of up to 8192 pages, 8 kv-heads, 101 MB in 28 us (3.6 TB/s) where the pages
 // lie scattered, 20 us (5.0) in order. (Blocks of all kv-heads, a page's codes of all of
 // them next to each other: 31 and 26 us.)
+template <int K>
 __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
   __shared__ __align__(16) int8_t w[16][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -791,7 +796,7 @@ __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
     int a, b;
   };
   struct Tiles {
-    CodeTile a, b;
+    CodeTile<K> a, b;
   };
   const int q0 = p0 + 32 * wave;  // the wave's first pages
   // (past the range its last page)
@@ -805,12 +810,12 @@ __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
   load(ia, ta);
   for (int j = wave; j < it.nt; j += 4) query_weights(a, group_q(a, it, j), lane, w[j]);
   __syncthreads();
-  i32x4 b[4];
+  i32x4 b[K];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
+  for (int k = 0; k < K; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
   float* out = a.scores + (size_t)group_slot(a, it, min(col, it.nt - 1)) * a.score_row + 4 * quad;
   auto put = [&](int q, const Tiles& t) __attribute__((always_inline)) {
-    const float4 x = tile_bounds(a, t.a, b, quad), y = tile_bounds(a, t.b, b, quad);
+    const float4 x = tile_bounds<K>(a, t.a, b, quad), y = tile_bounds<K>(a, t.b, b, quad);
     if (col < it.nt && q < p1) *(float4*)(out + q) = x;  // (rows hold whole tiles)
     if (col < it.nt && q + 16 < p1) *(float4*)(out + q + 16) = y;
   };
@@ -824,45 +829,50 @@ __global__ __launch_bounds__(256) void k_page_score(AttendArgs a) {
   }
 }
 
-// The choice from those bounds: a block of 16 waves per item, wave v's keys being the
+// The choice from those bounds: a block of W waves per item, wave v's keys being the
 // v-th run of 64 R candidates. The candidates are counted in kBins equal steps of
 // their range (which spreads them, so that the LDS atomics rarely meet), the step that
 // holds the want-th highest bound is found from the counts, and its candidates, a few,
 // are ranked one by one. Where they are more than kNear (bounds far from the rest
 // squeeze it into few steps), the bound is searched bit by bit as in pick_pages, with the
 // counts of the waves added up in LDS and two bits per barrier. A row of more than
-// 1024 R candidates (MANY) goes in rounds, whose keys are read again for every pass.
-// Bound: latency, some ten passes between barriers: 11 us for 72 rows of up to 8192
-// pages at R = 8 (15.4 at 16), 6 us for up to 1024 at R = 2 (9.4 at 8, 14.5 at 16).
+// 64 W R candidates (MANY) goes in rounds, whose keys are read again for every pass.
+// Bound: latency for few rows (some ten passes between barriers), for many the passes'
+// instructions, most of which are a wave's and not a key's. us with 16 / 8 / 4 waves:
+// rows of up to 8192 pages, 72 of them 11.2 / 14.2 / 22, 576 20.3 / 16.2; of up to 3750,
+// 72 7.5 / 8.6 / 12.8, 216 7.8 / 8.8 / 13.0, 576 13.8 / 10.0 / 14.0, 3264 74 / 37 / 33;
+// of up to 2000, 72 6.1 / 6.1 / 7.8, 576 9.6 / 7.8 / 9.1. More candidates per thread
+// than the pages need: 72 rows of 8192 15.4 at R = 16 (W = 16).
 constexpr int kBins = 2048, kNear = 512;
 __device__ __forceinline__ float order_value(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
-template <int R, bool MANY>
-__global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
+template <int W, int R, bool MANY>
+__global__ __launch_bounds__(64 * W) void k_page_select(AttendArgs a) {
+  constexpr int NT = 64 * W, C = kBins / NT;
   __shared__ int count[52], hist[kBins], near_page[kNear];
-  __shared__ uint32_t near_key[kNear], wmin[16], wmax[16], s_key;
-  __shared__ int wsum[2][16], s_bin, s_need, s_near, s_page;
+  __shared__ uint32_t near_key[kNear], wmin[W], wmax[W], s_key;
+  __shared__ int wsum[2][W], s_bin, s_need, s_near, s_page;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t item = blockIdx.x;
   const AttendItem it = attend_item(a, item);
   if (it.pages == 0 || (it.pages <= a.n_pages && !a.pages_out)) return;
   int32_t* list = const_cast<int32_t*>(page_list(a, it, item));
-  const int want = fixed_pages(a, it.pages, list, tid, 1024);
+  const int want = fixed_pages(a, it.pages, list, tid, NT);
   if (want == 0) return;
   list += a.first;
   const int lo = a.first, hi = it.pages - a.last;
-  const int rounds = MANY ? (hi - lo + 1024 * R - 1) / (1024 * R) : 1;
+  const int rounds = MANY ? (hi - lo + NT * R - 1) / (NT * R) : 1;
   const float* sc = a.scores + (size_t)item * a.score_row;
   uint32_t key[R];
   auto load = [&](int round) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const int p = lo + (round * 16 + wave) * 64 * R + 64 * i + lane;
+      const int p = lo + (round * W + wave) * 64 * R + 64 * i + lane;
       key[i] = p < hi ? order_key(sc[min(p, hi - 1)]) : 0u;
     }
   };
-  for (int i = tid; i < kBins; i += 1024) hist[i] = 0;
+  for (int i = tid; i < kBins; i += NT) hist[i] = 0;
   if (tid < 52) count[tid] = 0;
   load(0);
   // the range of the bounds
@@ -883,7 +893,7 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
   if (lane == 0) { wmin[wave] = kmin; wmax[wave] = kmax; }
   __syncthreads();
 #pragma unroll
-  for (int v = 0; v < 16; ++v) { kmin = min(kmin, wmin[v]); kmax = max(kmax, wmax[v]); }
+  for (int v = 0; v < W; ++v) { kmin = min(kmin, wmin[v]); kmax = max(kmax, wmax[v]); }
   const float low = order_value(kmin), span = order_value(kmax) - low;
   const float inv = span > 0.f ? (float)(kBins - 1) / span : 0.f;
   auto bin_of = [&](uint32_t k) { return min((int)((order_value(k) - low) * inv), kBins - 1); };  // (grows with k)
@@ -894,21 +904,26 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
       if (key[i]) atomicAdd(&hist[bin_of(key[i])], 1);
   }
   __syncthreads();
-  {  // thread i: bins kBins - 1 - 2i and the one below it
-    const int hi2 = hist[kBins - 1 - 2 * tid], lo2 = hist[kBins - 2 - 2 * tid];
-    int sum = hi2 + lo2, run = sum;
+  {  // thread i: C bins from kBins - 1 - C i down
+    int h[C], sum = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) sum += h[c] = hist[kBins - 1 - C * tid - c];
+    int run = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(run, o); if (lane >= o) run += x; }
     if (lane == 63) wsum[0][wave] = run;
     __syncthreads();
 #pragma unroll
-    for (int v = 0; v < 16; ++v) if (v < wave) run += wsum[0][v];
-    const int before = run - sum;
-    if (before < want && want <= before + sum) {
-      const bool first = want <= before + hi2;
-      s_bin = kBins - 1 - 2 * tid - (first ? 0 : 1);
-      s_need = want - before - (first ? 0 : hi2);
-      s_near = first ? hi2 : lo2;
+    for (int v = 0; v < W; ++v) if (v < wave) run += wsum[0][v];
+    int above = run - sum;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (above < want && want <= above + h[c]) {
+        s_bin = kBins - 1 - C * tid - c;
+        s_need = want - above;
+        s_near = h[c];
+      }
+      above += h[c];
     }
   }
   __syncthreads();
@@ -923,14 +938,14 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
         if (key[i] && bin_of(key[i]) == bin) {
           const int at = atomicAdd(&count[0], 1);
           near_key[at] = key[i];
-          near_page[at] = lo + (r * 16 + wave) * 64 * R + 64 * i + lane;
+          near_page[at] = lo + (r * W + wave) * 64 * R + 64 * i + lane;
         }
     }
     __syncthreads();
     const int n = s_near;
-    if (tid < n) {
-      const uint32_t k = near_key[tid];
-      const int p = near_page[tid];
+    for (int i = tid; i < n; i += NT) {
+      const uint32_t k = near_key[i];
+      const int p = near_page[i];
       int rank = 0;
       for (int j = 0; j < n; ++j) rank += near_key[j] > k || (near_key[j] == k && near_page[j] < p);
       if (rank == need - 1) { s_key = k; s_page = p; }
@@ -972,7 +987,7 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
     __syncthreads();
     ties = want - count[51];
   }
-  auto page_at = [&](int r, int i) { return lo + (r * 16 + wave) * 64 * R + 64 * i + lane; };
+  auto page_at = [&](int r, int i) { return lo + (r * W + wave) * 64 * R + 64 * i + lane; };
   auto tie = [&](int r, int i) { return key[i] == t && page_at(r, i) <= last_tie; };
   const uint64_t below = ((uint64_t)1 << lane) - 1;
   int base = 0, eq = 0;  // places taken and equal keys met before the round
@@ -985,7 +1000,7 @@ __global__ __launch_bounds__(1024) void k_page_select(AttendArgs a) {
     __syncthreads();
     int gb = 0, eb = 0, ga = 0, ea = 0;  // before this wave, and of all
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
+    for (int v = 0; v < W; ++v) {
       if (v < wave) { gb += wsum[0][v]; eb += wsum[1][v]; }
       ga += wsum[0][v];
       ea += wsum[1][v];
@@ -1121,7 +1136,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
     } else {
       const int p1 = it.pages - a.last;
       const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
-      CodeTile t[R];
+      CodeTile<4> t[R];
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (16 * (wave + 4 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
@@ -1137,7 +1152,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (16 * (wave + 4 * i) < p1) {
-          const float4 o = tile_sums(a, t[i], w);
+          const float4 o = tile_sums<4>(a, t[i], w);
           if (col == 0) *(float4*)&s_bound[16 * (wave + 4 * i) + 4 * quad] = o;
           if (quad == 0) s_scale[16 * (wave + 4 * i) + col] = t[i].scale;
         }
@@ -1406,13 +1421,24 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
     if (pages <= 256) return run(k_page_pick<4>);
     return run(k_page_pick<8>);
   }
-  const hipError_t e = go(k_page_score, dim3((unsigned)(groups * a.chunks)), dim3(256), 0, st, t0(tm), nullptr, a);
+  const dim3 sgrid((unsigned)(groups * a.chunks));
+  const hipError_t e = a.sum_row <= 128 ? go(k_page_score<2>, sgrid, dim3(256), 0, st, t0(tm), nullptr, a)
+                                        : go(k_page_score<4>, sgrid, dim3(256), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)items);
-  if (pages <= 2048) return go(k_page_select<2, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
-  if (pages <= 8192) return go(k_page_select<8, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
-  if (pages <= 16384) return go(k_page_select<16, false>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
-  return go(k_page_select<16, true>, grid, dim3(1024), 0, st, nullptr, t1(tm), a);
+  auto run = [&](auto kernel, int waves) { return go(kernel, grid, dim3(64 * waves), 0, st, nullptr, t1(tm), a); };
+  // Few rows: 16 waves each, the sooner done; more than one per compute unit: 8, whose
+  // passes cost half as much (see k_page_select).
+  if (items > (size_t)a.num_cus && pages <= 8192) {
+    if (pages <= 2048) return run(k_page_select<8, 4, false>, 8);
+    if (pages <= 4096) return run(k_page_select<8, 8, false>, 8);
+    return run(k_page_select<8, 16, false>, 8);
+  }
+  if (pages <= 2048) return run(k_page_select<16, 2, false>, 16);
+  if (pages <= 4096) return run(k_page_select<16, 4, false>, 16);
+  if (pages <= 8192) return run(k_page_select<16, 8, false>, 16);
+  if (pages <= 16384) return run(k_page_select<16, 16, false>, 16);
+  return run(k_page_select<16, 16, true>, 16);
 }
 
 hipError_t launch_attend(const AttendArgs& a0, bool pick, hipStream_t st, const Timing* tm, const Timing* tm_merge) {

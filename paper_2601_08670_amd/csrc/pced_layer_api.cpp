@@ -341,6 +341,7 @@ pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   a.maxpps = cfg.max_pages_per_seq;
   a.sum_row = summary_row(cfg.head_dim);
   a.bf16 = c->bf16;
+  a.num_cus = c->num_cus;
   a.n_pages = sel ? sel->n_pages : max_pages;
   a.first = sel ? sel->n_first : 0;
   a.last = sel ? sel->n_last : 1;
