@@ -728,7 +728,7 @@ __device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32
 // wave chooses the pages of a token. Bound: latency (lengths, ids, codes, weights and
 // the choice one after the other): 24 new tokens of 17 sequences of up to 8192
 // tokens, 4 kv-heads, 204 blocks, 15.2 us.
-template <int R>
+template <int R, int K>
 __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
   constexpr int W = 8, NT = 4 * R / W, T = kAttendTokens;
   __shared__ __align__(16) int8_t w[16][256];  // (columns past the tokens' count for nothing)
@@ -741,7 +741,7 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
     const int p1 = it.pages - a.last;  // pages [first, p1) are chosen between
     const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
     const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
-    CodeTile<4> t[NT];
+    CodeTile<K> t[NT];
     int phys[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) phys[i] = pt[min(16 * (wave + W * i) + col, p1 - 1)];
@@ -750,13 +750,13 @@ __global__ __launch_bounds__(512) void k_page_pick(AttendArgs a) {
       if (16 * (wave + W * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
     for (int j = wave; j < it.nt; j += W) query_weights(a, group_q(a, it, j), lane, w[j]);
     __syncthreads();
-    i32x4 b[4];
+    i32x4 b[K];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
+    for (int k = 0; k < K; ++k) b[k] = *(const i32x4*)&w[col][64 * k + 16 * quad];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
       if (16 * (wave + W * i) < p1) {
-        const float4 o = tile_sums<4>(a, t[i], b);
+        const float4 o = tile_sums<K>(a, t[i], b);
         if (col < it.nt) *(float4*)&bound[col][16 * (wave + W * i) + 4 * quad] = o;
         if (quad == 0) scale[16 * (wave + W * i) + col] = t[i].scale;
       }
@@ -1075,6 +1075,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   using Regs = PageRegs<BF16, NU>;
   constexpr int NJ = BF16 ? 2 * NU : NU;  // 16-dim output blocks
   constexpr int NB = Regs::NB;            // pages per batch
+  // fp32: row r of output block 4 g + c is dim 64 g + 4 r + c, so that a lane's V of four blocks is one 16-byte load
+  // (the blocks past the last four: dim 16 j + r)
+  constexpr int NV = BF16 ? 0 : NJ / 4 * 4;
   constexpr int DP = 16 * NJ + 4;
   __shared__ __align__(16) float sacc[4][kMaxGroup][DP];
   __shared__ float sm[4][kMaxGroup], sl[4][kMaxGroup];
@@ -1123,7 +1126,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   }
   if constexpr (PICK) {
     // (the page ids do not wait for the length: pages that the sequence does not have get some id)
-    constexpr int R = kPickPages / 64;
+    constexpr int R = kPickPages / 64, KC = BF16 ? NU : (NU + 1) / 2;  // (sum_row / 64)
     int phys[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -1136,7 +1139,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
     } else {
       const int p1 = it.pages - a.last;
       const size_t base = ((size_t)(a.layer + it.l) * a.n_kv_heads + it.h) * a.max_pages;
-      CodeTile<4> t[R];
+      CodeTile<KC> t[R];
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (16 * (wave + 4 * i) < p1) load_codes(a, base, phys[i], quad, t[i]);
@@ -1146,13 +1149,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
       if (wave == 0)
         query_weights(a, (const char*)a.q + (qrow - (size_t)min(col, G - 1) * D) * (BF16 ? 2 : 4), lane, s_w);
       __syncthreads();
-      i32x4 w[4];
+      i32x4 w[KC];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = *(const i32x4*)&s_w[64 * k + 16 * quad];  // (every column the token's)
+      for (int k = 0; k < KC; ++k) w[k] = *(const i32x4*)&s_w[64 * k + 16 * quad];  // (every column the token's)
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (16 * (wave + 4 * i) < p1) {
-          const float4 o = tile_sums<4>(a, t[i], w);
+          const float4 o = tile_sums<KC>(a, t[i], w);
           if (col == 0) *(float4*)&s_bound[16 * (wave + 4 * i) + 4 * quad] = o;
           if (quad == 0) s_scale[16 * (wave + 4 * i) + col] = t[i].scale;
         }
@@ -1193,9 +1196,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
 #pragma unroll
         for (int i = 0; i < NU; ++i) r.k[b][i] = *(const u32x4*)(kp + min(16 * i + 4 * quad, D - 4));
 #pragma unroll
-        for (int i = 0; i < NU; ++i)
+        for (int e = 0; e < 4; ++e) {
+          const float* row = vp + (4 * quad + e) * D;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) r.vf[i][e] = vp[(size_t)(4 * quad + e) * D + min(16 * i + col, D - 1)];
+          for (int i = 0; i < NV; i += 4) {
+            const f32x4 x = *(const f32x4*)(row + min(16 * i + 4 * col, D - 4));
+#pragma unroll
+            for (int c = 0; c < 4; ++c) r.vf[i + c][e] = x[c];
+          }
+#pragma unroll
+          for (int i = NV; i < NU; ++i) r.vf[i][e] = row[min(16 * i + col, D - 1)];
+        }
       }
     }
   };
@@ -1316,7 +1327,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   lsum += __shfl_xor(lsum, 32);
   if (col < G) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) *(f32x4*)&sacc[wave][col][16 * j + 4 * quad] = acc[j];
+    for (int j = 0; j < NV; j += 4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *(f32x4*)&sacc[wave][col][16 * (j + quad) + 4 * e] = f32x4{acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]};
+#pragma unroll
+    for (int j = NV; j < NJ; ++j) *(f32x4*)&sacc[wave][col][16 * j + 4 * quad] = acc[j];
     if (quad == 0) { sm[wave][col] = m; sl[wave][col] = lsum; }
   }
   __syncthreads();
@@ -1416,10 +1432,12 @@ hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, c
   if (items > 0x7FFFFFFFu || groups * a.chunks > 0x7FFFFFFFu) return hipErrorInvalidValue;
   const int pages = a.score_row;
   if (!score || pages <= kPickPages) {
-    auto run = [&](auto kernel) { return go(kernel, dim3((unsigned)groups), dim3(512), 0, st, t0(tm), t1(tm), a); };
-    if (!score || pages <= 128) return run(k_page_pick<2>);
-    if (pages <= 256) return run(k_page_pick<4>);
-    return run(k_page_pick<8>);
+    auto run = [&](auto two, auto four) {  // (by the 64-byte pieces of a page's codes)
+      return go(a.sum_row <= 128 ? two : four, dim3((unsigned)groups), dim3(512), 0, st, t0(tm), t1(tm), a);
+    };
+    if (!score || pages <= 128) return run(k_page_pick<2, 2>, k_page_pick<2, 4>);
+    if (pages <= 256) return run(k_page_pick<4, 2>, k_page_pick<4, 4>);
+    return run(k_page_pick<8, 2>, k_page_pick<8, 4>);
   }
   const dim3 sgrid((unsigned)(groups * a.chunks));
   const hipError_t e = a.sum_row <= 128 ? go(k_page_score<2>, sgrid, dim3(256), 0, st, t0(tm), nullptr, a)
