@@ -722,9 +722,9 @@ __device__ __forceinline__ int fixed_pages(const AttendArgs& a, int pages, int32
   return a.n_pages - a.first - a.last;
 }
 
-// Bounds and choice in one launch, for at most 64 R pages: one block of 8 waves per
-// (token group, layer, kv-head), R / 2 tiles of 16 pages per wave. The codes are on
-// their way while the weights are made; the bounds meet in LDS, from where each
+// Bounds and choice in one launch, for at most 64 R pages (of up to 64 K bytes of codes):
+// one block of 8 waves per (token group, layer, kv-head), R / 2 tiles of 16 pages per
+// wave. The codes are on their way while the weights are made; the bounds meet in LDS, from where each
 // wave chooses the pages of a token. Bound: latency (lengths, ids, codes, weights and
 // the choice one after the other): 24 new tokens of 17 sequences of up to 8192
 // tokens, 4 kv-heads, 204 blocks, 15.2 us.
