@@ -210,7 +210,8 @@ class PcedSession:
         shape = (self.S * n_tokens, n_layers, heads, d)
         if t.shape != shape:
             raise ValueError(f"{name}: {tuple(t.shape)}, not {shape}")
-        self._storage(t, name)
+        if t.dtype not in self._dtypes or t.get_device() != self._device_index:
+            self._storage(t, name)  # (names the fault)
         if t.is_contiguous():
             return n_layers * heads * d
         st = t.stride()
@@ -280,7 +281,7 @@ class PcedSession:
         if self._row_stride(q, "q", n_tokens, n_layers, g["n_q_heads"]) != n_layers * width:
             raise ValueError("q: rows must follow each other")
         if x_out is None:
-            x_out = torch.empty((rows, n_layers, width), dtype=q.dtype, device=q.device)
+            x_out = q.new_empty((rows, n_layers, width))
         elif self._storage(x_out, "x_out").shape != (rows, n_layers, width) or not x_out.is_contiguous():
             raise ValueError("x_out: [S * n_tokens][n_layers][Hq * D], contiguous")
         out, sel, pages = {"x": x_out}, None, None
