@@ -525,7 +525,7 @@ pced_status pced_summarize(pced_ctx* ctx, hipStream_t stream);
  * on sum_g q_g . k for the page's keys. It is computed exactly, so equal inputs give
  * equal pages; of equal measures the lower page comes first. */
 typedef struct pced_select {
-  int32_t n_pages;   /* >= n_first + n_last */
+  int32_t n_pages;   /* n_first + n_last .. 2^30 */
   int32_t n_first;   /* >= 0                */
   int32_t n_last;    /* >= 1                */
 } pced_select;

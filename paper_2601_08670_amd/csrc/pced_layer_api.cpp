@@ -302,6 +302,8 @@ pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   if (sel && (sel->n_first < 0 || sel->n_last < 1 || (long)sel->n_first + sel->n_last > sel->n_pages))
     return fail(PCED_ERR_INVALID_ARG, "n_first %d >= 0, n_last %d >= 1, their sum at most n_pages %d", sel->n_first,
                 sel->n_last, sel->n_pages);
+  if (sel && sel->n_pages > 1 << 30)  // (places in a list are 32-bit)
+    return fail(PCED_ERR_INVALID_ARG, "n_pages %d > 2^30", sel->n_pages);
   const size_t bytes = (size_t)c->S * n_tokens * n_layers * cfg.hidden * esize_of(cfg);
   if (ranges_meet(q, bytes, x_out, bytes)) return fail(PCED_ERR_INVALID_ARG, "q and x_out overlap");
   for (int l = layer; l < layer + n_layers; ++l)

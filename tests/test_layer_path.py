@@ -114,7 +114,8 @@ def test_append_takes(layer_host):
     (dict(n=0), INVALID), (dict(layer=2), INVALID), (dict(layers=3), INVALID), (dict(q=None), INVALID), (dict(x=None), INVALID),
     (dict(q=Q + 8), INVALID), (dict(x=X + 2), INVALID), (dict(sel=None, pages=K), INVALID), (dict(sel=(4, -1, 1)), INVALID),
     (dict(sel=(4, 0, 0)), INVALID), (dict(sel=(4, 2, 3)), INVALID), (dict(sel=(0, 0, 1)), INVALID),
-    (dict(sel=(-5, 0, 1)), INVALID), (dict(sel=(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1)), INVALID), (dict(x=Q), INVALID),
+    (dict(sel=(2 ** 30 + 1, 0, 1)), INVALID), (dict(sel=(-5, 0, 1)), INVALID),
+    (dict(sel=(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1)), INVALID), (dict(x=Q), INVALID),
     (dict(x=Q + 1024), INVALID), (dict(n=2), STATE), (dict(sel=(2, 0, 1)), STATE), (dict(n=1000), CAPACITY),
 ])
 def test_attend_refusals(layer_host, kw, status):
