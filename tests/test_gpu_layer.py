@@ -339,6 +339,30 @@ def test_long_choices_among_crowded_bounds(kind):
         assert out["pages"][0, 0, 0].tolist() == pages
 
 
+@pytest.mark.parametrize("n", [12000, 40000, 70000])
+@pytest.mark.parametrize("kind", ["random", "equal"])
+def test_long_choices_of_many_rows(n, kind):
+    """Rows beyond the compute units (all layers together) and within them (layer by layer) choose the same pages."""
+    m = Model([n, 20], 1, "f32", (64, 64, 4), layers=3, seed=32)
+    if kind == "equal":
+        m.k[0][1:] = 0.5
+        m.load()
+    m.sess.bind_summary()
+    m.sess.summarize()
+    q, kn, vn = m.rows(1)
+    if kind == "equal":
+        q = q.abs()
+    m.sess.append(None, kn, vn)
+    for sel in ((200, 1, 1), (7, 0, 2)):
+        a = m.sess.attend(q, select=sel, want=("pages",))["pages"]
+        for l in range(3):
+            b = m.sess.attend(q[:, l:l + 1].contiguous(), select=sel, layer=l, n_layers=1, want=("pages",))["pages"]
+            assert torch.equal(b[:, 0], a[:, l])
+            for h in (0, 63):
+                keys = np.concatenate([_f64(m.k[0][l, :, h]), _f64(kn[0, l, h:h + 1])])
+                assert a[0, l, h].tolist() == L.chosen_pages(_f64(q[0, l, h:h + 1]), keys, *sel)
+
+
 def test_attend_sharp_and_equal_scores():
     """Scores far apart (one token takes it all), and pages that measure the same: the lower ones are chosen."""
     m = Model([400, 333], 1, "bf16", (8, 2, 64), seed=8)
