@@ -1024,6 +1024,11 @@ __global__ __launch_bounds__(64 * W) void k_page_select(AttendArgs a) {
 
 // ------------------------------------------------ attention over chosen pages
 
+// The softmax's first reference: the lowest finite number, so that scores of -inf weigh
+// 2^(-inf - m) = 0 wherever they come first (a reference of -inf would make that NaN), and
+// every higher score still moves it. A row of nothing but -inf ends as 0 / 0, NaN.
+constexpr float kLowest = -3.402823466e38f;
+
 // Four output dims of a q-head in the storage type
 template <bool BF16>
 __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& it, int g, int d, int D, f32x4 o) {
@@ -1213,15 +1218,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   f32x4 acc[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = kNegInf, lsum = 0.f;
+  float m = kLowest, lsum = 0.f;
   auto work = [&](int u, int k0, Regs& r) __attribute__((always_inline)) {
     f32x4 c[NB];
-    int lim[NB];  // tokens of the page that count (a batch's slots past the part's end: none)
     float top = kNegInf;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int page = __builtin_amdgcn_readlane(my_page, u + b);
-      lim[b] = k0 + b < cnt ? min(it.pos + 1 - kPage * page, kPage) : 0;
+      // tokens of the page that count (a batch's slots past the part's end: none)
+      const int lim = k0 + b < cnt ? min(it.pos + 1 - kPage * page, kPage) : 0;
       c[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < NU; ++i) {
@@ -1238,10 +1243,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[b][e] *= a.scale_log2;
-      if (lim[b] < kPage) {  // uniform
+      if (lim < kPage) {  // uniform
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (4 * quad + e < lim[b]) continue;
+          if (4 * quad + e < lim) continue;
           c[b][e] = kNegInf;
           if constexpr (BF16) {
             const uint32_t keep = ~(0xFFFFu << (16 * (e & 1)));
@@ -1264,20 +1269,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[j] *= alpha;
     }
-    // a column whose scores so far are all -inf keeps the reference -inf: its weights, 2^(-inf + inf), are NaN,
-    // as the softmax of nothing but -inf is; slots and tokens that do not count weigh 0 all the same
-    float p[NB][4];
+    float p[NB][4];  // (of slots and tokens that do not count 2^(-inf - m) = 0)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f(c[b][e] - m);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (lim[b] < kPage)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[b][e] = 4 * quad + e < lim[b] ? p[b][e] : 0.f;
-      lsum += (p[b][0] + p[b][1]) + (p[b][2] + p[b][3]);
-    }
+    for (int b = 0; b < NB; ++b) lsum += (p[b][0] + p[b][1]) + (p[b][2] + p[b][3]);
     if constexpr (BF16) {
       bf16x8 hi, lo;
 #pragma unroll
@@ -1345,8 +1343,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
     float den = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      // (a wave without pages has l = 0 and m = -inf)
-      const float f = sl[w][g] == 0.f ? 0.f : exp2f(sm[w][g] - mm);
+      const float f = exp2f(sm[w][g] - mm);  // (a wave without pages: l = 0 and m = kLowest)
       den += f * sl[w][g];
       o += f * *(const f32x4*)&sacc[w][g][d];
     }
@@ -1372,7 +1369,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
     const int g = e / (D / 4), d = e % (D / 4) * 4;
     const size_t w0 = (size_t)item * a.parts * G + g;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float mm = kNegInf, den = 0.f;
+    float mm = kLowest, den = 0.f;
     for (int j0 = 0; j0 < n; j0 += 8) {  // (slots past the last part read it again and weigh nothing)
       f32x4 v[8];
       float2 ml[8];
