@@ -383,6 +383,7 @@ struct AttendArgs {
   int launch_seqs;          // sequences of the launch's groups (set by launch_attend)
   int num_cus;
   float scale_log2;         // log2(e) / sqrt(D)
+  float lead;               // difference of scores that makes a weight of 2^8
 };
 
 // Optional timing events attached to the first / last dispatch of a launcher.

@@ -1045,8 +1045,10 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // pages in turn, each with an online softmax of its own, and are merged in LDS.
 // As in k_attn_bf16 the G q-heads of the kv-head are the columns of both products:
 //   S^T[16 tok x 16 heads] = K[16 x D] Q^T,   O^T[D x 16 heads] += V^T[D x 32 tok] P^T,
-// and the softmax's reference moves only when a score exceeds it by 8 (weights stay
-// within 2^8), so that the common page needs no rescaling.
+// and the softmax's reference moves only when a score exceeds it by `lead` (weights stay
+// within 2^8), so that the common page needs no rescaling. Scores and references are the
+// products q . k as summed; log2(e) / sqrt(D) scales their differences, so that a weight's
+// error grows with its distance from the reference and not with the scores' own size.
 // bf16: a batch is two pages, which the second product takes at once: its inner
 // dimension holds four tokens of the one and four of the other per lane, which is
 // where the scores' registers and V's 16-byte units have them. P goes in as the sum
@@ -1241,8 +1243,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
                                                         __uint_as_float(q[i][e]), c[b], 0, 0, 0);
         }
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c[b][e] *= a.scale_log2;
       if (lim < kPage) {  // uniform
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -1260,10 +1260,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
       }
       top = fmaxf(top, fmaxf(fmaxf(c[b][0], c[b][1]), fmaxf(c[b][2], c[b][3])));
     }
-    if (__any(top > m + 8.f)) {
+    if (__any(top > m + a.lead)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m, top), alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      const float mn = fmaxf(m, top), alpha = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
       m = mn;
       lsum *= alpha;
 #pragma unroll
@@ -1273,7 +1273,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f(c[b][e] - m);
+      for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f((c[b][e] - m) * a.scale_log2);
 #pragma unroll
     for (int b = 0; b < NB; ++b) lsum += (p[b][0] + p[b][1]) + (p[b][2] + p[b][3]);
     if constexpr (BF16) {
@@ -1343,12 +1343,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
     float den = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = exp2f(sm[w][g] - mm);  // (a wave without pages: l = 0 and m = kLowest)
+      const float f = exp2f((sm[w][g] - mm) * a.scale_log2);  // (a wave without pages: l = 0 and m = kLowest)
       den += f * sl[w][g];
       o += f * *(const f32x4*)&sacc[w][g][d];
     }
     if (a.parts == 1) {
-      store_x4<BF16>(a, it, g, d, D, o * (1.f / den));
+      store_x4<BF16>(a, it, g, d, D, o / den);
     } else {
       const size_t w = ((size_t)item * a.parts + part) * G + g;
       *(f32x4*)(a.part_acc + w * D + d) = o;
@@ -1357,7 +1357,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   }
 }
 
-// The merge of an item's parts: o = sum_j acc_j 2^(m_j - m*) / sum_j l_j 2^(m_j - m*).
+// The merge of an item's parts: o = sum_j acc_j 2^(c (m_j - m*)) / sum_j l_j 2^(c (m_j - m*)), c = scale_log2.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
   const uint32_t item = blockIdx.x;
@@ -1382,20 +1382,20 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
       float top = mm;
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
-      const float r = mm == top ? 1.f : exp2f(mm - top);
+      const float r = mm == top ? 1.f : exp2f((mm - top) * a.scale_log2);
       mm = top;
       den *= r;
       o *= r;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float f = j0 + j < n ? exp2f(ml[j].x - mm) : 0.f;
+        const float f = j0 + j < n ? exp2f((ml[j].x - mm) * a.scale_log2) : 0.f;
         if (j0 + j < n) {
           den += f * ml[j].y;
           o += f * v[j];
         }
       }
     }
-    store_x4<BF16>(a, it, g, d, D, o * (1.f / den));
+    store_x4<BF16>(a, it, g, d, D, o / den);
   }
 }
 

@@ -348,6 +348,7 @@ pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
   a.first = sel ? sel->n_first : 0;
   a.last = sel ? sel->n_last : 1;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cfg.head_dim));
+  a.lead = 8.f / a.scale_log2;
   return run_attend(c, a, select, st);
 }
 

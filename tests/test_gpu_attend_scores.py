@@ -119,3 +119,35 @@ def test_finite_scores_far_below_zero(low):
     torch.cuda.synchronize()
     want = v[32:48].mean(0)
     assert np.abs(_f64(x[0, 0]).reshape(2, 4) - want).max() <= 84 * 2.0 ** -24 * np.abs(v).max()
+
+
+@pytest.mark.parametrize("heads", [(2, 1, 64), (2, 1, 36)])
+@pytest.mark.parametrize("sel", [None, (6, 1, 1)])
+@pytest.mark.parametrize("far", [0.0, 20000.0, -300000.0])
+def test_scores_far_from_zero(heads, sel, far):
+    """Whole-number q and K, whose products are exact, all scores around far / sqrt(D): only differences count."""
+    d = heads[2]
+    m = Model([250, 20], 1, "f32", heads, 1, seed=44)
+    for s in range(2):
+        m.k[s] = m.k[s].clamp(-3, 3).round()
+        m.k[s][..., 0] = far
+    m.load()
+    m.sess.bind_summary()
+    m.sess.summarize()
+    q, kn, vn = m.rows(1)
+    q, kn = q.clamp(-3, 3).round(), kn.clamp(-3, 3).round()
+    q[..., 0], kn[..., 0] = 1, far
+    m.sess.append(None, kn, vn, rope=None)
+    m.grow(kn, vn, 1)
+    x = m.sess.attend(q, select=sel)["x"]
+    torch.cuda.synchronize()
+    for s in range(2):
+        qq, kk, vv = _f64(q[s, 0]), _f64(m.k[s][0, :, 0]), _f64(m.v[s][0, :, 0])
+        pages = L.chosen_pages(qq, kk, *sel) if sel else list(range(-(-len(kk) // PAGE)))
+        at = np.concatenate([np.arange(PAGE * p, min(PAGE * (p + 1), len(kk))) for p in pages])
+        sc = (qq @ kk[at].T) * np.log2(np.e) / np.sqrt(d)
+        # exponents: a difference of whole numbers (exact), times a constant rounded to fp32 and a rounding, twice
+        # (to the wave's reference and to the block's); exp2 and its uses 2^-21; sums over the tokens; a division
+        rel = 2 * (np.log(2) * np.ptp(sc, axis=1).max() * 4 * 2.0 ** -24 + 2.0 ** -21) + 2 * (len(at) + 4) * 2.0 ** -24
+        err = np.abs(_f64(x[s, 0]).reshape(-1, d) - L.attend(qq, kk, vv, pages))
+        assert err.max() <= rel * np.abs(vv).max(), (s, float(err.max()), rel)
