@@ -1054,7 +1054,10 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // where the scores' registers and V's 16-byte units have them. P goes in as the sum
 // of two bf16 values (what the first leaves over goes into the second, a relative
 // error of 2^-17): the matrix cores are idle anyway while the pages come in. fp32:
-// one page, fp32 matrix cores throughout.
+// one page, fp32 matrix cores throughout, a score summed in NA chains that are then added:
+// rounding errors of a chain add up like its length (heads of 128 dims, rms error of wide
+// rows' outputs 1.35e-6 with one chain, 3.7e-7 with four; of 64, 4.9e-7 and 3.9e-7 with
+// two). Four need registers that only one wave per SIMD has.
 // A wave holds the ids of its pages (a part has at most 64 per wave) one per lane, so
 // that no batch waits for a chain of list and page table, and loads a batch while it
 // works on the one before (no load is conditional: the wait for a batch must leave
@@ -1082,6 +1085,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
   using Regs = PageRegs<BF16, NU>;
   constexpr int NJ = BF16 ? 2 * NU : NU;  // 16-dim output blocks
   constexpr int NB = Regs::NB;            // pages per batch
+  constexpr int NA = BF16 ? 1 : NU > 6 ? 4 : 2;  // chains of a score's sum
   // fp32: row r of output block 4 g + c is dim 64 g + 4 r + c, so that a lane's V of four blocks is one 16-byte load
   // (the blocks past the last four: dim 16 j + r)
   constexpr int NV = BF16 ? 0 : NJ / 4 * 4;
@@ -1230,6 +1234,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
       // tokens of the page that count (a batch's slots past the part's end: none)
       const int lim = k0 + b < cnt ? min(it.pos + 1 - kPage * page, kPage) : 0;
       c[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 ch[NA];
+#pragma unroll
+      for (int e = 0; e < NA; ++e) ch[e] = c[b];
 #pragma unroll
       for (int i = 0; i < NU; ++i) {
         if constexpr (BF16) {
@@ -1239,10 +1246,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(!BF16 && NU
           const bool in = 16 * i + 4 * quad < D;  // (dims past D: 0 x 0)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            c[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? __uint_as_float(r.k[b][i][e]) : 0.f,
-                                                        __uint_as_float(q[i][e]), c[b], 0, 0, 0);
+            ch[e % NA] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? __uint_as_float(r.k[b][i][e]) : 0.f,
+                                                              __uint_as_float(q[i][e]), ch[e % NA], 0, 0, 0);
         }
       }
+      if constexpr (!BF16) c[b] = NA == 4 ? (ch[0] + ch[1]) + (ch[2] + ch[NA - 1]) : ch[0] + ch[NA - 1];
       if (lim < kPage) {  // uniform
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

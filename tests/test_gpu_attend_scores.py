@@ -151,3 +151,36 @@ def test_scores_far_from_zero(heads, sel, far):
         rel = 2 * (np.log(2) * np.ptp(sc, axis=1).max() * 4 * 2.0 ** -24 + 2.0 ** -21) + 2 * (len(at) + 4) * 2.0 ** -24
         err = np.abs(_f64(x[s, 0]).reshape(-1, d) - L.attend(qq, kk, vv, pages))
         assert err.max() <= rel * np.abs(vv).max(), (s, float(err.max()), rel)
+
+
+def _one_chain(q, k):
+    """q k^T as one fp32 chain per score, products added one after the other (fused): what a single accumulator gives."""
+    s = np.zeros((len(q), len(k)), np.float32)
+    for d in range(q.shape[1]):
+        s = (s.astype(np.float64) + q[:, d:d + 1] * k[None, :, d]).astype(np.float32)
+    return s.astype(np.float64)
+
+
+@pytest.mark.parametrize("heads", [(4, 4, 64), (4, 4, 80), (4, 4, 128)])
+def test_fp32_scores_are_summed_in_more_than_one_chain(heads):
+    """Wide q, so that the scores' sums make most of the error. A chain's rounding errors add up like its length (each
+    is of the partial sum's size, which grows like the root): two halves, added, have 1/sqrt(2) = 0.71 of its error."""
+    d = heads[2]
+    m = Model([700, 900, 1100, 1300, 800], 1, "f32", heads, 2, seed=45)
+    q, kn, vn = m.rows(1)
+    q = q * 4
+    m.sess.append(None, kn, vn, rope=None)
+    m.grow(kn, vn, 1)
+    x = m.sess.attend(q)["x"]
+    torch.cuda.synchronize()
+    mine = chain = 0.0
+    for s in range(m.S):
+        for l in range(2):
+            for h in range(m.hkv):
+                qq, kk, vv = _f64(q[s, l, h:h + 1]), _f64(m.k[s][l, :, h]), _f64(m.v[s][l, :, h])
+                want = L.attend(qq, kk, vv, range(-(-len(kk) // PAGE)))
+                w = _one_chain(qq, kk) / np.sqrt(d)
+                w = np.exp(w - w.max())
+                mine += ((_f64(x[s, l]).reshape(-1, d)[h] - want) ** 2).sum() / (want ** 2).sum()
+                chain += (((w / w.sum()) @ vv - want) ** 2).sum() / (want ** 2).sum()
+    assert mine <= 0.85 ** 2 * chain, (mine ** 0.5, chain ** 0.5)
