@@ -506,10 +506,11 @@ pced_status pced_advance(pced_ctx* ctx, int32_t n_tokens);
  * pced_summary_bytes: size of the buffer for cfg (0 if invalid).
  * pced_bind_summary (host-only) gives the context a caller-owned device buffer of
  * that size, 256-byte aligned, without contents (NULL: none). pced_summarize brings
- * it up to date with the loaded caches and all appended tokens: call it after
- * binding, after pced_load_caches, and after steps or prefills made by other calls
- * than pced_append, which keeps an up-to-date buffer so. Work is enqueued for pages
- * not covered yet only.
+ * it up to date with the sequences as long as they are: call it after binding, after
+ * pced_load_caches, and after steps or prefills made by other calls than pced_append,
+ * which keeps an up-to-date buffer so. Rows that were appended before the buffer was up
+ * to date and are not part of the sequences yet are not covered: append them again
+ * behind this call. Work is enqueued for pages not covered yet only.
  * Errors: INVALID_ARG (misaligned), STATE (nothing loaded, none bound), HIP.
  */
 size_t pced_summary_bytes(const pced_config* cfg);
@@ -544,7 +545,7 @@ typedef struct pced_select {
  *              (numbers within the sequence) of each row and kv-head, ascending, -1
  *              behind the last (needs sel)
  * Errors: STATE (nothing loaded; fewer rows appended to a layer; summaries wanted but
- * not bound or not up to date), INVALID_ARG, CAPACITY (pages), HIP.
+ * not bound, or not up to date when the rows were appended), INVALID_ARG, CAPACITY (pages), HIP.
  */
 pced_status pced_attend(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q,
                         const pced_select* sel, void* x_out, int32_t* pages_out, hipStream_t stream);

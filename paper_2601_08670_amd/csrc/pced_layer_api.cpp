@@ -286,8 +286,8 @@ pced_status pced_summarize(pced_ctx* c, hipStream_t st) {
   for (int s = 0; s < c->S; ++s)
     a.span = std::max(a.span, c->len[s] / kPage - std::max(c->len[s] - a.behind, 0) / kPage);
   HIP_OK(launch_summarize(a, c->bf16, st));
+  // (rows behind the lengths that pced_append has summarised stay so: their layers were up to date)
   std::fill(c->behind.begin(), c->behind.end(), 0);
-  std::fill(c->ahead.begin(), c->ahead.end(), 0);
   return PCED_OK;
 }
 
