@@ -217,7 +217,11 @@ class PcedSession:
         st = t.stride()
         if (d > 1 and st[3] != 1) or (heads > 1 and st[2] != d) or (n_layers > 1 and st[1] != heads * d):
             raise ValueError(f"{name}: a row's elements must follow each other")
-        return st[0] if shape[0] > 1 else n_layers * heads * d
+        if shape[0] == 1:
+            return n_layers * heads * d
+        if st[0] < n_layers * heads * d:  # (a broadcast row has distance 0, which the library takes for rows without gaps)
+            raise ValueError(f"{name}: the rows overlap")
+        return st[0]
 
     def _rope(self, rope):
         """(theta, rot_dim, halves) as the library takes it."""
