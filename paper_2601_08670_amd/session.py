@@ -39,7 +39,7 @@ class Adjust:
         unknown = set(tensors) - set(self.DTYPES)
         if unknown:
             raise ValueError(f"unknown adjustments {sorted(unknown)}")
-        self.n_queries, self.vocab = n_queries, vocab
+        self.n_queries, self.vocab, self.device = n_queries, vocab, device
         self.tensors = {k: t for k, t in tensors.items() if t is not None}
         for name, t in self.tensors.items():
             if t.dtype != getattr(torch, self.DTYPES[name]):
@@ -312,6 +312,8 @@ class PcedSession:
     def _adjust(self, adjust):
         if adjust.n_queries != self.B or adjust.vocab != self.geom["vocab"]:
             raise ValueError("the adjustments are another batch's")
+        if adjust.device != self.k_pool.device:
+            raise ValueError(f"the adjustments are on {adjust.device}, the session is on {self.k_pool.device}")
         return adjust.struct
 
     def adjust_logits(self, logits, adjust, out=None):

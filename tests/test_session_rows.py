@@ -55,3 +55,13 @@ def test_distances_of_rows(session):
     session.S = 1  # (one row: no distance)
     session.append(*(x[:1].expand(1, -1, -1, -1) for x in _rows(1)))
     assert session.ctx.rows == [(HQ * w, HKV * w, HKV * w), (0, 100, 100), (w * (HQ + 2 * HKV),) * 3, (HQ * w, HKV * w, HKV * w)]
+
+
+def test_adjustments_of_another_device_are_refused(session):
+    """Same number of queries and vocabulary, but their lists lie elsewhere."""
+    from paper_2601_08670_amd.session import Adjust
+    here, there = Adjust(1, 10, torch.device("cpu")), Adjust(1, 10, torch.device("cuda", 1))
+    session.k_pool = torch.empty(0)
+    assert session._adjust(here) is here.struct
+    with pytest.raises(ValueError, match="cuda:1"):
+        session._adjust(there)
