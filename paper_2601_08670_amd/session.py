@@ -79,7 +79,6 @@ class PcedSession:
                  max_attn_chunks=0, aggregation="max", beta_scalar=False, ffn_dim=0, rope_theta=500000):
         torch = _torch()
         self.dtype = dtype
-        self.device = device
         self.geom = dict(n_layers=n_layers, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads,
                          head_dim=head_dim, vocab=vocab)
         self.ffn_dim = ffn_dim
@@ -96,6 +95,7 @@ class PcedSession:
         if poison:  # all-ones bytes: NaN in bf16 and f32, to expose reads of unwritten memory
             for t in (self.k_pool, self.v_pool, self.ctx.workspace):
                 t.fill_(255)
+        self.device = self.k_pool.device  # ("cuda": the one that is current now, for later allocations too)
         self._device_index = self.k_pool.get_device()
         self._dtypes = (torch.bfloat16, torch.int16, torch.uint16) if dtype == "bf16" else (torch.float32,)
         self._rows, self._ropes, self._out_like = _lib.pced_rows(), {}, {}

@@ -65,3 +65,20 @@ def test_adjustments_of_another_device_are_refused(session):
     assert session._adjust(here) is here.struct
     with pytest.raises(ValueError, match="cuda:1"):
         session._adjust(there)
+
+
+def test_a_session_names_its_device(monkeypatch):
+    """"cuda" is the device that is current when the session is made; what it allocates later lies there too."""
+    class Context:
+        def __init__(self, cfg, device):
+            self.workspace = torch.empty(1)
+
+        def pced_bind_summary(self, summary):
+            pass
+
+    monkeypatch.setattr(_lib, "Context", Context)
+    s = PcedSession(n_layers=1, n_q_heads=4, n_kv_heads=2, head_dim=8, vocab=10, dtype="f32", max_queries=1, max_seqs=2,
+                    max_pages=2, max_pages_per_seq=1, device="cpu")
+    assert s.device == s.k_pool.device == torch.device("cpu")
+    s.bind_summary()
+    assert s.summary.device == s.k_pool.device
