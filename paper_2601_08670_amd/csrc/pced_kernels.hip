@@ -2313,7 +2313,7 @@ __device__ __forceinline__ AdjustTok4 adjust_tok4(const AdjustArgs& a, int b, in
   for (int c = 0; c < 4; ++c) {
     const int n = L.cnt[i + c], e = L.bias[i + c];
     t.shift[c] = freq * (float)n;
-    t.bias[c] = e > 0 ? a.bias_value[e - 1] : 0.f;
+    t.bias[c] = e > 0 ? a.bias_value[e - 1] : -0.f;  // (none: x + -0 is x, zeros of either sign too)
     t.seen |= (n > 0 ? 1u : 0u) << c;
   }
   return t;
