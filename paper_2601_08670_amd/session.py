@@ -302,7 +302,7 @@ class PcedSession:
     # ------------------------------------------------------- adjusted logits
     def adjust(self, **tensors):
         """The loaded batch's adjustments (see Adjust) for adjust_logits and fuse_adjusted."""
-        return Adjust(self.B, self.geom["vocab"], self.k_pool.device, **tensors)
+        return Adjust(self.B, self.geom["vocab"], self.device, **tensors)
 
     def _logits(self, t, name):
         if t.dtype != _torch().float32 or t.shape != (self.S, self.geom["vocab"]) or not t.is_contiguous():
@@ -312,8 +312,8 @@ class PcedSession:
     def _adjust(self, adjust):
         if adjust.n_queries != self.B or adjust.vocab != self.geom["vocab"]:
             raise ValueError("the adjustments are another batch's")
-        if adjust.device != self.k_pool.device:
-            raise ValueError(f"the adjustments are on {adjust.device}, the session is on {self.k_pool.device}")
+        if adjust.device != self.device:
+            raise ValueError(f"the adjustments are on {adjust.device}, the session is on {self.device}")
         return adjust.struct
 
     def adjust_logits(self, logits, adjust, out=None):

@@ -22,6 +22,7 @@ def session(monkeypatch):
     s = object.__new__(PcedSession)
     s.geom = dict(n_layers=L, n_q_heads=HQ, n_kv_heads=HKV, head_dim=D, vocab=10)
     s.S, s.B, s._device_index, s.k_pool, s.dtype, s._dtypes = S, 1, -1, torch.empty(0), "f32", (torch.float32,)
+    s.device = torch.device("cpu")
     s._rows, s._ropes, s.ctx = _lib.pced_rows(), {}, Calls()
     monkeypatch.setattr(_lib, "current_device", lambda: -1)
     return s
@@ -61,7 +62,6 @@ def test_adjustments_of_another_device_are_refused(session):
     """Same number of queries and vocabulary, but their lists lie elsewhere."""
     from paper_2601_08670_amd.session import Adjust
     here, there = Adjust(1, 10, torch.device("cpu")), Adjust(1, 10, torch.device("cuda", 1))
-    session.k_pool = torch.empty(0)
     assert session._adjust(here) is here.struct
     with pytest.raises(ValueError, match="cuda:1"):
         session._adjust(there)
