@@ -1065,7 +1065,7 @@ __device__ __forceinline__ void store_x4(const AttendArgs& a, const AttendItem& 
 // Tokens behind the row's own position get weight 0, and their V counts as 0 (those
 // rows may hold anything).
 // Bound: HBM where items abound (16 layers of 33 sequences, 32 of up to 128 pages, 8
-// kv-heads, PICK: 1.18 GB in 208 us, 5.7 TB/s); start and drain of short streams at one
+// kv-heads, PICK: 1.18 GB in 209 us, 5.6 TB/s); start and drain of short streams at one
 // layer (18 us for 74 MB; 256 pages of 9 sequences in 504 work-groups, 29 us for 134 MB);
 // with many tokens the way from the L2, which has most of their pages (24 tokens of 17
 // sequences, 64 pages each, 53 us for 0.8 GB of which HBM gives a sixth).
