@@ -1,0 +1,646 @@
+"""Performance cases of decoding over caches held in 8 bits and of sampling: append, attention, token draw.
+
+A program that owns its projections keeps the documents' caches in 8 bits and draws its tokens. A decode
+step is append -> attend per layer, then logits -> sample. The three operators:
+
+* ``append``: the new tokens' K / V rows of every sequence go behind the last token, K and the query rows
+  rotated by each token's own position; pages (16 tokens) that the rows fill are encoded: 8-bit codes with
+  a scale per page, kv-head and K or V (pced_append8).
+* ``attend``: every new token attends to all tokens of its sequence up to itself, those of the pages that
+  were complete before the call from their codes, the rest as stored (pced_attend8).
+* ``sample``: a token per query, drawn with given random numbers from the softmax of Eq. 2's best scores at
+  a temperature, cut by top-k, top-p and min-p, over logits with penalties and a mask (pced_sample).
+
+Sequence lengths, the page order and what the calls are given as host values are functions of the case
+alone; tensor values come from the seed.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False  # True: run() makes the framework's calls; False: the operators' plain forms
+
+DEV = "cuda"
+PAGE = 16
+THETA = 500000.0
+GAMMA = 2.5
+TOP = {"e4m3": 448.0, "int8": 127.0}  # the largest code
+LLAMA = dict(hq=32, hkv=8, d=128)
+
+
+def listed():
+    return [
+        # the smallest append: one token of a small model into five short caches; latency
+        dict(name="append_token_4docs", kind="append", code="e4m3", layers=1, hq=8, hkv=2, d=64, docs=4, lo=100, hi=128,
+             amateur=16, tokens=1, rot=64, halves=False),
+        # a decode step's token into 33 caches, eight layers whose rows are at hand together
+        dict(name="append_token_8layers", kind="append", code="e4m3", layers=8, **LLAMA, docs=32, lo=32, hi=256,
+             amateur=16, tokens=1, rot=128, halves=False),
+        # a 64-token question processed into 33 caches, one layer, rows straight from a fused projection's output;
+        # three or four pages of every cache fill up and are encoded
+        dict(name="append_question", kind="append", code="e4m3", layers=1, **LLAMA, docs=32, lo=100, hi=1024, amateur=16,
+             tokens=64, rot=128, halves=True, fused=True),
+        # the smallest attention: one token of a small model over five short caches; latency
+        dict(name="attend_token_4docs", kind="attend", code="e4m3", layers=1, hq=8, hkv=2, d=64, docs=4, lo=100, hi=300,
+             amateur=16, tokens=1),
+        # a decode step's layer over 32 retrieved documents
+        dict(name="attend_32docs", kind="attend", code="int8", layers=1, **LLAMA, docs=32, lo=512, hi=2048, amateur=64,
+             tokens=1),
+        # the same for 16 layers whose queries are at hand together
+        dict(name="attend_32docs_16layers", kind="attend", code="e4m3", layers=16, **LLAMA, docs=32, lo=512, hi=2048,
+             amateur=64, tokens=1),
+        # decode over whole books of up to 131072 tokens, pages scattered over the pool
+        dict(name="attend_books", kind="attend", code="e4m3", layers=1, **LLAMA, docs=8, lo=32768, hi=131072, amateur=64,
+             tokens=1, scatter=True),
+        # a 24-token question over 16 long documents, seven q-heads to a kv-head
+        dict(name="attend_question", kind="attend", code="int8", layers=1, hq=28, hkv=4, d=128, docs=16, lo=2000, hi=8192,
+             amateur=33, tokens=24),
+        # one document, a small vocabulary, the usual filters: the shortest draw
+        dict(name="sample_1doc", kind="sample", vocab=32000, queries=1, docs=1, history=0, allowed=None, temperature=0.7,
+             top_k=50, top_p=0.9, min_p=0.0),
+        # one query over 32 documents, nucleus sampling behind a chat's penalties
+        dict(name="sample_32docs", kind="sample", vocab=128256, queries=1, docs=32, history=700, allowed=None,
+             temperature=0.8, top_k=0, top_p=0.95, min_p=0.0),
+        # five creative generations: a high temperature and a floor, so that tens of thousands of tokens count
+        dict(name="sample_hot", kind="sample", vocab=50257, queries=5, docs=8, history=0, allowed=None, temperature=1.5,
+             top_k=0, top_p=1.0, min_p=0.0005),
+        # concurrent queries over many documents, half of the tokens allowed, every filter at once
+        dict(name="sample_16x16", kind="sample", vocab=151936, queries=16, docs=16, history=1000, allowed=0.5,
+             temperature=1.0, top_k=1000, top_p=0.98, min_p=0.001),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+HEADS = [(32, 8, 128), (32, 8, 128), (8, 2, 64), (16, 16, 64), (28, 4, 128), (40, 8, 128), (64, 8, 64), (32, 2, 128)]
+VOCABS = [32000, 50257, 128256, 151936]
+
+
+def draw(rng):
+    kind = rng.choices(["append", "attend", "sample"], [25, 40, 35])[0]
+    if kind == "sample":
+        queries = rng.choice([1, 1, 2, 5, 16])
+        return dict(kind=kind, vocab=rng.choice(VOCABS + [_log(rng, 1000, 152000)]), queries=queries,
+                    docs=max(1, min(_log(rng, 1, 64), 270 // queries - 1)),
+                    history=rng.choice([0, _log(rng, 1, 4000)]), allowed=rng.choice([None, None, 0.9, 0.5, 0.02]),
+                    temperature=rng.choice([0.0, round(rng.uniform(0.05, 2.0), 3), round(rng.uniform(0.5, 1.2), 3)]),
+                    top_k=rng.choice([0, 0, 1, _log(rng, 2, 5000)]),
+                    top_p=rng.choice([1.0, round(rng.uniform(0.3, 0.999), 3)]),
+                    min_p=rng.choice([0.0, round(rng.uniform(0.0001, 0.2), 4)]))
+    hq, hkv, d = rng.choice(HEADS)
+    tokens = rng.choice([1, 1, 1, _log(rng, 2, 64)])
+    docs = _log(rng, 1, 48)
+    c = dict(kind=kind, code="e4m3", hq=hq, hkv=hkv, d=d, docs=docs, tokens=tokens,
+             layers=1 if tokens > 1 or rng.random() < 0.5 else _log(rng, 2, 8 if kind == "append" else 16))
+    per_page = 4.0 * PAGE * hkv * d * c["layers"] * (docs + 1)  # bytes of a page of every cache, in 16 bits
+    room = 2.5e8 if kind == "append" else 2.0e9 / max(1.0, tokens * hq / hkv / 128)
+    hi = max(16, min(_log(rng, 64, 16384 if kind == "append" else 131072), int(room / per_page) * PAGE))
+    c.update(lo=max(1, hi // rng.choice([1, 4, 8])), hi=hi, amateur=rng.choice([1, 15, 16, 33, 64]),
+             scatter=rng.random() < 0.4)
+    if kind == "append":
+        return dict(c, rot=rng.choice([d, d, d // 16 * 8]), halves=rng.random() < 0.5,
+                    fused=c["layers"] == 1 and rng.random() < 0.5)
+    return dict(c, code=rng.choice(["e4m3", "int8"]))
+
+
+# ------------------------------------------------------------------ shapes
+
+def _lens(c):
+    """Tokens of each sequence before the call: one amateur, then the documents."""
+    rng = random.Random("%s" % sorted((k, v) for k, v in c.items() if k != "name"))
+    return [c["amateur"]] + [rng.randint(c["lo"], c["hi"]) for _ in range(c["docs"])]
+
+
+def _table(c):
+    """Physical page of every page of every sequence, -1 past its last one; the pool's pages."""
+    need = [-(-(n + c["tokens"]) // PAGE) for n in _lens(c)]
+    order = np.arange(sum(need), dtype=np.int64)
+    if c.get("scatter"):
+        np.random.RandomState(sum(need)).shuffle(order)
+    table, at = np.full((len(need), max(need)), -1, np.int64), 0
+    for s, n in enumerate(need):
+        table[s, :n] = order[at:at + n]
+        at += n
+    return table, sum(need)
+
+
+def _ring(c):
+    """Open pages that a sequence holds: those that its new rows may touch. Page p is in place p % ring."""
+    return (c["tokens"] + 14) // PAGE + 1
+
+
+def _gen(seed, tag):
+    return torch.Generator(DEV).manual_seed((int(seed) * 1009 + tag) % (1 << 62))
+
+
+def _normal(shape, seed, tag, dtype=torch.float32, scale=1.0):
+    return torch.empty(shape, dtype=dtype, device=DEV).normal_(0.0, scale, generator=_gen(seed, tag))
+
+
+def _ints(x):
+    return torch.as_tensor(np.asarray(x), device=DEV)
+
+
+def _places(c):
+    """Place of element (token, dim) in a tile of 16 tokens: K codes, V codes, open K page, open V page."""
+    t, d = np.arange(PAGE)[:, None], np.arange(c["d"])[None, :]
+    quad, j = d % 32 // 8, d // 16
+    k8 = (d // 64 * 64 + t + 16 * quad) * 16 + d % 64 // 32 * 8 + d % 8
+    v8 = (d // 64 * 64 + d % 16 + 16 * (t // 4)) * 16 + d % 64 // 16 * 4 + t % 4
+    k16 = (d // 32 * 64 + t + 16 * quad) * 8 + d % 8
+    v16 = ((j // 2 * 64 + d % 16 + 16 * (t // 4)) * 2 + j % 2) * 4 + t % 4
+    return [_ints(x) for x in (k8, v8, k16, v16)]
+
+
+# ------------------------------------------------------------------ inputs
+
+def _caches(c, seed):
+    """K and V of every page of the pool, [L][pages][Hkv][16][D] in bf16: keys of neighbouring tokens resemble each
+    other, as a text's do (a direction per page, and noise), and a few dims of K are far larger than the others."""
+    pages = _table(c)[1]
+    shape = (c["layers"], pages, c["hkv"], PAGE, c["d"])
+    k = _normal(shape, seed, 11, torch.bfloat16) + 0.7 * _normal(shape[:3] + (1, c["d"]), seed, 12, torch.bfloat16)
+    k[..., 5::32] *= 6.0
+    return k, _normal(shape, seed, 13, torch.bfloat16)
+
+
+def _rows(c, seed):
+    """q, k, v rows of the new tokens, [S * tokens][L][heads][D]; fused: views of one projection's output."""
+    R, L, d = len(_lens(c)) * c["tokens"], c["layers"], c["d"]
+    hs = (c["hq"], c["hkv"], c["hkv"])
+    if c.get("fused"):
+        qkv = _normal((R, sum(hs) * d), seed, 21, torch.bfloat16)
+        return tuple(x.view(R, 1, h, d) for x, h in zip(qkv.split([h * d for h in hs], dim=1), hs))
+    return tuple(_normal((R, L, h, d), seed, 22 + i, torch.bfloat16) for i, h in enumerate(hs))
+
+
+def _scale(x, code):
+    """The scales of blocks (last dim) of values: the largest magnitude over the largest code, rounded up to bf16."""
+    top = x.float().abs().amax(-1).clamp(2.0 ** -100, 2.0 ** 127)
+    top = top / torch.full_like(top, TOP[code])  # (by a number torch would multiply by its inverse)
+    return ((top.view(torch.int32) + 0xFFFF) & ~0xFFFF).view(torch.float32)
+
+
+def _codes(x, scale, code):
+    """Blocks (last dim) of values as codes: values times 1 / scale, to the nearest code, ties to the even one."""
+    y = (x.float() * (1.0 / scale)[..., None]).clamp(-TOP[code], TOP[code])
+    return y.to(torch.float8_e4m3fn) if code == "e4m3" else y.round().to(torch.int8)
+
+
+def _held(x, code):
+    """Codes and scales of pages [..., 16, D]."""
+    flat = x.flatten(-2)
+    scale = _scale(flat, code)
+    return _codes(flat, scale, code).view(x.shape), scale
+
+
+def _limits(c, seed):
+    """What a serving program holds per query: the tokens so far (-1 where a slot of a padded batch is empty) with
+    their penalties, the grammar's allowed tokens as bits, the sampling's settings and this step's random numbers."""
+    r = np.random.RandomState((int(seed) * 31 + 7) % (1 << 31))
+    B, V, n = c["queries"], c["vocab"], c["history"]
+    adj = {}
+    if n:
+        history = np.minimum(r.zipf(1.3, B * n) - 1, V - 1).astype(np.int32)
+        history = np.where(r.rand(B * n) < 0.3, r.randint(0, V, B * n), history).astype(np.int32)
+        history[r.rand(B * n) < 0.05] = -1
+        adj = dict(history=_ints(history), history_off=_ints((np.arange(B + 1) * n).astype(np.int32)),
+                   repetition=_ints(r.uniform(1.0, 1.4, B).astype(np.float32)),
+                   presence=_ints(r.uniform(0.0, 0.8, B).astype(np.float32)),
+                   frequency=_ints(r.uniform(0.0, 0.3, B).astype(np.float32)))
+    if c["allowed"] is not None:
+        words = -(-V // 32)
+        bits = torch.rand((B, words, 32), device=DEV, generator=_gen(seed, 31)) < c["allowed"]
+        bits[:, 0, 1] = True  # the end of the answer is always allowed
+        word = (bits.long() << torch.arange(32, device=DEV)).sum(-1)
+        adj["mask"] = torch.where(word >= 1 << 31, word - (1 << 32), word).to(torch.int32)
+    each = r.uniform(0.9, 1.1, B)  # the queries' users have settings of their own
+    cut = dict(temperature=_ints((c["temperature"] * each).astype(np.float32)))
+    if c["top_k"]:
+        cut["top_k"] = _ints(np.maximum(1, (c["top_k"] * each).astype(np.int32)))
+    if c["top_p"] < 1.0:
+        cut["top_p"] = _ints((c["top_p"] * np.minimum(each, 1.0)).astype(np.float32))
+    if c["min_p"]:
+        cut["min_p"] = _ints((c["min_p"] * each).astype(np.float32))
+    return adj, cut, _ints(r.random_sample(B).astype(np.float32) * np.float32(1.0 - 2.0 ** -24))
+
+
+def _logits(c, seed):
+    """Logits of related rows: an expert mostly agrees with its amateur."""
+    per = c["docs"] + 1
+    t = _normal((c["queries"], per, c["vocab"]), seed, 41, scale=0.8)
+    return (t + _normal((c["queries"], 1, c["vocab"]), seed, 42, scale=2.5)).view(c["queries"] * per, c["vocab"])
+
+
+def _scores(c, seed):
+    """Relevance scores and fixed contrastive strengths, per document."""
+    r = np.random.RandomState((int(seed) * 17 + 3) % (1 << 31))
+    n = c["queries"] * c["docs"]
+    return r.uniform(0.02, 0.98, n).astype(np.float32), r.uniform(0.1, 1.0, n).astype(np.float32)
+
+
+# ------------------------------------------------------------------ prepare
+
+def _session(c, k, v):
+    """A session that holds the sequences' caches in 8 bits, loaded as a datastore holds them ([L][len][Hkv][D])."""
+    from paper_2601_08670_amd.session import PcedSession
+    table, pages = _table(c)
+    sess = PcedSession(n_layers=c["layers"], n_q_heads=c["hq"], n_kv_heads=c["hkv"], head_dim=c["d"], vocab=1000,
+                       dtype="bf16", max_queries=1, max_seqs=table.shape[0], max_pages=pages,
+                       max_pages_per_seq=table.shape[1], device=DEV, kv8=c["code"], max_new=c["tokens"])
+    for t in (sess.k_codes, sess.v_codes, sess.scales, sess.k_open, sess.v_open):
+        t.zero_()
+    lens = _lens(c)
+    flat = lambda x, s, n: x[:, _ints(table[s, :-(-n // PAGE)])].permute(0, 1, 3, 2, 4).reshape(  # noqa: E731
+        c["layers"], -1, c["hkv"], c["d"])[:, :n].contiguous()
+    ks, vs = [flat(k, s, n) for s, n in enumerate(lens)], [flat(v, s, n) for s, n in enumerate(lens)]
+    sess.load([c["docs"]], lens, ks, vs, [0.5] * c["docs"], beta=[0.5] * c["docs"], page_table=table.astype(np.int32))
+    torch.cuda.current_stream().synchronize()
+    return sess
+
+
+def _complete(c):
+    """[pages]: whether the pool's page was complete before the call."""
+    table, pages = _table(c)
+    there = np.arange(table.shape[1])[None, :] < np.asarray(_lens(c))[:, None] // PAGE
+    full = np.zeros(pages, bool)
+    full[table[there]] = True
+    return _ints(full)
+
+
+def _held_state(c, k, v):
+    """The codes, scales and open pages of the sequences as they are before the call, as the framework lays them out."""
+    table, pages = _table(c)
+    lens, ring, L, H, d = np.asarray(_lens(c)), _ring(c), c["layers"], c["hkv"], c["d"]
+    at = _places(c)
+    full = _complete(c).view(1, -1, 1, 1)
+    st = {}
+    scales = torch.zeros((L, H, pages, 2), dtype=torch.bfloat16, device=DEV)
+    for i, (name, x) in enumerate((("k", k), ("v", v))):
+        codes, scale = _held(x, c["code"])
+        raw = torch.where(full, codes.view(torch.uint8).flatten(-2), 0)
+        st[name + "_codes"] = torch.zeros((L, pages, H, PAGE * d), dtype=torch.uint8, device=DEV)
+        st[name + "_codes"][..., at[i].reshape(-1)] = raw
+        scales[..., i] = torch.where(full[..., 0], scale, 0).transpose(1, 2).to(torch.bfloat16)
+        st[name + "_open"] = torch.zeros((L, lens.size * ring, H, PAGE * d), dtype=torch.bfloat16, device=DEV)
+        s = np.nonzero(lens % PAGE)[0]
+        if s.size:
+            p = lens[s] // PAGE
+            tail = x[:, _ints(table[s, p])]
+            tail = torch.where(_ints(np.arange(PAGE)[None, :] < (lens[s] % PAGE)[:, None])[None, :, None, :, None], tail, 0)
+            tile = torch.zeros((L, s.size, H, PAGE * d), dtype=torch.bfloat16, device=DEV)
+            tile[..., at[2 + i].reshape(-1)] = tail.flatten(-2)
+            st[name + "_open"][:, _ints(s * ring + p % ring)] = tile
+    st["scales"] = scales
+    return st
+
+
+def prepare(case, seed):
+    c, kind = dict(case), case["kind"]
+    st = dict(case=c, kind=kind)
+    if kind == "sample":
+        st["logits"] = _logits(c, seed)
+        st["adj"], st["cut"], st["u"] = _limits(c, seed)
+        rel, beta = _scores(c, seed)
+        if own:
+            from paper_2601_08670_amd.session import PcedSession
+            S = c["queries"] * (c["docs"] + 1)
+            sess = st["sess"] = PcedSession(n_layers=1, n_q_heads=4, n_kv_heads=1, head_dim=64, vocab=c["vocab"],
+                                            dtype="bf16", max_queries=c["queries"], max_seqs=S, max_pages=S,
+                                            max_pages_per_seq=1, device=DEV)
+            cache = [torch.zeros((1, 1, 1, 64), dtype=torch.bfloat16, device=DEV)] * S
+            sess.load([c["docs"]] * c["queries"], [1] * S, cache, cache, rel.tolist(), gamma=GAMMA, beta=beta.tolist())
+            st["adj"] = sess.adjust(**st["adj"]) if st["adj"] else None
+            st["cut"] = sess.sampling(**st["cut"])
+        st["beta"] = _ints(beta)
+        st["prior"] = _ints((GAMMA * np.log(np.clip(rel.astype(np.float64), 1e-8, 1 - 1e-8))).astype(np.float32))
+        return st
+    k, v = _caches(c, seed)
+    st["lens"], st["table"] = _ints(np.asarray(_lens(c))), _ints(_table(c)[0])
+    if kind == "append":
+        st["q"], st["k"], st["v"] = _rows(c, seed)
+        if own:
+            st["sess"] = _session(c, k, v)
+        else:
+            st.update(_held_state(c, k, v), at=_places(c))
+        return st
+    st["q"] = _rows(c, seed)[0]
+    pos = st["lens"][:, None] + torch.arange(c["tokens"], device=DEV)
+    if own:
+        st["sess"] = _session(c, k, v)
+        phys = torch.gather(st["table"], 1, pos // PAGE).reshape(-1)
+        new = [x[:, phys, :, pos.reshape(-1) % PAGE].contiguous() for x in (k, v)]  # [R][L][Hkv][D]
+        st["sess"].append(None, *new, n_tokens=c["tokens"], rope=None)
+        return st
+    (st["k_codes"], st["k_scale"]), (st["v_codes"], st["v_scale"]) = _held(k, c["code"]), _held(v, c["code"])
+    # the open pages of every sequence, [S][ring]: as stored
+    first = st["lens"][:, None] // PAGE + torch.arange(_ring(c), device=DEV)
+    phys = torch.gather(st["table"], 1, first.clamp(max=st["table"].shape[1] - 1)).clamp(min=0)
+    st["k_open"], st["v_open"], st["open_page"] = k[:, phys], v[:, phys], first  # [L][S][ring][Hkv][16][D]
+    return st
+
+
+# -------------------------------------------------------------- plain forms
+
+def _rotated(x, cos, sin, rot, halves):
+    """x [S][T][L][H][D] in fp32, the pairs of its first `rot` dims turned by the rows' angles."""
+    x, rest = x[..., :rot].float(), x[..., rot:].float()
+    a, b = (x[..., :rot // 2], x[..., rot // 2:]) if halves else (x[..., 0::2], x[..., 1::2])
+    cos, sin = cos[:, :, None, None], sin[:, :, None, None]
+    pair = (a * cos - b * sin, a * sin + b * cos)
+    return torch.cat([torch.cat(pair, -1) if halves else torch.stack(pair, -1).flatten(-2), rest], -1)
+
+
+def _filled(c):
+    """The pages that the call's rows complete: sequence, page, physical page."""
+    lens, T = np.asarray(_lens(c)), c["tokens"]
+    page = np.arange(_table(c)[0].shape[1])[None, :]
+    s, p = np.nonzero((page >= (lens // PAGE)[:, None]) & (page < ((lens + T) // PAGE)[:, None]))
+    return s, p, _table(c)[0][s, p]
+
+
+def _append(st):
+    c = st["case"]
+    S, T, L, d, ring = st["lens"].numel(), c["tokens"], c["layers"], c["d"], _ring(c)
+    pos = st["lens"][:, None] + torch.arange(T, device=DEV)
+    i = torch.arange(c["rot"] // 2, device=DEV, dtype=torch.float64)
+    angle = pos[..., None].double() * THETA ** (-2.0 * i / c["rot"])
+    cos, sin = angle.cos().float(), angle.sin().float()
+    q, k = (_rotated(x.view(S, T, L, -1, d), cos, sin, c["rot"], c["halves"]).to(torch.bfloat16)
+            for x in (st["q"], st["k"]))
+    place = (torch.arange(S, device=DEV)[:, None] * ring + pos // PAGE % ring).view(-1, 1, 1, 1)
+    slot = (pos % PAGE).view(-1)
+    layer = torch.arange(L, device=DEV).view(1, L, 1, 1)
+    head = torch.arange(c["hkv"], device=DEV).view(1, 1, -1, 1)
+    k8, v8, k16, v16 = st["at"]
+    st["k_open"][layer, place, head, k16[slot][:, None, None]] = k.reshape(S * T, L, -1, d)
+    st["v_open"][layer, place, head, v16[slot][:, None, None]] = st["v"].reshape(S * T, L, -1, d)
+    s, p, phys = _filled(c)
+    if s.size:
+        at, phys = _ints(s * ring + p % ring), _ints(phys)
+        k_page, v_page = st["k_open"][:, at][..., k16.reshape(-1)], st["v_open"][:, at][..., v16.reshape(-1)]
+        k_scale, v_scale = _scale(k_page, c["code"]), _scale(v_page, c["code"])
+        k_tile = torch.zeros(k_page.shape, dtype=torch.uint8, device=DEV)
+        v_tile = torch.zeros(v_page.shape, dtype=torch.uint8, device=DEV)
+        k_tile[..., k8.reshape(-1)] = _codes(k_page, k_scale, c["code"]).view(torch.uint8)
+        v_tile[..., v8.reshape(-1)] = _codes(v_page, v_scale, c["code"]).view(torch.uint8)
+        st["k_codes"][:, phys], st["v_codes"][:, phys] = k_tile, v_tile
+        st["scales"][:, :, phys] = torch.stack([k_scale, v_scale], -1).transpose(1, 2).to(torch.bfloat16)
+    return dict(q=q.reshape(S * T, L, -1, d), **_buffers(st))
+
+
+def _buffers(st):
+    """The updated state: codes as the numbers they are, scales, open pages."""
+    return dict(k_codes=st["k_codes"].view(torch.float8_e4m3fn).view(-1),
+                v_codes=st["v_codes"].view(torch.float8_e4m3fn).view(-1), scales=st["scales"].view(-1),
+                k_open=st["k_open"].view(-1), v_open=st["v_open"].view(-1))
+
+
+def _sequences(st, which):
+    """Keys or values of every sequence as attention sees them, [L][S][Hkv][tokens][D] in fp32."""
+    c, table = st["case"], st["table"].clamp(min=0)
+    x = st[which + "_codes"][:, table].float() * st[which + "_scale"][:, table][..., None, None]  # [L][S][P][Hkv][16][D]
+    S, P = table.shape
+    seq, page = torch.arange(S, device=DEV)[:, None].expand_as(st["open_page"]), st["open_page"]
+    ok = page < P
+    x[:, seq[ok], page[ok]] = st[which + "_open"][:, ok].float()
+    return x.permute(0, 1, 3, 2, 4, 5).reshape(c["layers"], S, c["hkv"], P * PAGE, c["d"])
+
+
+def _attend(st):
+    c = st["case"]
+    S, T, L, H, d = st["lens"].numel(), c["tokens"], c["layers"], c["hkv"], c["d"]
+    G = c["hq"] // H
+    q = st["q"].view(S, T, L, H, G, d).permute(2, 0, 3, 1, 4, 5).reshape(L, S, H, T * G, d).float()
+    s = torch.matmul(q, _sequences(st, "k").transpose(-1, -2)) / math.sqrt(d)
+    token = torch.arange(s.shape[-1], device=DEV)
+    pos = st["lens"][:, None] + torch.arange(T, device=DEV)
+    seen = (token <= pos[..., None]).repeat_interleave(G, 1)[None, :, None]  # [1][S][1][T G][tokens]
+    s = torch.where(seen, s, -math.inf)
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    # rows behind the last new token count for nothing, whatever they hold
+    v = torch.where((token <= pos[:, -1:])[None, :, None, :, None], _sequences(st, "v"), 0)
+    o = torch.matmul(p, v) / p.sum(-1, keepdim=True)
+    return o.view(L, S, H, T, G, d).permute(1, 3, 0, 2, 4, 5).reshape(S * T, L, c["hq"] * d).to(torch.bfloat16)
+
+
+def _adjusted(st):
+    """The logits [B][N + 1][V] after penalties and mask."""
+    c, a = st["case"], st["adj"]
+    B, V = c["queries"], c["vocab"]
+    s = st["logits"].view(B, -1, V)
+    if "history" in a:
+        token = a["history"]
+        row = torch.searchsorted(a["history_off"][1:].long(), torch.arange(token.numel(), device=DEV), right=True)
+        at, ok = row * V + token.long().clamp(0, V - 1), (token >= 0) & (token < V)
+        count = torch.zeros(B * V, dtype=torch.int32, device=DEV).index_add_(0, at, ok.to(torch.int32)).view(B, 1, V)
+        rep, pres, freq = (a[n].view(B, 1, 1) for n in ("repetition", "presence", "frequency"))
+        seen = count > 0
+        s = torch.where(seen, torch.where(s > 0, s / rep, s * rep), s)
+        s = torch.where(seen, (s - freq * count.float()) - pres, s)
+    if "mask" in a:
+        v = torch.arange(V, device=DEV)
+        s = torch.where(((a["mask"][:, v // 32] >> (v % 32)) & 1).bool()[:, None], s, -math.inf)
+    return s
+
+
+def _sample(st):
+    """Scores in 32 bits, as Eq. 2 is everywhere; their softmax in 64, where sums of 150000 weights meet borders."""
+    c, cut = st["case"], st["cut"]
+    B, V = c["queries"], c["vocab"]
+    s = _adjusted(st)
+    beta, prior = st["beta"].view(B, -1, 1), st["prior"].view(B, -1, 1)
+    fused = ((1.0 + beta) * s[:, 1:] - beta * s[:, :1]) + prior
+    fused = torch.where(torch.isfinite(s[:, 1:]), fused, -math.inf)  # a masked token is nobody's choice
+    best = fused.amax(1)
+    score, order = torch.sort(best, dim=-1, descending=True, stable=True)  # equal scores: the lower token first
+    top = score[:, :1].double()
+    t = cut["temperature"].double()[:, None]
+    greedy = t <= 0
+    t = torch.where(greedy, 1.0, t)
+    z = (score.double() - top) / t
+    w = z.exp()
+    rank = torch.arange(V, device=DEV)
+    keep = (score > -math.inf) & (~greedy | (rank < 1))
+    if "top_k" in cut:
+        keep &= rank < cut["top_k"][:, None]
+    w = torch.where(keep, w, 0)
+    if "top_p" in cut:
+        keep &= (w.cumsum(-1) - w < cut["top_p"].double()[:, None] * w.sum(-1, keepdim=True)) | (rank < 1)
+    if "min_p" in cut:
+        keep &= (score.double() >= top + t * cut["min_p"].double()[:, None].log()) | (rank < 1)
+    w = torch.where(keep, w, 0)
+    total = w.sum(-1, keepdim=True)
+    kept = keep.sum(-1, keepdim=True)
+    at = torch.minimum((w.cumsum(-1) <= st["u"].double()[:, None] * total).sum(-1, keepdim=True), kept - 1)
+    token = order.gather(1, at)
+    who = fused.gather(2, token.view(-1, 1, 1).expand(-1, c["docs"], 1))[..., 0]
+    expert = torch.arange(1, c["docs"] + 1, device=DEV).view(1, -1)
+    got = score.gather(1, at)
+    winner = torch.where(who == got, expert, c["docs"] + 1).amin(-1)
+    return dict(tokens=token[:, 0].to(torch.int32), winner=winner.to(torch.int32), score=got[:, 0],
+                logprob=(z.gather(1, at) - total.log())[:, 0].float(), kept=kept[:, 0].to(torch.int32))
+
+
+# ---------------------------------------------------------------------- run
+
+def run(state):
+    st, kind, c = state, state["kind"], state["case"]
+    if not own:
+        return {"append": _append, "attend": _attend, "sample": _sample}[kind](st)
+    sess = st["sess"]
+    if kind == "append":
+        q = sess.append(st["q"], st["k"], st["v"], n_tokens=c["tokens"], rope=(THETA, c["rot"], c["halves"]))
+        return dict(q=q, **_buffers(dict(k_codes=sess.k_codes, v_codes=sess.v_codes, scales=sess.scales,
+                                         k_open=sess.k_open, v_open=sess.v_open)))
+    if kind == "attend":
+        return sess.attend(st["q"], n_tokens=c["tokens"])["x"]
+    return sess.sample(st["logits"], st["cut"], st["u"], adjust=st["adj"], want=("winner", "score", "logprob", "kept"))
+
+
+# --------------------------------------------------------------------- work
+
+def work(case):
+    c, kind = case, case["kind"]
+    if kind == "sample":
+        n = 4.0 * c["queries"] * (c["docs"] + 1) * c["vocab"]
+        lists = c["queries"] * (4.0 * c["history"] + (c["vocab"] / 8.0 if c["allowed"] is not None else 0))
+        return dict(bytes=n + lists, flops=n)
+    lens = _lens(c)
+    R, L, T, H, d = len(lens) * c["tokens"], c["layers"], c["tokens"], c["hkv"], c["d"]
+    if kind == "append":
+        full = sum((n + T) // PAGE - n // PAGE for n in lens)
+        old = sum(n % PAGE for n in lens if (n + T) // PAGE > n // PAGE)  # tokens of filled pages that were there
+        return dict(bytes=4.0 * R * L * d * (c["hq"] + 2.0 * H) + 2.0 * L * H * (d * (PAGE * full + 2.0 * old) + 2.0 * full),
+                    flops=L * (3.0 * R * c["rot"] * (c["hq"] + H) + 4.0 * H * d * PAGE * full))
+    by = sum(n // PAGE * (2.0 * PAGE * d + 4) + (n % PAGE + T) * 4.0 * d for n in lens)
+    fl = sum(4.0 * d * (c["hq"] // H) * sum(n + i + 1 for i in range(T)) for n in lens)
+    return dict(bytes=L * (H * by + R * 4.0 * c["hq"] * d), flops=L * H * fl)
+
+
+# -------------------------------------------------------------------- exact
+
+def _exact_append(c, seed):
+    """Rotation as a product of complex numbers, sequence by sequence; a code is the value over its scale."""
+    q, k, v = (x.double() for x in _rows(c, seed))
+    T, rot, L, d, ring = c["tokens"], c["rot"], c["layers"], c["d"], _ring(c)
+    table, pages = _table(c)
+    k8, v8, k16, v16 = _places(c)
+    lens = _lens(c)
+
+    def turn(x, p):
+        z = x[..., :rot]
+        z = torch.complex(z[..., :rot // 2], z[..., rot // 2:]) if c["halves"] else torch.view_as_complex(
+            z.reshape(z.shape[:-1] + (rot // 2, 2)).contiguous())
+        w = p[:, None, None, None].double() * torch.exp(
+            -math.log(THETA) * torch.arange(0, rot, 2, device=DEV, dtype=torch.float64) / rot)
+        z = z * torch.polar(torch.ones_like(w), w)
+        z = torch.cat([z.real, z.imag], -1) if c["halves"] else torch.view_as_real(z).flatten(-2)
+        return torch.cat([z, x[..., rot:]], -1)
+
+    zeros = lambda n, dt=torch.float64: torch.zeros((L, n, c["hkv"], PAGE * d), dtype=dt, device=DEV)  # noqa: E731
+    codes, opened = (zeros(pages), zeros(pages)), (zeros(len(lens) * ring), zeros(len(lens) * ring))
+    scales = torch.zeros((L, c["hkv"], pages, 2), dtype=torch.float64, device=DEV)
+    turned = []
+    for s, n in enumerate(lens):
+        p = torch.arange(n, n + T, device=DEV)
+        mine = slice(s * T, (s + 1) * T)
+        turned.append(turn(q[mine], p))
+        new = (turn(k[mine], p), v[mine])
+        for i, x in enumerate(_caches(c, seed)):
+            need = -(-(n + T) // PAGE)
+            x = x[:, _ints(table[s, :need])].double().permute(0, 1, 3, 2, 4).reshape(L, need * PAGE, c["hkv"], d).clone()
+            x[:, n:n + T] = new[i].transpose(0, 1)
+            x[:, n + T:] = 0
+            x = x.view(L, need, PAGE, c["hkv"], d).transpose(2, 3)
+            for page in range(need):
+                tile = x[:, page].flatten(-2)
+                if page >= n // PAGE:
+                    opened[i][:, s * ring + page % ring][..., (k16, v16)[i].reshape(-1)] = tile
+                if page < (n + T) // PAGE:
+                    held = tile.to(torch.bfloat16).double()  # (what the page holds is what is encoded)
+                    top = held.abs().amax(-1).clamp(min=2.0 ** -100)
+                    top = top / torch.full_like(top, TOP[c["code"]])
+                    m, e = torch.frexp(top)
+                    unit = (e.long() - 8 + 1023 << 52).view(torch.float64)  # 2^(e - 8), exactly
+                    scale = torch.ceil(m * 256) * unit  # eight bits, from above
+                    codes[i][:, table[s, page]][..., (k8, v8)[i].reshape(-1)] = held / scale[..., None]
+                    scales[:, :, table[s, page], i] = scale
+    return dict(q=torch.cat(turned).view(-1, L, c["hq"], d), k_codes=codes[0].view(-1), v_codes=codes[1].view(-1),
+                scales=scales.view(-1), k_open=opened[0].view(-1), v_open=opened[1].view(-1))
+
+
+def _exact_attend(c, seed):
+    """One sequence, layer and kv-head at a time."""
+    k, v = _caches(c, seed)
+    T, L, H, d, G = c["tokens"], c["layers"], c["hkv"], c["d"], c["hq"] // c["hkv"]
+    table, lens = _table(c)[0], _lens(c)
+    if len(lens) * L * H > 6000 or sum(lens) * T * H * L > 3e8:
+        return None
+    q = _rows(c, seed)[0].double().view(len(lens), T, L, H, G, d)
+    out = torch.zeros((len(lens), T, L, H, G, d), dtype=torch.float64, device=DEV)
+    for s, n in enumerate(lens):
+        ids = _ints(table[s, :-(-(n + T) // PAGE)])
+        for l in range(L):
+            seq = []
+            for x in (k, v):
+                x = x[l, ids]  # [pages][Hkv][16][D]
+                codes, scale = _held(x, c["code"])
+                full = (torch.arange(len(ids), device=DEV) < n // PAGE).view(-1, 1, 1, 1)
+                seq.append(torch.where(full, codes.double() * scale.double()[..., None, None], x.double()))
+            for h in range(H):
+                kk, vv = (x[:, h].reshape(-1, d)[:n + T] for x in seq)
+                z = q[s, :, l, h].reshape(T * G, d) @ kk.T / d ** 0.5
+                late = torch.arange(n + T, device=DEV)[None, :] > n + torch.arange(T, device=DEV)[:, None]
+                z = z.masked_fill(late.repeat_interleave(G, 0), -math.inf)
+                out[s, :, l, h] = (torch.softmax(z, -1) @ vv).view(T, G, d)
+    return out.view(len(lens) * T, L, c["hq"] * d)
+
+
+def _exact_sample(c, seed):
+    """Query by query on the host: the scores in 64 bits, sorted, summed one after the other."""
+    logits = _logits(c, seed).cpu().numpy().astype(np.float64)
+    adj, cut, u = _limits(c, seed)
+    adj, cut = ({n: x.cpu().numpy() for n, x in y.items()} for y in (adj, cut))
+    rel, beta = (x.astype(np.float64) for x in _scores(c, seed))
+    B, V, N, n = c["queries"], c["vocab"], c["docs"], c["history"]
+    got = dict(tokens=[], winner=[], score=[], logprob=[], kept=[])
+    for b in range(B):
+        s = logits[b * (N + 1):(b + 1) * (N + 1)]
+        if n:
+            mine = adj["history"][b * n:(b + 1) * n]
+            count = np.bincount(mine[mine >= 0], minlength=V).astype(np.float64)
+            rep = np.float64(adj["repetition"][b])
+            s = np.where(count > 0, np.where(s > 0, s / rep, s * rep), s)
+            s = s - count * np.float64(adj["frequency"][b]) - (count > 0) * np.float64(adj["presence"][b])
+        w = slice(b * N, (b + 1) * N)
+        f = s[1:] + beta[w, None] * (s[1:] - s[:1]) + GAMMA * np.log(rel[w, None])
+        best = f.max(0)
+        if "mask" in adj:
+            best[~np.unpackbits(adj["mask"][b].view(np.uint8), bitorder="little")[:V].astype(bool)] = -np.inf
+        t = float(cut["temperature"][b])
+        order = np.argsort(-best, kind="stable")[:int(np.isfinite(best).sum())]
+        k = 1 if t <= 0 else int(cut["top_k"][b]) if "top_k" in cut else len(order)
+        order = order[:max(1, k)]
+        z = (best[order] - best[order[0]]) / (t if t > 0 else 1.0)
+        mass = np.cumsum(np.exp(z))
+        if "top_p" in cut:
+            mass = mass[:1 + int((mass < float(cut["top_p"][b]) * mass[-1]).sum())]
+        if "min_p" in cut:
+            mass = mass[:max(1, int((np.exp(z[:len(mass)]) >= float(cut["min_p"][b])).sum()))]
+        i = min(int((mass <= float(u[b]) * mass[-1]).sum()), len(mass) - 1)
+        got["tokens"].append(np.int32(order[i]))
+        got["winner"].append(np.int32(f[:, order[i]].argmax() + 1))
+        got["score"].append(best[order[i]])
+        got["logprob"].append(z[i] - math.log(mass[-1]))
+        got["kept"].append(np.int32(len(mass)))
+    return {name: _ints(np.asarray(x)) for name, x in got.items()}
+
+
+def exact(case, seed):
+    c = dict(case)
+    return {"append": _exact_append, "attend": _exact_attend, "sample": _exact_sample}[c["kind"]](c, seed)
