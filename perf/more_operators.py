@@ -5,9 +5,9 @@ step is append -> attend per layer, then logits -> sample. The three operators:
 
 * ``append``: the new tokens' K / V rows of every sequence go behind the last token, K and the query rows
   rotated by each token's own position; pages (16 tokens) that the rows fill are encoded: 8-bit codes with
-  a scale per page, kv-head and K or V (pced_append8).
+  a scale per page, kv-head and K or V (pced_append_codes).
 * ``attend``: every new token attends to all tokens of its sequence up to itself, those of the pages that
-  were complete before the call from their codes, the rest as stored (pced_attend8).
+  were complete before the call from their codes, the rest as stored (pced_attend_codes).
 * ``sample``: a token per query, drawn with given random numbers from the softmax of Eq. 2's best scores at
   a temperature, cut by top-k, top-p and min-p, over logits with penalties and a mask (pced_sample).
 
