@@ -551,6 +551,76 @@ pced_status pced_attend(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t 
                         const pced_select* sel, void* x_out, int32_t* pages_out, hipStream_t stream);
 
 /*
+ * Caches held in 8 bits, for batches whose documents' caches would not fit, or whose steps wait for them
+ * (Section 3: one precomputed cache per document; bf16 contexts). A sequence's complete
+ * pages (16 tokens) are codes, with one scale per page, layer, kv-head and K or V; the rows behind its
+ * last complete page stay bf16, in a ring of open pages per sequence, until they fill
+ * one. For the 16 * head_dim values x of such a block, in fp32:
+ *     scale = min(max(max |x|, 2^-100), 2^127) / M, rounded up to bf16     (M = 448 or 127)
+ *     code  = x * (1 / scale), rounded to the nearest code (ties to even) within -M .. M
+ * and a value is code * scale exactly. NaN counts as 0. A block is off by at most half a step of its
+ * codes: relative 2^-4 of each value (E4M3, of values from 2^-6 scale on), or scale / 2 (INT8).
+ * The calls below take the place of pced_load_caches, pced_append, pced_attend and pced_read_cache; pced_advance,
+ * pced_get_lengths, and the calls on logits and hidden states serve both. The others, which read or write
+ * the pools, refuse such a batch (UNSUPPORTED), as these refuse one in the pools (STATE).
+ */
+typedef enum pced_code {
+  PCED_CODE_E4M3 = 1,  /* 8-bit floating point: 4 exponent bits, 3 of the significand, largest 448 */
+  PCED_CODE_INT8 = 2   /* -127 .. 127                                                              */
+} pced_code;
+
+/* Device buffers of such a batch, caller-owned, 256-byte aligned, without contents at first. Codes lie as
+ * the pools' tiles do: [layer][page][kv_head][16 x head_dim] bytes; scales: [layer][kv_head][page] of
+ * a bf16 for K and one for V; open pages: bf16 tiles [layer][seq * R + page % R][kv_head], R =
+ * (max_new + 14) / 16 + 1. */
+typedef struct pced_cache8 {
+  int32_t code;      /* pced_code                                                          */
+  int32_t max_new;   /* tokens per sequence that one pced_append_codes may bring, at most: 1 .. 2^20 */
+  void* k_codes;     /* pced_codes_bytes(cfg) each */
+  void* v_codes;
+  void* scales;      /* pced_scales_bytes(cfg) */
+  void* k_open;      /* pced_open_bytes(cfg, max_new) each */
+  void* v_open;
+} pced_cache8;
+
+/* Sizes of the buffers (0 for an invalid cfg, an fp32 one, or max_new < 1). */
+size_t pced_codes_bytes(const pced_config* cfg);
+size_t pced_scales_bytes(const pced_config* cfg);
+size_t pced_open_bytes(const pced_config* cfg, int32_t max_new);
+
+/*
+ * pced_load_caches into a cache in 8 bits (copied as a struct; the buffers stay in use until the next
+ * load). Arguments, order of work and errors are those of pced_load_caches; UNSUPPORTED for
+ * fp32 contexts.
+ */
+pced_status pced_load_codes(pced_ctx* ctx, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
+                       const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
+                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                       const float* beta, hipStream_t stream);
+
+/*
+ * pced_append into a cache in 8 bits: the rows go into the open pages, K rotated, and pages that
+ * they fill are encoded. Like there the call may be repeated, for other or fewer rows, until pced_advance.
+ * Arguments and errors are those of pced_append; CAPACITY also for n_tokens > max_new.
+ */
+pced_status pced_append_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
+                         const pced_rope* rope, void* q_out, hipStream_t stream);
+
+/*
+ * Attention of the new tokens over a cache in 8 bits, after pced_append_codes of the same layers: row (s, i)
+ * attends to tokens 0 .. len_s + i, those of the pages that were complete at len_s as codes * scale, the others as
+ * they were appended. Sums and softmax in fp32; arguments and errors are those of pced_attend
+ * without sel.
+ */
+pced_status pced_attend_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q, void* x_out,
+                         hipStream_t stream);
+
+/* pced_read_cache of a cache in 8 bits: codes * scale, rounded to bf16, and the rows behind the last
+ * complete page as they are. */
+pced_status pced_read_codes(pced_ctx* ctx, int32_t seq, int32_t layer, int32_t start, int32_t count, void* k_out,
+                       void* v_out, hipStream_t stream);
+
+/*
  * Adjustments of a query's logits before a token is chosen. All pointers are device
  * memory, read when the call runs. For query b and token v, with h the number of
  * history entries that are v:

@@ -26,7 +26,9 @@ EXPORTED = ("pced_pool_bytes", "pced_lm_head_bytes", "pced_pack_lm_head", "pced_
             "pced_model_bytes", "pced_pack_model_layer", "pced_pack_model_globals", "pced_model_prefill",
             "pced_model_step", "pced_model_generate", "pced_read_cache", "pced_lmhead_noalloc",
             "pced_stream_read", "pced_append", "pced_advance", "pced_summary_bytes", "pced_bind_summary",
-            "pced_summarize", "pced_attend", "pced_adjust_logits", "pced_fuse_adjusted")
+            "pced_summarize", "pced_attend", "pced_adjust_logits", "pced_fuse_adjusted",
+            "pced_codes_bytes", "pced_scales_bytes", "pced_open_bytes", "pced_load_codes", "pced_append_codes", "pced_attend_codes",
+            "pced_read_codes")
 
 
 class PcedError(RuntimeError):
@@ -66,6 +68,12 @@ class pced_rows(ctypes.Structure):
 
 class pced_select(ctypes.Structure):
     _fields_ = [("n_pages", ctypes.c_int32), ("n_first", ctypes.c_int32), ("n_last", ctypes.c_int32)]
+
+
+class pced_cache8(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_int32), ("max_new", ctypes.c_int32), ("k_codes", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("k_open", ctypes.c_void_p),
+                ("v_open", ctypes.c_void_p)]
 
 
 class pced_adjust(ctypes.Structure):
@@ -127,6 +135,13 @@ def load_library() -> ctypes.CDLL:
         "pced_attend": (I, [P, I, I, I, P, ctypes.POINTER(pced_select), P, P, V]),
         "pced_adjust_logits": (I, [P, P, ctypes.POINTER(pced_adjust), P, V]),
         "pced_fuse_adjusted": (I, [P, P, I, ctypes.POINTER(pced_adjust), P, ctypes.POINTER(pced_step_out), V]),
+        "pced_codes_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config)]),
+        "pced_scales_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config)]),
+        "pced_open_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config), I]),
+        "pced_load_codes": (I, [P, I, P, P, P, P, ctypes.POINTER(pced_cache8), P, I, P, ctypes.c_float, P, V]),
+        "pced_append_codes": (I, [P, I, I, I, ctypes.POINTER(pced_rows), ctypes.POINTER(pced_rope), P, V]),
+        "pced_attend_codes": (I, [P, I, I, I, P, P, V]),
+        "pced_read_codes": (I, [P, I, I, I, I, P, P, V]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -186,6 +201,18 @@ def pced_summary_bytes(cfg: pced_config) -> int:
     return load_library().pced_summary_bytes(ctypes.byref(cfg))
 
 
+def pced_codes_bytes(cfg: pced_config) -> int:
+    return load_library().pced_codes_bytes(ctypes.byref(cfg))
+
+
+def pced_scales_bytes(cfg: pced_config) -> int:
+    return load_library().pced_scales_bytes(ctypes.byref(cfg))
+
+
+def pced_open_bytes(cfg: pced_config, max_new: int) -> int:
+    return load_library().pced_open_bytes(ctypes.byref(cfg), int(max_new))
+
+
 def pced_model_bytes(cfg: pced_config) -> int:
     return load_library().pced_model_bytes(ctypes.byref(cfg))
 
@@ -205,6 +232,7 @@ def pced_pack_model_globals(cfg: pced_config, embed, final_norm, model, stream=N
 
 SCORE_MODES = {"dense": 0, "colbert": 1, "sparse": 2}
 AGGREGATIONS = {"max": 0, "moe": 1, "poe": 2}
+CODES = {"e4m3": 1, "int8": 2}
 
 
 def pced_relevance(mode: str, retrieval, reranker_logits=None):
@@ -300,6 +328,22 @@ class Context:
     def pced_load_caches(self, n_experts: Sequence[int], cache_len: Sequence[int], src_k, src_v,
                          k_pool, v_pool, relevance, gamma=2.5, beta=None, page_table=None,
                          reserve_tokens=0, stream=None):
+        self._load(self.lib.pced_load_caches, n_experts, cache_len, src_k, src_v,
+                   (k_pool.data_ptr(), v_pool.data_ptr()), relevance, gamma, beta, page_table, reserve_tokens, stream)
+        # the sources are read by the load kernel: keep them alive with the context
+        self._keep = [list(src_k), list(src_v), k_pool, v_pool]
+
+    def pced_load_codes(self, n_experts: Sequence[int], cache_len: Sequence[int], src_k, src_v, code, max_new, k_codes,
+                   v_codes, scales, k_open, v_open, relevance, gamma=2.5, beta=None, page_table=None,
+                   reserve_tokens=0, stream=None):
+        buffers = (k_codes, v_codes, scales, k_open, v_open)
+        cache = pced_cache8(CODES[code], max_new, *[_ptr(t) for t in buffers])
+        self._load(self.lib.pced_load_codes, n_experts, cache_len, src_k, src_v, (ctypes.byref(cache),), relevance, gamma,
+                   beta, page_table, reserve_tokens, stream)
+        self._keep = [list(src_k), list(src_v), *buffers]
+
+    def _load(self, call, n_experts, cache_len, src_k, src_v, to, relevance, gamma, beta, page_table, reserve_tokens,
+              stream):
         S = len(cache_len)
         ks = (ctypes.c_void_p * S)(*[t.data_ptr() for t in src_k])
         vs = (ctypes.c_void_p * S)(*[t.data_ptr() for t in src_v])
@@ -312,11 +356,8 @@ class Context:
         cl = _i32_array(cache_len)
         rel = _f32_array(relevance)
         bt = None if beta is None else _f32_array(beta)
-        _check(self.lib.pced_load_caches(self.handle, len(n_experts), ne, cl, ks, vs, k_pool.data_ptr(),
-                                         v_pool.data_ptr(), pt, int(reserve_tokens), rel,
-                                         ctypes.c_float(gamma), bt, _stream(stream)))
-        # the sources are read by the load kernel: keep them alive with the context
-        self._keep = [list(src_k), list(src_v), k_pool, v_pool]
+        _check(call(self.handle, len(n_experts), ne, cl, ks, vs, *to, pt, int(reserve_tokens), rel,
+                    ctypes.c_float(gamma), bt, _stream(stream)))
 
     def pced_step(self, q, k_new, v_new, lm_head, tokens_out, extra: Optional[dict] = None, stream=None):
         so = _step_out(extra)
@@ -381,6 +422,21 @@ class Context:
                                       _stream(stream))
         if status:
             _check(status)
+
+    def pced_append_codes(self, layer, n_layers, n_tokens, rows: pced_rows, rope: Optional[pced_rope], q_out, stream=None):
+        status = self.lib.pced_append_codes(self.handle, layer, n_layers, n_tokens, ctypes.byref(rows),
+                                       None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream))
+        if status:
+            _check(status)
+
+    def pced_attend_codes(self, layer, n_layers, n_tokens, q, x_out, stream=None):
+        status = self.lib.pced_attend_codes(self.handle, layer, n_layers, n_tokens, _ptr(q), _ptr(x_out), _stream(stream))
+        if status:
+            _check(status)
+
+    def pced_read_codes(self, seq, layer, start, count, k_out, v_out, stream=None):
+        _check(self.lib.pced_read_codes(self.handle, int(seq), int(layer), int(start), int(count), k_out.data_ptr(),
+                                   v_out.data_ptr(), _stream(stream)))
 
     def pced_adjust_logits(self, logits, adjust: pced_adjust, out, stream=None):
         _check(self.lib.pced_adjust_logits(self.handle, _ptr(logits), ctypes.byref(adjust), _ptr(out),

@@ -300,8 +300,8 @@ bool is_device_memory(const void* p) {
 // whole layers as the region holds (K in its first half, V in its second), or,
 // where one layer does not fit, as many of its pages. Copies and kernels follow
 // each other on the stream, so the region is free again for the next piece.
-pced_status load_from_host(pced_ctx* c, LoadArgs a, int s, int len, const char* src_k, const char* src_v,
-                           hipStream_t st) {
+pced_status load_from_host(pced_ctx* c, LoadArgs a, const LoadTarget& to, int s, int len, const char* src_k,
+                           const char* src_v, hipStream_t st) {
   const size_t row = (size_t)c->cfg.n_kv_heads * c->cfg.head_dim * esize_of(c->cfg);
   const size_t half = c->lay.stage_bytes / 2;
   char* stage = c->at<char>(c->lay.part_acc);
@@ -318,7 +318,7 @@ pced_status load_from_host(pced_ctx* c, LoadArgs a, int s, int len, const char* 
     a.n_layers = nl;
     a.page0 = t0 / kPage;
     a.one_len = n;
-    HIP_OK(launch_load(a, ceil_div(n, kPage), c->bf16, st));
+    HIP_OK(to.launch(a, to, ceil_div(n, kPage), c->bf16, st));
     return PCED_OK;
   };
   const int L = c->cfg.n_layers, fit = (int)std::min<size_t>(L, half / (len * row));
@@ -339,6 +339,12 @@ pced_status check_ctx(const pced_ctx* c, bool need_loaded) {
   if (!c) return fail(PCED_ERR_INVALID_ARG, "ctx is NULL");
   if (need_loaded && !c->loaded) return fail(PCED_ERR_STATE, "no batch loaded (call pced_load_caches first)");
   return PCED_OK;
+}
+
+pced_status check_pools(const pced_ctx* c) {
+  const pced_status r = check_ctx(c, true);
+  if (r == PCED_OK && c->c8.code) return fail(PCED_ERR_UNSUPPORTED, "the batch's caches are in 8 bits (pced_load_codes)");
+  return r;
 }
 
 void advance(pced_ctx* c, int n, bool by_rows) {
@@ -1010,7 +1016,7 @@ pced_status run_prefill_chunk(pced_ctx* c, const char* model, const int32_t* tok
 }
 
 pced_status check_model(const pced_ctx* c, const void* model) {
-  pced_status r = check_ctx(c, true);
+  pced_status r = check_pools(c);
   if (r != PCED_OK) return r;
   if (c->cfg.ffn_dim <= 0) return fail(PCED_ERR_STATE, "no decoder stack configured (ffn_dim == 0)");
   if (!model) return fail(PCED_ERR_INVALID_ARG, "model is NULL");
@@ -1150,84 +1156,17 @@ pced_status run_step(pced_ctx* c, const void* q, const void* k_new, const void* 
 
 }  // namespace
 
-extern "C" {
-
-size_t pced_pool_bytes(const pced_config* cfg) {
-  if (!cfg_valid(cfg, nullptr)) return 0;
-  return (size_t)cfg->n_layers * cfg->max_pages * cfg->n_kv_heads * kPage * cfg->head_dim * esize_of(*cfg);
-}
-
-size_t pced_lm_head_bytes(const pced_config* cfg) {
-  if (!cfg_valid(cfg, nullptr)) return 0;
-  if (cfg->dtype == PCED_BF16) return (size_t)ceil_div(cfg->vocab, 16) * 16 * cfg->hidden * 2;
-  return (size_t)cfg->vocab * cfg->hidden * 4;
-}
-
-pced_status pced_pack_lm_head(const pced_config* cfg, const void* w, void* w_packed, hipStream_t st) {
-  std::string why;
-  if (!cfg_valid(cfg, &why)) return fail(PCED_ERR_INVALID_ARG, "invalid config: %s", why.c_str());
-  if (!w || !w_packed) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
-  const char* a = (const char*)w;
-  const char* b = (const char*)w_packed;
-  const size_t na = (size_t)cfg->vocab * cfg->hidden * esize_of(*cfg), nb = pced_lm_head_bytes(cfg);
-  if (a < b + nb && b < a + na) return fail(PCED_ERR_INVALID_ARG, "w and w_packed overlap");
-  HIP_OK(launch_pack_lm_head(w, w_packed, cfg->vocab, cfg->hidden, cfg->dtype == PCED_BF16, st));
-  return PCED_OK;
-}
-
-size_t pced_workspace_bytes(const pced_config* cfg) {
-  if (!cfg_valid(cfg, nullptr)) return 0;
-  return make_layout(*cfg).total;
-}
-
-const char* pced_last_error(void) { return g_err.c_str(); }
-
-pced_status pced_create(const pced_config* cfg, void* d_workspace, size_t ws_bytes, pced_ctx** out) {
-  std::string why;
-  if (!out) return fail(PCED_ERR_INVALID_ARG, "out is NULL");
-  *out = nullptr;
-  if (!cfg_valid(cfg, &why)) return fail(PCED_ERR_INVALID_ARG, "invalid config: %s", why.c_str());
-  if (!d_workspace) return fail(PCED_ERR_INVALID_ARG, "workspace is NULL");
-  if ((uintptr_t)d_workspace % kAlign) return fail(PCED_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  const Layout lay = make_layout(*cfg);
-  if (ws_bytes < lay.total)
-    return fail(PCED_ERR_CAPACITY, "workspace too small: %zu < %zu bytes", ws_bytes, lay.total);
-  pced_ctx* c = new pced_ctx();
-  c->cfg = *cfg;
-  c->lay = lay;
-  c->ws = (char*)d_workspace;
-  c->bf16 = cfg->dtype == PCED_BF16;
-  c->G = cfg->n_q_heads / cfg->n_kv_heads;
-  c->appended.assign(cfg->n_layers, 0);
-  c->ahead.assign(cfg->n_layers, 0);
-  c->behind.assign(cfg->n_layers, kNotCovered);
-  *out = c;
-  return PCED_OK;
-}
-
-void pced_destroy(pced_ctx* ctx) {
-  if (!ctx) return;
-  for (auto& r : ctx->recs) {
-    (void)hipEventDestroy(r.a);
-    (void)hipEventDestroy(r.b);
-  }
-  for (auto e : ctx->ev_free) (void)hipEventDestroy(e);
-  if (ctx->blas) rocblas_destroy_handle(ctx->blas);
-  delete ctx;
-}
-
-pced_status pced_load_caches(pced_ctx* c, int32_t n_queries, const int32_t* n_experts,
-                             const int32_t* cache_len, const void* const* src_k,
-                             const void* const* src_v, void* k_pool, void* v_pool,
-                             const int32_t* page_table, int32_t reserve_tokens,
-                             const float* relevance, float gamma, const float* beta,
-                             hipStream_t st) {
+namespace pced {
+pced_status load_batch(pced_ctx* c, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
+                       const void* const* src_k, const void* const* src_v, const LoadTarget& to,
+                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                       const float* beta, hipStream_t st) {
   pced_status r = check_ctx(c, false);
   if (r != PCED_OK) return r;
   const pced_config& cfg = c->cfg;
   if (n_queries < 1 || n_queries > cfg.max_queries)
     return fail(PCED_ERR_INVALID_ARG, "n_queries %d not in [1, %d]", n_queries, cfg.max_queries);
-  if (!n_experts || !cache_len || !src_k || !src_v || !k_pool || !v_pool || !relevance)
+  if (!n_experts || !cache_len || !src_k || !src_v || !to.k_pool || !to.v_pool || !relevance)
     return fail(PCED_ERR_INVALID_ARG, "NULL argument");
   if (!std::isfinite(gamma)) return fail(PCED_ERR_INVALID_ARG, "gamma is not finite");
   if (reserve_tokens < 0) return fail(PCED_ERR_INVALID_ARG, "reserve_tokens < 0");
@@ -1377,19 +1316,19 @@ pced_status pced_load_caches(pced_ctx* c, int32_t n_queries, const int32_t* n_ex
   la.items = c->at<int32_t>(L.load_items);
   la.len0 = c->at<int32_t>(L.len0);
   la.page_table = c->at<int32_t>(L.page_table);
-  la.kpool = k_pool;
-  la.vpool = v_pool;
+  la.kpool = to.k_pool;
+  la.vpool = to.v_pool;
   la.n_layers = cfg.n_layers;
   la.n_kv_heads = cfg.n_kv_heads;
   la.head_dim = cfg.head_dim;
   la.max_pages = cfg.max_pages;
   la.maxpps = P;
-  if (!items.empty()) HIP_OK(launch_load(la, (int)(items.size() / 2), c->bf16, st));
+  if (!items.empty()) HIP_OK(to.launch(la, to, (int)(items.size() / 2), c->bf16, st));
   bool any_host = false;
   for (long s = 0; s < S; ++s) {
     if (!on_host[s]) continue;
     any_host = true;
-    r = load_from_host(c, la, (int)s, cache_len[s], (const char*)src_k[s], (const char*)src_v[s], st);
+    r = load_from_host(c, la, to, (int)s, cache_len[s], (const char*)src_k[s], (const char*)src_v[s], st);
     if (r != PCED_OK) {  // the host buffers are the caller's again: earlier copies may still be reading them
       (void)hipStreamSynchronize(st);
       return r;
@@ -1397,19 +1336,101 @@ pced_status pced_load_caches(pced_ctx* c, int32_t n_queries, const int32_t* n_ex
   }
   if (any_host) HIP_OK(hipStreamSynchronize(st));  // the host buffers have been read
 
-  c->kpool = k_pool;
-  c->vpool = v_pool;
+  c->kpool = to.k_pool;
+  c->vpool = to.v_pool;
+  c->c8 = to.c8;
+  c->max_new = to.max_new;
   c->dynamic_beta = beta == nullptr;
   c->beta_frozen = false;
   c->t = 0;
   c->loaded = true;
   return PCED_OK;
 }
+}  // namespace pced
+
+extern "C" {
+
+size_t pced_pool_bytes(const pced_config* cfg) {
+  if (!cfg_valid(cfg, nullptr)) return 0;
+  return (size_t)cfg->n_layers * cfg->max_pages * cfg->n_kv_heads * kPage * cfg->head_dim * esize_of(*cfg);
+}
+
+size_t pced_lm_head_bytes(const pced_config* cfg) {
+  if (!cfg_valid(cfg, nullptr)) return 0;
+  if (cfg->dtype == PCED_BF16) return (size_t)ceil_div(cfg->vocab, 16) * 16 * cfg->hidden * 2;
+  return (size_t)cfg->vocab * cfg->hidden * 4;
+}
+
+pced_status pced_pack_lm_head(const pced_config* cfg, const void* w, void* w_packed, hipStream_t st) {
+  std::string why;
+  if (!cfg_valid(cfg, &why)) return fail(PCED_ERR_INVALID_ARG, "invalid config: %s", why.c_str());
+  if (!w || !w_packed) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
+  const char* a = (const char*)w;
+  const char* b = (const char*)w_packed;
+  const size_t na = (size_t)cfg->vocab * cfg->hidden * esize_of(*cfg), nb = pced_lm_head_bytes(cfg);
+  if (a < b + nb && b < a + na) return fail(PCED_ERR_INVALID_ARG, "w and w_packed overlap");
+  HIP_OK(launch_pack_lm_head(w, w_packed, cfg->vocab, cfg->hidden, cfg->dtype == PCED_BF16, st));
+  return PCED_OK;
+}
+
+size_t pced_workspace_bytes(const pced_config* cfg) {
+  if (!cfg_valid(cfg, nullptr)) return 0;
+  return make_layout(*cfg).total;
+}
+
+const char* pced_last_error(void) { return g_err.c_str(); }
+
+pced_status pced_create(const pced_config* cfg, void* d_workspace, size_t ws_bytes, pced_ctx** out) {
+  std::string why;
+  if (!out) return fail(PCED_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  if (!cfg_valid(cfg, &why)) return fail(PCED_ERR_INVALID_ARG, "invalid config: %s", why.c_str());
+  if (!d_workspace) return fail(PCED_ERR_INVALID_ARG, "workspace is NULL");
+  if ((uintptr_t)d_workspace % kAlign) return fail(PCED_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  const Layout lay = make_layout(*cfg);
+  if (ws_bytes < lay.total)
+    return fail(PCED_ERR_CAPACITY, "workspace too small: %zu < %zu bytes", ws_bytes, lay.total);
+  pced_ctx* c = new pced_ctx();
+  c->cfg = *cfg;
+  c->lay = lay;
+  c->ws = (char*)d_workspace;
+  c->bf16 = cfg->dtype == PCED_BF16;
+  c->G = cfg->n_q_heads / cfg->n_kv_heads;
+  c->appended.assign(cfg->n_layers, 0);
+  c->ahead.assign(cfg->n_layers, 0);
+  c->behind.assign(cfg->n_layers, kNotCovered);
+  *out = c;
+  return PCED_OK;
+}
+
+void pced_destroy(pced_ctx* ctx) {
+  if (!ctx) return;
+  for (auto& r : ctx->recs) {
+    (void)hipEventDestroy(r.a);
+    (void)hipEventDestroy(r.b);
+  }
+  for (auto e : ctx->ev_free) (void)hipEventDestroy(e);
+  if (ctx->blas) rocblas_destroy_handle(ctx->blas);
+  delete ctx;
+}
+
+pced_status pced_load_caches(pced_ctx* c, int32_t n_queries, const int32_t* n_experts,
+                             const int32_t* cache_len, const void* const* src_k,
+                             const void* const* src_v, void* k_pool, void* v_pool,
+                             const int32_t* page_table, int32_t reserve_tokens,
+                             const float* relevance, float gamma, const float* beta,
+                             hipStream_t st) {
+  const LoadTarget to{k_pool, v_pool, {}, 0, [](const LoadArgs& a, const LoadTarget&, int n_items, bool bf16, hipStream_t s) {
+                        return launch_load(a, n_items, bf16, s);
+                      }};
+  return load_batch(c, n_queries, n_experts, cache_len, src_k, src_v, to, page_table, reserve_tokens, relevance, gamma,
+                    beta, st);
+}
 
 pced_status pced_step(pced_ctx* c, const void* q, const void* k_new, const void* v_new,
                       const void* lm_head, int32_t* tokens_out, const pced_step_out* extra,
                       hipStream_t st) {
-  pced_status r = check_ctx(c, true);
+  pced_status r = check_pools(c);
   if (r != PCED_OK) return r;
   if (!q || !k_new || !v_new || !lm_head || !tokens_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
   // the kernels read q, k_new and v_new in 16-byte units
@@ -1420,7 +1441,7 @@ pced_status pced_step(pced_ctx* c, const void* q, const void* k_new, const void*
 
 pced_status pced_generate(pced_ctx* c, int32_t n_steps, const pced_synth* synth, const void* lm_head,
                           int32_t* tokens_out, const pced_step_out* last_extra, hipStream_t st) {
-  pced_status r = check_ctx(c, true);
+  pced_status r = check_pools(c);
   if (r != PCED_OK) return r;
   if (!synth || !lm_head || !tokens_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
   if (n_steps < 1) return fail(PCED_ERR_INVALID_ARG, "n_steps < 1");
@@ -1693,7 +1714,7 @@ pced_status pced_relevance(int32_t mode, int32_t n, const float* retrieval, cons
 
 pced_status pced_read_cache(pced_ctx* c, int32_t seq, int32_t layer, int32_t start, int32_t count, void* k_out,
                             void* v_out, hipStream_t st) {
-  pced_status r = check_ctx(c, true);
+  pced_status r = check_pools(c);
   if (r != PCED_OK) return r;
   if (!k_out || !v_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
   if (seq < 0 || seq >= c->S) return fail(PCED_ERR_INVALID_ARG, "seq %d not in [0, %d)", seq, c->S);

@@ -1,0 +1,236 @@
+// Host side of caches held in 8 bits: loading, append, attention, reading back. See
+// include/pced.h.
+#include "pced_host.h"
+
+#include <algorithm>
+#include <cmath>
+
+using namespace pced;
+
+namespace {
+
+// Pages that n new tokens touch, at most: one open place each
+int ring_of(int n) { return (int)(((long)n + kPage - 2) / kPage) + 1; }
+
+size_t code_bytes(const pced_config& c) {
+  return (size_t)c.n_layers * c.max_pages * c.n_kv_heads * kPage * c.head_dim;
+}
+
+pced_status check_cache8(const pced_ctx* c, const pced_cache8* m) {
+  const pced_config& cfg = c->cfg;
+  if (!m) return fail(PCED_ERR_INVALID_ARG, "cache is NULL");
+  if (!c->bf16) return fail(PCED_ERR_UNSUPPORTED, "caches in 8 bits need a bf16 context");
+  if (m->code != PCED_CODE_E4M3 && m->code != PCED_CODE_INT8) return fail(PCED_ERR_INVALID_ARG, "unknown code %d", m->code);
+  if (m->max_new < 1 || m->max_new > 1 << 20) return fail(PCED_ERR_INVALID_ARG, "max_new %d: 1 .. 2^20", m->max_new);
+  if ((long)cfg.max_seqs * ring_of(m->max_new) > 0x7FFFFFFF)  // (places of open pages are 32-bit)
+    return fail(PCED_ERR_INVALID_ARG, "max_new %d for %d sequences: too many open pages", m->max_new, cfg.max_seqs);
+  const void* at[5] = {m->k_codes, m->v_codes, m->scales, m->k_open, m->v_open};
+  const size_t n[5] = {pced_codes_bytes(&cfg), pced_codes_bytes(&cfg), pced_scales_bytes(&cfg),
+                       pced_open_bytes(&cfg, m->max_new), pced_open_bytes(&cfg, m->max_new)};
+  for (int i = 0; i < 5; ++i) {
+    if (!at[i]) return fail(PCED_ERR_INVALID_ARG, "NULL buffer in cache");
+    if ((uintptr_t)at[i] % kAlign) return fail(PCED_ERR_INVALID_ARG, "cache's buffers must be 256-byte aligned");
+    for (int j = 0; j < i; ++j)
+      if (ranges_meet(at[i], n[i], at[j], n[j])) return fail(PCED_ERR_INVALID_ARG, "cache's buffers overlap");
+  }
+  return PCED_OK;
+}
+
+pced_status check_loaded8(const pced_ctx* c) {
+  const pced_status r = check_ctx(c, true);
+  if (r == PCED_OK && !c->c8.code) return fail(PCED_ERR_STATE, "the batch's caches are not in 8 bits (call pced_load_codes)");
+  return r;
+}
+
+pced_status check_new(const pced_ctx* c, int n_tokens) {
+  if (n_tokens > c->max_new) return fail(PCED_ERR_CAPACITY, "%d tokens > max_new %d", n_tokens, c->max_new);
+  return PCED_OK;
+}
+
+// How a launch of pced_attend_codes divides its work (see attend_plan): parts of the items' pages,
+// and the workspace that their states take.
+struct Plan8 {
+  int parts, part_pages;
+  size_t ml, bytes;
+};
+Plan8 plan8(const pced_ctx* c, const Attend8Args& a, int max_pages, int groups, int layers, int min_part) {
+  Plan8 p{};
+  const size_t items = (size_t)groups * layers * a.n_kv_heads, cols = (size_t)a.gt * a.group;
+  const size_t want = std::max<size_t>(1, 2 * (size_t)c->num_cus / items);
+  p.part_pages = std::min(std::max<int>({min_part, ceil_div(ceil_div(max_pages, (long)want), 8) * 8, 8}), kAttendPart);
+  p.parts = ceil_div(max_pages, p.part_pages);
+  if (p.parts > 1) {
+    p.ml = align_up(items * p.parts * cols * a.head_dim * 4);
+    p.bytes = p.ml + align_up(items * p.parts * cols * 8);
+  }
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pced_codes_bytes(const pced_config* cfg) {
+  if (!cfg_valid(cfg, nullptr) || cfg->dtype != PCED_BF16) return 0;
+  return code_bytes(*cfg);
+}
+
+size_t pced_scales_bytes(const pced_config* cfg) {
+  if (!cfg_valid(cfg, nullptr) || cfg->dtype != PCED_BF16) return 0;
+  return (size_t)cfg->n_layers * cfg->n_kv_heads * cfg->max_pages * 4;
+}
+
+size_t pced_open_bytes(const pced_config* cfg, int32_t max_new) {
+  if (!cfg_valid(cfg, nullptr) || cfg->dtype != PCED_BF16 || max_new < 1) return 0;
+  return (size_t)cfg->n_layers * cfg->max_seqs * ring_of(max_new) * cfg->n_kv_heads * kPage * cfg->head_dim * 2;
+}
+
+pced_status pced_load_codes(pced_ctx* c, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
+                       const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
+                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                       const float* beta, hipStream_t st) {
+  pced_status r = check_ctx(c, false);
+  if (r == PCED_OK) r = check_cache8(c, cache);
+  if (r != PCED_OK) return r;
+  LoadTarget to{cache->k_codes, cache->v_codes, {}, cache->max_new,
+                [](const LoadArgs& a, const LoadTarget& t, int n_items, bool, hipStream_t s) {
+                  return launch_load8(a, t.c8, n_items, s);
+                }};
+  to.c8.k_codes = (uint8_t*)cache->k_codes;
+  to.c8.v_codes = (uint8_t*)cache->v_codes;
+  to.c8.scales = (uint32_t*)cache->scales;
+  to.c8.k_open = (uint16_t*)cache->k_open;
+  to.c8.v_open = (uint16_t*)cache->v_open;
+  to.c8.code = cache->code;
+  to.c8.ring = ring_of(cache->max_new);
+  to.c8.open_pages = c->cfg.max_seqs * to.c8.ring;
+  to.c8.max_pages = c->cfg.max_pages;
+  return load_batch(c, n_queries, n_experts, cache_len, src_k, src_v, to, page_table, reserve_tokens, relevance, gamma,
+                    beta, st);
+}
+
+pced_status pced_append_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
+                         const pced_rope* rope, void* q_out, hipStream_t st) {
+  pced_status r = check_loaded8(c);
+  if (r != PCED_OK) return r;
+  AppendRowsArgs a{};
+  r = append_args(c, layer, n_layers, n_tokens, rows, rope, q_out, &a);
+  if (r == PCED_OK) r = check_new(c, n_tokens);
+  if (r != PCED_OK) return r;
+  const pced_config& cfg = c->cfg;
+  a.kpool = c->c8.k_open;
+  a.vpool = c->c8.v_open;
+  a.max_pages = c->c8.open_pages;
+  {
+    const double heads = (rows->q ? cfg.n_q_heads : 0) + 2.0 * cfg.n_kv_heads;
+    ProfScope ps(c, PCED_PROF_APPEND, 4.0 * c->S * n_tokens * n_layers * heads * cfg.head_dim, 0);
+    HIP_OK(launch_append8(a, c->c8, st, ps.timing()));
+  }
+  for (int l = layer; l < layer + n_layers; ++l) {
+    c->appended[l] = n_tokens;
+    c->ahead[l] = 0;
+  }
+  return PCED_OK;
+}
+
+pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q, void* x_out,
+                         hipStream_t st) {
+  pced_status r = check_loaded8(c);
+  if (r == PCED_OK) r = check_layers(c, layer, n_layers, n_tokens);
+  if (r == PCED_OK) r = check_new(c, n_tokens);
+  if (r != PCED_OK) return r;
+  const pced_config& cfg = c->cfg;
+  if (!q || !x_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
+  if (((uintptr_t)q | (uintptr_t)x_out) % 16) return fail(PCED_ERR_INVALID_ARG, "q and x_out must be 16-byte aligned");
+  const size_t bytes = (size_t)c->S * n_tokens * n_layers * cfg.hidden * 2;
+  if (ranges_meet(q, bytes, x_out, bytes)) return fail(PCED_ERR_INVALID_ARG, "q and x_out overlap");
+  for (int l = layer; l < layer + n_layers; ++l)
+    if (c->appended[l] < n_tokens)
+      return fail(PCED_ERR_STATE, "layer %d has %d appended tokens, not %d", l, c->appended[l], n_tokens);
+  Attend8Args a{};
+  a.c = c->c8;
+  a.q = q;
+  a.x_out = x_out;
+  a.len0 = c->at<int32_t>(c->lay.len0);
+  a.page_table = c->at<int32_t>(c->lay.page_table);
+  a.t = c->t;
+  a.n_tokens = n_tokens;
+  a.layer0 = layer;
+  a.n_layers = n_layers;
+  a.n_q_heads = cfg.n_q_heads;
+  a.n_kv_heads = cfg.n_kv_heads;
+  a.group = c->G;
+  a.head_dim = cfg.head_dim;
+  a.maxpps = cfg.max_pages_per_seq;
+  a.tiles = n_tokens * c->G <= 16 ? 1 : 2;
+  const int most = 16 * a.tiles / c->G;  // tokens that the tiles hold
+  a.seq_groups = ceil_div(n_tokens, most);
+  a.gt = ceil_div(n_tokens, a.seq_groups);
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cfg.head_dim));
+  a.lead = 8.f / a.scale_log2;
+  int max_pages = 0;
+  for (int s = 0; s < c->S; ++s) max_pages = std::max(max_pages, (c->len[s] + n_tokens - 1) / kPage + 1);
+  // as many layers and groups per launch as the workspace takes
+  const int all = c->S * a.seq_groups;
+  int groups = all, layers = n_layers, min_part = 8;
+  Plan8 p = plan8(c, a, max_pages, groups, layers, min_part);
+  while (p.bytes > c->lay.part_acc_bytes) {
+    if (layers > 1) layers = (layers + 1) / 2;
+    else if (groups > 1) groups = (groups + 1) / 2;
+    else if (p.parts > 1 && p.part_pages < kAttendPart) min_part = 2 * p.part_pages;
+    else return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
+    p = plan8(c, a, max_pages, groups, layers, min_part);
+  }
+  char* ws = c->at<char>(c->lay.part_acc);
+  a.part_acc = (float*)ws;
+  a.part_ml = (float*)(ws + p.ml);
+  a.parts = p.parts;
+  a.part_pages = p.part_pages;
+  double tokens = 0;  // seen, per layer and kv-head
+  for (int s = 0; c->prof && s < c->S; ++s) tokens += c->len[s] + n_tokens;
+  for (int l = 0; l < n_layers; l += layers) {
+    a.layer = layer + l;
+    a.launch_layers = std::min(layers, n_layers - l);
+    for (int g = 0; g < all; g += groups) {
+      a.group0 = g;
+      a.n_groups = std::min(groups, all - g);
+      const double part = tokens * a.n_groups / all * a.launch_layers * cfg.n_kv_heads * cfg.head_dim;
+      ProfScope ps(c, PCED_PROF_ATTN, part * 2, part * 4 * c->G * n_tokens);
+      ProfScope pm(c, PCED_PROF_COMBINE, 0, 0);
+      if (p.parts == 1) pm.drop();
+      HIP_OK(launch_attend8(a, st, ps.timing(), pm.timing()));
+    }
+  }
+  return PCED_OK;
+}
+
+pced_status pced_read_codes(pced_ctx* c, int32_t seq, int32_t layer, int32_t start, int32_t count, void* k_out, void* v_out,
+                       hipStream_t st) {
+  pced_status r = check_loaded8(c);
+  if (r != PCED_OK) return r;
+  if (seq < 0 || seq >= c->S) return fail(PCED_ERR_INVALID_ARG, "seq %d not in [0, %d)", seq, c->S);
+  if (layer < 0 || layer >= c->cfg.n_layers)
+    return fail(PCED_ERR_INVALID_ARG, "layer %d not in [0, %d)", layer, c->cfg.n_layers);
+  if (start < 0 || count < 0 || (long)start + count > c->len[seq])
+    return fail(PCED_ERR_INVALID_ARG, "tokens [%d, %ld) beyond the %d of sequence %d", start, (long)start + count,
+                c->len[seq], seq);
+  if (count == 0) return PCED_OK;
+  if (!k_out || !v_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
+  ReadCacheArgs a{};
+  a.page_table = c->at<int32_t>(c->lay.page_table);
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.seq = seq;
+  a.layer = layer;
+  a.start = start;
+  a.count = count;
+  a.n_kv_heads = c->cfg.n_kv_heads;
+  a.head_dim = c->cfg.head_dim;
+  a.max_pages = c->cfg.max_pages;
+  a.maxpps = c->cfg.max_pages_per_seq;
+  a.bf16 = 1;
+  HIP_OK(launch_read8(a, c->c8, c->len[seq], st));
+  return PCED_OK;
+}
+
+}  // extern "C"

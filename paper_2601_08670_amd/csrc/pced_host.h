@@ -74,6 +74,9 @@ struct pced_ctx {
   char* summary = nullptr;
   void* kpool = nullptr;
   void* vpool = nullptr;
+  // a batch loaded by pced_load_codes (code 0: by pced_load_caches)
+  pced::Cache8Args c8{};
+  int max_new = 0;
   std::vector<char> staging;
   int num_cus = 0;
   int attn_waves_per_cu = 8;
@@ -139,6 +142,27 @@ struct ProfScope {
 bool cfg_valid(const pced_config* c, std::string* why);
 pced_status check_ctx(const pced_ctx* c, bool need_loaded);
 pced_status check_room(const pced_ctx* c, int n_tokens);
+// A loaded batch whose caches are in the pools, for the calls that read or write them there.
+pced_status check_pools(const pced_ctx* c);
+// The layers and tokens of a layer-wise call.
+pced_status check_layers(const pced_ctx* c, int layer, int n_layers, int n_tokens);
+bool ranges_meet(const void* a, size_t na, const void* b, size_t nb);
+// pced_append's checks of its arguments, and the kernel's arguments but for the pages.
+pced_status append_args(const pced_ctx* c, int layer, int n_layers, int n_tokens, const pced_rows* rows,
+                        const pced_rope* rope, void* q_out, AppendRowsArgs* out);
+
+// Where a load puts the caches: the pools, or (c8.code != 0) a cache in 8 bits; `launch` moves pages there.
+struct LoadTarget {
+  void* k_pool;
+  void* v_pool;
+  Cache8Args c8;
+  int max_new;
+  hipError_t (*launch)(const LoadArgs& a, const LoadTarget& to, int n_items, bool bf16, hipStream_t st);
+};
+pced_status load_batch(pced_ctx* c, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
+                       const void* const* src_k, const void* const* src_v, const LoadTarget& to,
+                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                       const float* beta, hipStream_t st);
 
 // The lengths grow by n tokens. by_rows: tokens that pced_append wrote (the
 // summaries cover what they covered of them); otherwise other calls wrote them.

@@ -347,6 +347,34 @@ struct AppendRowsArgs {
   int rot_dim, halves;
   double log2_theta;
 };
+// A batch's caches in 8 bits (see pced_cache8): codes and scales of complete pages by physical
+// page, the pages behind in 16 bits by place: page p of sequence s at s * ring + p % ring.
+struct Cache8Args {
+  uint8_t* k_codes;         // [L][max_pages][Hkv][16 D]
+  uint8_t* v_codes;
+  uint32_t* scales;         // [L][Hkv][max_pages]: K's in the low half, V's in the high one (bf16)
+  uint16_t* k_open;         // [L][open_pages][Hkv][16 D]
+  uint16_t* v_open;
+  int code, ring, open_pages, max_pages;
+};
+// Attention of new tokens over caches in 8 bits (see pced_attend_codes). An item is a group of gt
+// consecutive new tokens of a sequence (seq_groups of them per sequence), a layer and a kv-head; a launch takes
+// n_groups groups from group0 on and launch_layers layers from `layer` on.
+struct Attend8Args {
+  Cache8Args c;
+  const void* q;            // [S * n_tokens][n_layers][Hq][D]
+  void* x_out;              // [S * n_tokens][n_layers][Hq][D]
+  const int32_t* len0;
+  const int32_t* page_table;
+  float* part_acc;          // [item][parts][gt * G][D]
+  float* part_ml;           // [item][parts][gt * G][2]
+  int t, n_tokens, gt, seq_groups, group0, n_groups, layer0, n_layers, layer, launch_layers;
+  int n_q_heads, n_kv_heads, group, head_dim, maxpps, tiles;  // tiles: 16-column tiles of a group's query rows
+  int parts, part_pages;    // parts of an item's pages, and pages per part
+  int launch_seqs;          // sequences of the launch's groups (set by launch_attend8)
+  float scale_log2;         // log2(e) / sqrt(D)
+  float lead;               // difference of scores that makes a weight of 2^8
+};
 // Summaries of the complete pages of every sequence from token len - behind on, all layers.
 struct SummaryArgs {
   const void* kpool;
@@ -459,6 +487,12 @@ hipError_t launch_summarize(const SummaryArgs& a, bool bf16, hipStream_t st);
 hipError_t launch_page_select(const AttendArgs& a, bool score, hipStream_t st, const Timing* tm = nullptr);
 // pick: the lists are chosen by the same launch (n_tokens and parts 1, at most kPickPages pages)
 hipError_t launch_attend(const AttendArgs& a, bool pick, hipStream_t st, const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
+// pced_cache8.hip: caches in 8 bits. launch_load8: as launch_load, complete pages encoded.
+hipError_t launch_load8(const LoadArgs& a, const Cache8Args& c, int n_items, hipStream_t st);
+hipError_t launch_attend8(const Attend8Args& a, hipStream_t st, const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
+hipError_t launch_read8(const ReadCacheArgs& a, const Cache8Args& c, int len, hipStream_t st);
+// pced_layer.hip: launch_append_rows into the open pages (a's pools), pages that become full encoded
+hipError_t launch_append8(const AppendRowsArgs& a, const Cache8Args& c, hipStream_t st, const Timing* tm = nullptr);
 // RoPE table of GemmArgs::rope for positions 0 .. positions - 1, in fp64 rounded to fp32
 hipError_t launch_rope_table(float2* out, int positions, int head_dim, double log2_theta, hipStream_t st);
 

@@ -1,7 +1,10 @@
 // gfx950 kernels of the layer-wise calls: append of new rows with rotation, 8-bit
 // page summaries, the choice of pages from them, and attention over the chosen
 // pages. Tile layouts: see pced_kernels.hip.
+#include "pced_code8.h"
 #include "pced_device.h"
+
+#include <type_traits>
 
 namespace pced {
 namespace {
@@ -201,9 +204,11 @@ __device__ __forceinline__ void turn_slot(const Slot<BF16>& sl, const float2* cs
 // tokens (64 of 33 sequences, 32/8 heads of 128: 15.8 us for 52 MB, 3.3 TB/s; reads and
 // writes in turn reach 5.1), the chain of length, rows and stores for one (eight layers
 // of 33 sequences 6.8 us, one of five 3.6).
+// With CODE the pages are those behind the complete ones of a cache in 8 bits (c: places in a
+// ring per sequence), and K's and V's block of a page that becomes full encode it.
 constexpr int kAppendTasks = 1024;
-template <bool BF16>
-__global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
+template <bool BF16, int CODE>
+__device__ __forceinline__ void append_rows(const AppendRowsArgs& a, const Cache8Args& c) {
   constexpr int N = Unit<BF16>::N, es = BF16 ? 2 : 4;
   __shared__ union {
     struct {
@@ -278,9 +283,36 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
     return;
   }
 
-  const int phys = a.page_table[(size_t)s * a.maxpps + p];
+  const int phys = CODE ? s * c.ring + p % c.ring : a.page_table[(size_t)s * a.maxpps + p];
   const size_t tile = (size_t)kPage * D;
   const size_t tile0 = ((size_t)(a.layer0 + l) * a.max_pages + phys) * Hkv;
+  // the full page's codes, from the block's own stores
+  auto encode = [&] {
+    if constexpr (CODE != 0) {
+      if (t1 < kPage) return;
+      const int cp = a.page_table[(size_t)s * a.maxpps + p];
+      __syncthreads();
+      for (int h = tid >> 6; h < Hkv; h += 4) {
+        const size_t at = ((size_t)(a.layer0 + l) * c.max_pages + cp) * Hkv + h;
+        const u32x4* in = (const u32x4*)((const uint16_t*)(z == 1 ? a.vpool : a.kpool) + (tile0 + h) * tile) + (tid & 63);
+        u32x4* out = (u32x4*)((z == 1 ? c.v_codes : c.k_codes) + at * tile) + (tid & 63);
+        uint32_t sc;
+        auto run = [&](auto units) {
+          constexpr int NU = decltype(units)::value;
+          u32x4 u[NU], w[NU / 2];
+#pragma unroll
+          for (int i = 0; i < NU; ++i) u[i] = in[64 * i];
+          encode_tile<CODE, NU>(u, w, &sc);
+#pragma unroll
+          for (int i = 0; i < NU / 2; ++i) out[64 * i] = w[i];
+        };
+        if (D == 128) run(std::integral_constant<int, 4>{});
+        else run(std::integral_constant<int, 2>{});
+        if ((tid & 63) == 0)
+          ((uint16_t*)(c.scales + ((size_t)(a.layer0 + l) * Hkv + h) * c.max_pages + cp))[z] = (uint16_t)sc;
+      }
+    }
+  };
   if constexpr (BF16) {
     if (z == 1) {
       const int runs = D / 16;  // of a kv-head's token quad
@@ -313,6 +345,7 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
           }
           wave_lds_sync();
         }
+        encode();
         return;
       }
       // runs of 128 bytes, four tokens of dims d0 .. d0 + 7 and d0 + 16 .. d0 + 23
@@ -343,6 +376,7 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) __builtin_nontemporal_store(cur[i], run + i);
       }
+      encode();
       return;
     }
     if (n == kPage) {
@@ -441,6 +475,10 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
       if (sl.d2 >= 0) *(u32x4*)(out + sl.d2) = o2;
     }
   }
+  if constexpr (CODE != 0) {
+    encode();
+    return;
+  }
   if (a.codes && t1 == kPage) {
     __syncthreads();  // the block's own stores of the page's keys are read back
     for (int h = tid >> 6; h < Hkv; h += 4) {
@@ -450,6 +488,11 @@ __global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) {
     }
   }
 }
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_append_rows(AppendRowsArgs a) { append_rows<BF16, 0>(a, Cache8Args{}); }
+template <int CODE>
+__global__ __launch_bounds__(256) void k_append8(AppendRowsArgs a, Cache8Args c) { append_rows<true, CODE>(a, c); }
 
 // ------------------------------------------------------------- page selection
 
@@ -1411,16 +1454,32 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a) {
 
 // ------------------------------------------------------------------ launchers
 
-hipError_t launch_append_rows(const AppendRowsArgs& a0, bool bf16, hipStream_t st, const Timing* tm) {
-  AppendRowsArgs a = a0;
+namespace {
+template <class F>
+hipError_t append_grid(AppendRowsArgs& a, bool bf16, F&& run) {
   const int unit = bf16 ? 8 : 4, nslot = (a.head_dim - (a.halves ? a.rot_dim / 2 : 0)) / unit;
   const int tasks = (a.n_tokens < kPage ? a.n_tokens : kPage) * a.n_q_heads * nslot;  // of a page, at most
   a.q_blocks = a.q ? (tasks + kAppendTasks - 1) / kAppendTasks : 0;
   const size_t blocks = (size_t)a.n_seqs * a.slots * a.n_layers * (2 + a.q_blocks);
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks);
-  if (bf16) return go(k_append_rows<true>, grid, dim3(256), 0, st, t0(tm), t1(tm), a);
-  return go(k_append_rows<false>, grid, dim3(256), 0, st, t0(tm), t1(tm), a);
+  return run(dim3((unsigned)blocks));
+}
+}  // namespace
+
+hipError_t launch_append_rows(const AppendRowsArgs& a0, bool bf16, hipStream_t st, const Timing* tm) {
+  AppendRowsArgs a = a0;
+  return append_grid(a, bf16, [&](dim3 grid) {
+    if (bf16) return go(k_append_rows<true>, grid, dim3(256), 0, st, t0(tm), t1(tm), a);
+    return go(k_append_rows<false>, grid, dim3(256), 0, st, t0(tm), t1(tm), a);
+  });
+}
+
+hipError_t launch_append8(const AppendRowsArgs& a0, const Cache8Args& c, hipStream_t st, const Timing* tm) {
+  AppendRowsArgs a = a0;
+  return append_grid(a, true, [&](dim3 grid) {
+    if (c.code == kE4m3) return go(k_append8<kE4m3>, grid, dim3(256), 0, st, t0(tm), t1(tm), a, c);
+    return go(k_append8<kInt8>, grid, dim3(256), 0, st, t0(tm), t1(tm), a, c);
+  });
 }
 
 hipError_t launch_summarize(const SummaryArgs& a, bool bf16, hipStream_t st) {

@@ -7,13 +7,12 @@
 
 using namespace pced;
 
-namespace {
+namespace pced {
 
 bool ranges_meet(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
-// The layers and tokens of a layer-wise call
 pced_status check_layers(const pced_ctx* c, int layer, int n_layers, int n_tokens) {
   pced_status r = check_ctx(c, true);
   if (r != PCED_OK) return r;
@@ -24,6 +23,70 @@ pced_status check_layers(const pced_ctx* c, int layer, int n_layers, int n_token
     return fail(PCED_ERR_CAPACITY, "%d tokens > max_pages_per_seq", n_tokens);
   return check_room(c, n_tokens);
 }
+
+pced_status append_args(const pced_ctx* c, int layer, int n_layers, int n_tokens, const pced_rows* rows,
+                        const pced_rope* rope, void* q_out, AppendRowsArgs* out) {
+  pced_status r = check_layers(c, layer, n_layers, n_tokens);
+  if (r != PCED_OK) return r;
+  const pced_config& cfg = c->cfg;
+  if (!rows || !rows->k || !rows->v) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
+  if (!rows->q != !q_out) return fail(PCED_ERR_INVALID_ARG, "q rows without q_out, or q_out without q rows");
+  const size_t es = esize_of(cfg), D = cfg.head_dim, R = (size_t)c->S * n_tokens;
+  const int64_t qd = (int64_t)n_layers * cfg.n_q_heads * D, kd = (int64_t)n_layers * cfg.n_kv_heads * D;
+  AppendRowsArgs a{};
+  a.q = rows->q;
+  a.k = rows->k;
+  a.v = rows->v;
+  a.q_out = q_out;
+  a.q_row = rows->q && rows->q_row ? rows->q_row : qd;
+  a.k_row = rows->k_row ? rows->k_row : kd;
+  a.v_row = rows->v_row ? rows->v_row : kd;
+  if (a.q_row < qd || a.k_row < kd || a.v_row < kd)
+    return fail(PCED_ERR_INVALID_ARG, "rows overlap: distances %lld, %lld, %lld", (long long)a.q_row, (long long)a.k_row,
+                (long long)a.v_row);
+  // the kernel moves rows in 16-byte units
+  if (((uintptr_t)rows->q | (uintptr_t)rows->k | (uintptr_t)rows->v | (uintptr_t)q_out) % 16 ||
+      (size_t)a.q_row * es % 16 || (size_t)a.k_row * es % 16 || (size_t)a.v_row * es % 16)
+    return fail(PCED_ERR_INVALID_ARG, "rows and q_out must be 16-byte aligned, and the rows' distances too");
+  if (q_out) {
+    const size_t nq = ((R - 1) * a.q_row + qd) * es, nk = ((R - 1) * a.k_row + kd) * es, nv = ((R - 1) * a.v_row + kd) * es;
+    const bool in_place = q_out == rows->q && a.q_row == qd;
+    if ((!in_place && ranges_meet(q_out, R * qd * es, rows->q, nq)) || ranges_meet(q_out, R * qd * es, rows->k, nk) ||
+        ranges_meet(q_out, R * qd * es, rows->v, nv))
+      return fail(PCED_ERR_INVALID_ARG, "q_out overlaps the rows");
+  }
+  if (rope) {
+    const int unit = c->bf16 ? 16 : 8;
+    if (!(rope->theta > 1.0) || !std::isfinite(rope->theta)) return fail(PCED_ERR_INVALID_ARG, "rope theta must be > 1");
+    if (rope->rot_dim < 0 || rope->rot_dim > cfg.head_dim || rope->rot_dim % 2)
+      return fail(PCED_ERR_INVALID_ARG, "rot_dim %d: even, 0 .. %d", rope->rot_dim, cfg.head_dim);
+    if (rope->halves != 0 && rope->halves != 1) return fail(PCED_ERR_INVALID_ARG, "halves must be 0 or 1");
+    if (rope->halves && rope->rot_dim % unit)
+      return fail(PCED_ERR_INVALID_ARG, "rot_dim %d: a multiple of %d with halves", rope->rot_dim, unit);
+    a.rot_dim = rope->rot_dim;
+    a.halves = rope->halves;
+    a.log2_theta = std::log2(rope->theta);
+  }
+  a.len0 = (const int32_t*)(c->ws + c->lay.len0);
+  a.page_table = (const int32_t*)(c->ws + c->lay.page_table);
+  a.n_seqs = c->S;
+  a.n_tokens = n_tokens;
+  a.layer0 = layer;
+  a.n_layers = n_layers;
+  a.n_q_heads = cfg.n_q_heads;
+  a.n_kv_heads = cfg.n_kv_heads;
+  a.head_dim = cfg.head_dim;
+  a.max_pages = cfg.max_pages;
+  a.maxpps = cfg.max_pages_per_seq;
+  a.t = c->t;
+  a.sum_row = summary_row(cfg.head_dim);
+  for (int s = 0; s < c->S; ++s)
+    a.slots = std::max(a.slots, (c->len[s] + n_tokens - 1) / kPage - c->len[s] / kPage + 1);
+  *out = a;
+  return PCED_OK;
+}
+}  // namespace pced
+namespace {
 
 size_t summary_codes(const pced_config& c) {
   return align_up((size_t)c.n_layers * c.n_kv_heads * c.max_pages * summary_row(c.head_dim));
@@ -161,64 +224,14 @@ extern "C" {
 
 pced_status pced_append(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
                         const pced_rope* rope, void* q_out, hipStream_t st) {
-  pced_status r = check_layers(c, layer, n_layers, n_tokens);
+  pced_status r = check_pools(c);
+  if (r != PCED_OK) return r;
+  AppendRowsArgs a{};
+  r = append_args(c, layer, n_layers, n_tokens, rows, rope, q_out, &a);
   if (r != PCED_OK) return r;
   const pced_config& cfg = c->cfg;
-  if (!rows || !rows->k || !rows->v) return fail(PCED_ERR_INVALID_ARG, "NULL argument");
-  if (!rows->q != !q_out) return fail(PCED_ERR_INVALID_ARG, "q rows without q_out, or q_out without q rows");
-  const size_t es = esize_of(cfg), D = cfg.head_dim, R = (size_t)c->S * n_tokens;
-  const int64_t qd = (int64_t)n_layers * cfg.n_q_heads * D, kd = (int64_t)n_layers * cfg.n_kv_heads * D;
-  AppendRowsArgs a{};
-  a.q = rows->q;
-  a.k = rows->k;
-  a.v = rows->v;
-  a.q_out = q_out;
-  a.q_row = rows->q && rows->q_row ? rows->q_row : qd;
-  a.k_row = rows->k_row ? rows->k_row : kd;
-  a.v_row = rows->v_row ? rows->v_row : kd;
-  if (a.q_row < qd || a.k_row < kd || a.v_row < kd)
-    return fail(PCED_ERR_INVALID_ARG, "rows overlap: distances %lld, %lld, %lld", (long long)a.q_row, (long long)a.k_row,
-                (long long)a.v_row);
-  // the kernel moves rows in 16-byte units
-  if (((uintptr_t)rows->q | (uintptr_t)rows->k | (uintptr_t)rows->v | (uintptr_t)q_out) % 16 ||
-      (size_t)a.q_row * es % 16 || (size_t)a.k_row * es % 16 || (size_t)a.v_row * es % 16)
-    return fail(PCED_ERR_INVALID_ARG, "rows and q_out must be 16-byte aligned, and the rows' distances too");
-  if (q_out) {
-    const size_t nq = ((R - 1) * a.q_row + qd) * es, nk = ((R - 1) * a.k_row + kd) * es, nv = ((R - 1) * a.v_row + kd) * es;
-    const bool in_place = q_out == rows->q && a.q_row == qd;
-    if ((!in_place && ranges_meet(q_out, R * qd * es, rows->q, nq)) || ranges_meet(q_out, R * qd * es, rows->k, nk) ||
-        ranges_meet(q_out, R * qd * es, rows->v, nv))
-      return fail(PCED_ERR_INVALID_ARG, "q_out overlaps the rows");
-  }
-  if (rope) {
-    const int unit = c->bf16 ? 16 : 8;
-    if (!(rope->theta > 1.0) || !std::isfinite(rope->theta)) return fail(PCED_ERR_INVALID_ARG, "rope theta must be > 1");
-    if (rope->rot_dim < 0 || rope->rot_dim > cfg.head_dim || rope->rot_dim % 2)
-      return fail(PCED_ERR_INVALID_ARG, "rot_dim %d: even, 0 .. %d", rope->rot_dim, cfg.head_dim);
-    if (rope->halves != 0 && rope->halves != 1) return fail(PCED_ERR_INVALID_ARG, "halves must be 0 or 1");
-    if (rope->halves && rope->rot_dim % unit)
-      return fail(PCED_ERR_INVALID_ARG, "rot_dim %d: a multiple of %d with halves", rope->rot_dim, unit);
-    a.rot_dim = rope->rot_dim;
-    a.halves = rope->halves;
-    a.log2_theta = std::log2(rope->theta);
-  }
   a.kpool = c->kpool;
   a.vpool = c->vpool;
-  a.len0 = c->at<int32_t>(c->lay.len0);
-  a.page_table = c->at<int32_t>(c->lay.page_table);
-  a.n_seqs = c->S;
-  a.n_tokens = n_tokens;
-  a.layer0 = layer;
-  a.n_layers = n_layers;
-  a.n_q_heads = cfg.n_q_heads;
-  a.n_kv_heads = cfg.n_kv_heads;
-  a.head_dim = cfg.head_dim;
-  a.max_pages = cfg.max_pages;
-  a.maxpps = cfg.max_pages_per_seq;
-  a.t = c->t;
-  a.sum_row = summary_row(cfg.head_dim);
-  for (int s = 0; s < c->S; ++s)
-    a.slots = std::max(a.slots, (c->len[s] + n_tokens - 1) / kPage - c->len[s] / kPage + 1);
   bool covered = c->summary != nullptr;  // (of several layers all or none: a launch has one answer)
   for (int l = layer; l < layer + n_layers; ++l) covered = covered && c->behind[l] == 0;
   if (covered) {
@@ -226,7 +239,8 @@ pced_status pced_append(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_
     a.scale = (float*)(c->summary + summary_codes(cfg));
   }
   {
-    ProfScope ps(c, PCED_PROF_APPEND, 2.0 * R * ((rows->q ? qd : 0) + 2 * kd) * es, 0);
+    const double heads = (rows->q ? cfg.n_q_heads : 0) + 2.0 * cfg.n_kv_heads;
+    ProfScope ps(c, PCED_PROF_APPEND, 2.0 * c->S * n_tokens * n_layers * heads * cfg.head_dim * esize_of(cfg), 0);
     HIP_OK(launch_append_rows(a, c->bf16, st, ps.timing()));
   }
   for (int l = layer; l < layer + n_layers; ++l) {
@@ -263,7 +277,7 @@ pced_status pced_bind_summary(pced_ctx* c, void* summary) {
 }
 
 pced_status pced_summarize(pced_ctx* c, hipStream_t st) {
-  pced_status r = check_ctx(c, true);
+  pced_status r = check_pools(c);
   if (r != PCED_OK) return r;
   if (!c->summary) return fail(PCED_ERR_STATE, "no summary buffer bound (call pced_bind_summary first)");
   const pced_config& cfg = c->cfg;
@@ -293,7 +307,8 @@ pced_status pced_summarize(pced_ctx* c, hipStream_t st) {
 
 pced_status pced_attend(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q,
                         const pced_select* sel, void* x_out, int32_t* pages_out, hipStream_t st) {
-  pced_status r = check_layers(c, layer, n_layers, n_tokens);
+  pced_status r = check_pools(c);
+  if (r == PCED_OK) r = check_layers(c, layer, n_layers, n_tokens);
   if (r != PCED_OK) return r;
   const pced_config& cfg = c->cfg;
   if (!q || !x_out) return fail(PCED_ERR_INVALID_ARG, "NULL argument");

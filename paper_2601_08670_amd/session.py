@@ -72,12 +72,23 @@ class Adjust:
 
 
 class PcedSession:
-    """A context plus its two KV pools for one model geometry and capacity."""
+    """A context plus its two KV pools for one model geometry and capacity.
+
+    ``kv8`` ("e4m3" or "int8", bf16 sessions): the caches are held in 8 bits instead, in the
+    buffers k_codes, v_codes, scales, k_open and v_open (see pced_cache8). load, append, advance,
+    attend, read_cache, lengths and the calls on logits then work as they do over pools (attend
+    without ``select``); append takes up to ``max_new`` tokens at once."""
+
+    kv8 = None
 
     def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, vocab, dtype, max_queries,
                  max_seqs, max_pages, max_pages_per_seq, norm="rms", device="cuda", poison=False,
-                 max_attn_chunks=0, aggregation="max", beta_scalar=False, ffn_dim=0, rope_theta=500000):
+                 max_attn_chunks=0, aggregation="max", beta_scalar=False, ffn_dim=0, rope_theta=500000, kv8=None,
+                 max_new=1):
         torch = _torch()
+        if kv8 is not None and (kv8 not in _lib.CODES or dtype != "bf16" or max_new < 1):
+            raise ValueError(f"kv8 is one of {sorted(_lib.CODES)}, in bf16 sessions, with max_new >= 1")
+        self.kv8, self.max_new = kv8, max_new
         self.dtype = dtype
         self.geom = dict(n_layers=n_layers, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads,
                          head_dim=head_dim, vocab=vocab)
@@ -89,14 +100,21 @@ class PcedSession:
                                     max_attn_chunks=max_attn_chunks, aggregation=aggregation,
                                     beta_scalar=beta_scalar, ffn_dim=ffn_dim, rope_theta=rope_theta)
         self.ctx = _lib.Context(self.cfg, device=device)
-        pool = _lib.pced_pool_bytes(self.cfg)
-        self.k_pool = torch.empty(pool, dtype=torch.uint8, device=device)
-        self.v_pool = torch.empty(pool, dtype=torch.uint8, device=device)
+        room = lambda n: torch.empty(n, dtype=torch.uint8, device=device)  # noqa: E731
+        if kv8 is None:
+            pool = _lib.pced_pool_bytes(self.cfg)
+            self.k_pool, self.v_pool = held = room(pool), room(pool)
+        else:
+            codes, opened = _lib.pced_codes_bytes(self.cfg), _lib.pced_open_bytes(self.cfg, max_new)
+            self.k_codes, self.v_codes, self.scales, self.k_open, self.v_open = held = (
+                room(codes), room(codes), room(_lib.pced_scales_bytes(self.cfg)), room(opened), room(opened))
         if poison:  # all-ones bytes: NaN in bf16 and f32, to expose reads of unwritten memory
-            for t in (self.k_pool, self.v_pool, self.ctx.workspace):
+            for t in (*held, self.ctx.workspace):
                 t.fill_(255)
-        self.device = self.k_pool.device  # ("cuda": the one that is current now, for later allocations too)
-        self._device_index = self.k_pool.get_device()
+        if kv8 is not None:
+            self.scales, self.k_open, self.v_open = (t.view(torch.bfloat16) for t in held[2:])
+        self.device = held[0].device  # ("cuda": the one that is current now, for later allocations too)
+        self._device_index = held[0].get_device()
         self._dtypes = (torch.bfloat16, torch.int16, torch.uint16) if dtype == "bf16" else (torch.float32,)
         self._rows, self._ropes, self._out_like = _lib.pced_rows(), {}, {}
         self.n_experts: list = []
@@ -141,9 +159,12 @@ class PcedSession:
         self.B = len(self.n_experts)
         self.S = int(sum(n + 1 for n in self.n_experts))
         self.NE = int(sum(self.n_experts))
-        self.ctx.pced_load_caches(n_experts, cache_len, src_k, src_v, self.k_pool, self.v_pool, relevance,
-                                  gamma=gamma, beta=beta, page_table=page_table,
-                                  reserve_tokens=reserve_tokens)
+        batch = dict(gamma=gamma, beta=beta, page_table=page_table, reserve_tokens=reserve_tokens)
+        if self.kv8 is None:
+            self.ctx.pced_load_caches(n_experts, cache_len, src_k, src_v, self.k_pool, self.v_pool, relevance, **batch)
+        else:
+            self.ctx.pced_load_codes(n_experts, cache_len, src_k, src_v, self.kv8, self.max_new, self.k_codes, self.v_codes,
+                                self.scales, self.k_open, self.v_open, relevance, **batch)
         # (shapes of fuse_adjusted's outputs: empty_like takes a third less time than a shape and a type)
         self._out_like = self.out_buffers(("winner", "top1", "top2", "beta_used"))
 
@@ -197,11 +218,14 @@ class PcedSession:
     def _on_device(self):
         """The calls go to the current device's stream, which has to be the session's."""
         if _lib.current_device() != self._device_index:
-            raise ValueError(f"the session is on {self.k_pool.device}, which is not the current device")
+            raise ValueError(f"the session is on {self._where()}, which is not the current device")
+
+    def _where(self):
+        return (self.k_pool if self.kv8 is None else self.k_codes).device
 
     def _here(self, t, name):
         if t.get_device() != self._device_index:
-            raise ValueError(f"{name}: on {t.device}, the session is on {self.k_pool.device}")
+            raise ValueError(f"{name}: on {t.device}, the session is on {self._where()}")
         return t
 
     def _row_stride(self, t, name, n_tokens, n_layers, heads):
@@ -254,7 +278,8 @@ class PcedSession:
                 q_out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
             elif self._storage(q_out, "q_out").shape != q.shape or not q_out.is_contiguous():
                 raise ValueError("q_out: q's shape, contiguous")
-        self.ctx.pced_append(layer, n_layers, n_tokens, rows, self._rope(rope), q_out)
+        call = self.ctx.pced_append if self.kv8 is None else self.ctx.pced_append_codes
+        call(layer, n_layers, n_tokens, rows, self._rope(rope), q_out)
         return q_out
 
     def advance(self, n_tokens=1):
@@ -289,6 +314,11 @@ class PcedSession:
         elif self._storage(x_out, "x_out").shape != (rows, n_layers, width) or not x_out.is_contiguous():
             raise ValueError("x_out: [S * n_tokens][n_layers][Hq * D], contiguous")
         out, sel, pages = {"x": x_out}, None, None
+        if self.kv8 is not None:
+            if select is not None or want:
+                raise ValueError("a cache in 8 bits is attended to whole: no select, no pages")
+            self.ctx.pced_attend_codes(layer, n_layers, n_tokens, q, x_out)
+            return out
         if select is not None:
             sel = _lib.pced_select(*select)
             if want:
@@ -348,7 +378,8 @@ class PcedSession:
         dt = torch.int16 if self.dtype == "bf16" else torch.float32
         k = torch.empty((count, g["n_kv_heads"], g["head_dim"]), dtype=dt, device=self.device)
         v = torch.empty_like(k)
-        self.ctx.pced_read_cache(seq, layer, start, count, k, v)
+        call = self.ctx.pced_read_cache if self.kv8 is None else self.ctx.pced_read_codes
+        call(seq, layer, start, count, k, v)
         return k, v
 
 

@@ -1,0 +1,446 @@
+"""Caches held in 8 bits on the GPU (load, append, attention, reading back) against the oracle (oracle/codes.py) and
+against a twin session whose caches are in the pools. Codes, scales and open pages are exact; the attention's
+tolerance follows from its roundings."""
+import numpy as np
+import pytest
+
+from oracle import codes as C
+from tests.test_gpu_layer import DEV, PAGE, Model, _eq, _f64
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+CODES = ["e4m3", "int8"]
+
+
+class Coded(Model):
+    """A session over caches in 8 bits (poisoned buffers, pages in random order) and the caches' rows as bf16."""
+
+    def __init__(self, lens, room, code, heads=(8, 2, 64), layers=1, max_new=None, **kw):
+        self.code = code
+        self.max_new = max_new or max(1, room)
+        super().__init__(lens, room, "bf16", heads, layers, kv8=code, max_new=self.max_new, **kw)
+
+    @property
+    def ring(self):
+        return (self.max_new + 14) // PAGE + 1
+
+    def tokens(self, which):
+        """Codes of every physical page, [L][pages][Hkv][16][D], and scales [L][Hkv][pages]."""
+        t, d = np.arange(PAGE)[:, None], np.arange(self.d)[None, :]
+        if which == "k":
+            at = (d // 64 * 64 + t + 16 * (d % 32 // 8)) * 16 + d % 64 // 32 * 8 + d % 8
+        else:
+            at = (d // 64 * 64 + d % 16 + 16 * (t // 4)) * 16 + d % 64 // 16 * 4 + t % 4
+        raw = getattr(self.sess, which + "_codes").view(self.layers, -1, self.hkv, PAGE * self.d).cpu().numpy()
+        scales = self.sess.scales.view(self.layers, self.hkv, -1, 2)[..., "kv".index(which)]
+        return raw[..., at.reshape(-1)].reshape(raw.shape[:3] + (PAGE, self.d)), scales.float().cpu().numpy()
+
+    def opened(self, which):
+        """Open pages, [L][max_seqs][ring][Hkv][16][D]."""
+        x = getattr(self.sess, which + "_open").view(self.layers, -1, self.ring, self.hkv, PAGE * self.d)
+        at = self.tile_offsets()["kv".index(which)]
+        return x[..., at.reshape(-1)].view(x.shape[:4] + (PAGE, self.d))
+
+    def check_state(self, lens):
+        """Codes and scales of every complete page, the rows behind; what no page holds is as it was."""
+        for which, rows in (("k", self.k), ("v", self.v)):
+            codes, scales = self.tokens(which)
+            opened = self.opened(which)
+            used = np.zeros(codes.shape[1], bool)
+            for s, n in enumerate(lens):
+                x = _f64(rows[s])
+                for p in range(n // PAGE):
+                    phys = int(self.table[s, p])
+                    used[phys] = True
+                    for l in range(self.layers):
+                        for h in range(self.hkv):
+                            b, sc = C.encode(x[l, PAGE * p:PAGE * (p + 1), h], self.code)
+                            # (of a zero either sign: NaN's codes and those of -0 are zeros)
+                            got, zero = codes[l, phys, h], 128 if self.code == "e4m3" else 0
+                            assert ((got == b) | ((got | zero == zero) & (b | zero == zero))).all(), (which, s, p, l, h)
+                            assert scales[l, h, phys] == sc, (which, s, p, l, h)
+                if n % PAGE:
+                    p = n // PAGE
+                    _eq(opened[:, s, p % self.ring, :, :n % PAGE], rows[s][:, PAGE * p:n].transpose(1, 2), (which, s))
+            spare = np.setdiff1d(np.arange(codes.shape[1]), self.table[self.table >= 0])
+            assert (codes[:, spare] == 255).all() and np.isnan(scales[..., spare]).all()
+            unused = ~used & np.isin(np.arange(codes.shape[1]), self.table)
+            yield which, unused, codes
+
+    def check(self, lens):
+        for _ in self.check_state(lens):
+            pass
+
+    def values(self, lens):
+        """The caches' rows in float64 as the codes hold them, complete pages at lens."""
+        return [[np.stack([C.held(_f64(x[s][l]), n // PAGE * PAGE, self.code) for l in range(self.layers)])
+                 for s, n in enumerate(lens)] for x in (self.k, self.v)]
+
+
+# (heads, layers, lengths)
+LOADS = [
+    ((8, 2, 64), 1, [5, 40, 16, 31, 1]),
+    ((4, 4, 64), 2, [15, 32, 64]),
+    ((32, 8, 128), 2, [2, 47, 17]),
+    ((28, 4, 128), 1, [100, 33]),
+    ((12, 3, 128), 1, [64, 17]),
+    ((20, 5, 64), 1, [33, 16]),
+    ((16, 1, 128), 3, [14, 48]),
+]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,layers,lens", LOADS)
+def test_load(code, heads, layers, lens):
+    m = Coded(lens, 3, code, heads, layers, scale=2.0)
+    torch.cuda.synchronize()
+    for which, unused, codes in m.check_state(lens):
+        assert (codes[:, unused] == 255).all()
+    for s, n in enumerate(lens):  # and read back, in parts
+        want = m.values(lens)
+        for l in range(layers):
+            for a, b in {(0, n), (n // 3, n), (n // 2, n // 2), (min(n, 17), n)}:
+                got = m.sess.read_cache(s, l, a, b - a)
+                for x, y in zip(got, want):
+                    y = torch.from_numpy(y[s][l, a:b]).to(torch.bfloat16).to(DEV)
+                    assert torch.equal(x.view(torch.bfloat16), y), (s, l, a)  # (exact values, rounded once)
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_blocks_of_extremes(code):
+    """Zeros, one value, the smallest and the largest numbers, infinities and NaN."""
+    m = Coded([160, 40], 1, code, (8, 2, 64))
+    k = m.k[0]
+    k[0, :16] = 0
+    k[0, 16:32] = 0.37
+    k[0, 32:48] *= 1e-30
+    k[0, 48:64] *= 1e-38
+    k[0, 64:80] *= 1e38
+    k[0, 80] = float("inf")
+    k[0, 96, :, 3] = float("-inf")
+    k[0, 112:128, :, 5] = float("nan")
+    k[0, 128:144] = float("nan")
+    k[0, 144:160] = torch.finfo(torch.bfloat16).max
+    m.v[0] = k.flip(1).contiguous()
+    m.load()
+    torch.cuda.synchronize()
+    m.check([160, 40])
+    for x in m.sess.read_cache(0, 0, 0, 160):
+        assert torch.isfinite(x.view(torch.bfloat16)).all()
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_load_from_host_memory(code):
+    """Caches in host memory, whole and in pieces, give what device memory does."""
+    a, b = (Coded([37, 64, 1000], 2, code, (8, 2, 128), 2, seed=4) for _ in range(2))
+    b.k, b.v = [x.cpu() for x in b.k], [x.cpu() for x in b.v]
+    b.load()
+    torch.cuda.synchronize()
+    for name in ("k_codes", "v_codes", "scales", "k_open", "v_open"):
+        _eq(getattr(a.sess, name), getattr(b.sess, name), name)
+
+
+# (heads, layers, lengths, new tokens)
+APPENDS = [
+    ((8, 2, 64), 1, [5, 40, 16, 31, 1, 15], 1),
+    ((4, 4, 64), 2, [15, 32], 1),
+    ((32, 8, 128), 3, [2, 47, 17], 1),
+    ((8, 8, 128), 1, [13, 30, 64], 7),
+    ((28, 4, 128), 1, [1, 100], 33),
+    ((16, 1, 128), 2, [14, 3, 31], 50),
+    ((20, 5, 64), 1, [16, 9], 64),
+]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,layers,lens,T", APPENDS)
+@pytest.mark.parametrize("rot,halves", [(1.0, False), (0.5, True), (None, False)])
+def test_append(code, heads, layers, lens, T, rot, halves):
+    """The rows as an append into the pools stores them, and the codes of the pages that they fill."""
+    m, twin = Coded(lens, T, code, heads, layers, seed=2), Model(lens, T, "bf16", heads, layers, seed=2)
+    rope = None if rot is None else (10000.0, int(heads[2] * rot), halves)
+    q, k, v = m.rows(T)
+    for _ in range(2):  # (repeated: the same)
+        _eq(m.sess.append(q, k, v, n_tokens=T, rope=rope), twin.sess.append(q, k, v, n_tokens=T, rope=rope))
+    m.sess.advance(T)
+    twin.sess.advance(T)
+    now = [n + T for n in lens]
+    assert m.sess.lengths() == now
+    got = [twin.sess.read_cache(s, l, 0, n) for s, n in enumerate(now) for l in range(layers)]
+    for i, x in enumerate((m.k, m.v)):
+        for s in range(m.S):
+            x[s] = torch.stack([got[s * layers + l][i].view(torch.bfloat16) for l in range(layers)])
+    torch.cuda.synchronize()
+    m.check(now)
+
+
+def test_append_of_strided_rows_and_of_layers():
+    """Views of one projection's output, one layer at a time, K / V only: as whole contiguous calls."""
+    heads, T, lens, rope = (8, 2, 128), 5, [14, 40], (500000.0, 128, True)
+    hq, hkv, d = heads
+    a, b, c = (Coded(lens, T, "e4m3", heads, 2, seed=3) for _ in range(3))
+    q, k, v = a.rows(T)
+    want = a.sess.append(q, k, v, n_tokens=T, rope=rope)
+    for l in range(2):
+        fused = torch.cat([x[:, l].reshape(len(lens) * T, -1) for x in (q, k, v)] + [a.rand((len(lens) * T, 16))], 1)
+        parts = [x.unflatten(1, (1, h, d)) for x, h in zip(fused.split([hq * d, hkv * d, hkv * d, 16], 1), (hq, hkv, hkv))]
+        _eq(b.sess.append(*parts, n_tokens=T, rope=rope, layer=l, n_layers=1)[:, 0], want[:, l])
+    assert c.sess.append(None, k, v, n_tokens=T, rope=rope) is None
+    torch.cuda.synchronize()
+    for name in ("k_codes", "v_codes", "scales", "k_open", "v_open"):
+        _eq(getattr(a.sess, name), getattr(b.sess, name), name)
+        _eq(getattr(a.sess, name), getattr(c.sess, name), name)
+
+
+def _check_attend(m, q, x, T, lens, layers=None):
+    """x [S * T][L][Hq * D] against the oracle over the values that the cache holds at lens (rows appended behind)."""
+    G, half = m.hq // m.hkv, 2.0 ** -8
+    layers = list(range(m.layers)) if layers is None else layers
+    ks, vs = m.values(lens)
+    got = _f64(x).reshape(m.S * T, len(layers), m.hq, m.d)
+    for s in range(m.S):
+        for i in range(T):
+            n = lens[s] + i + 1
+            for at, l in enumerate(layers):
+                for h in range(m.hkv):
+                    qq = _f64(q[s * T + i, at, h * G:(h + 1) * G])
+                    kk, vv = ks[s][l, :n, h], vs[s][l, :n, h]
+                    want = C.attend(qq, kk, vv)
+                    # a score's fp32 sum of D products, its block's scale and the difference of scores are off by at
+                    # most (D + 6) 2^-24 times the sum of the products' sizes; a weight's relative error is at most that
+                    # of scores (twice, with the reference's), of exp2 (2^-22), of its product with V's scale (2^-24)
+                    # and of its two bf16 parts (2^-17), in numerator and sum; the fp32 sums over n tokens and over
+                    # the parts' states add (n + 64) 2^-24 to each; the result is rounded to bf16 once (half a step:
+                    # 2^-8)
+                    ds = (m.d + 6) * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T).max() / np.sqrt(m.d)
+                    rel = 2 * (2 * ds + 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -17) + 2 * (n + 64) * 2.0 ** -24
+                    tol = half * np.abs(want) + rel * (1 + half) * np.abs(vv).max()
+                    err = np.abs(got[s * T + i, at, h * G:(h + 1) * G] - want) - tol
+                    assert (err <= 0).all(), (s, i, l, h, float(err.max()))
+
+
+def _append_rows(m, T, spread=1.0):
+    q, k, v = m.rows(T)
+    m.sess.append(None, k, v, n_tokens=T, rope=None)
+    return q * spread, k, v
+
+
+# (heads, layers, lengths, new tokens)
+ATTENDS = [
+    ((8, 2, 64), 1, [1, 300, 16, 47, 15], 1),
+    ((8, 2, 64), 2, [500, 15], 1),
+    ((32, 8, 128), 1, [64, 700, 431], 1),
+    ((28, 4, 128), 1, [1000, 20], 5),
+    ((16, 1, 128), 1, [400, 33], 19),
+    ((4, 4, 64), 3, [250, 60, 7], 17),
+    ((8, 2, 128), 1, [300, 40], 33),
+    ((8, 2, 128), 2, [130, 16, 1], 2),
+    ((32, 2, 64), 1, [77, 200], 3),
+    ((12, 1, 128), 1, [129, 5], 4),
+    ((8, 2, 64), 1, [6000, 1], 1),
+    ((8, 2, 64), 1, [4500, 17], 20),
+]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,layers,lens,T", ATTENDS)
+def test_attend(code, heads, layers, lens, T):
+    m = Coded(lens, T, code, heads, layers, seed=7)
+    q, k, v = _append_rows(m, T)
+    x = m.sess.attend(q, n_tokens=T)["x"]
+    m.grow(k, v, T)
+    torch.cuda.synchronize()
+    _check_attend(m, q, x, T, lens)
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_attend_sharp_scores_and_uneven_blocks(code):
+    """Scores far apart, blocks whose scales differ by twenty orders, zero queries."""
+    m = Coded([400, 333], 2, code, (8, 2, 64), seed=8)
+    m.v[0][:, 32:64] *= 1e10
+    m.v[0][:, 64:96] *= 1e-10
+    m.k[1][:, 48:64] = 0
+    m.load()
+    q, k, v = _append_rows(m, 2, spread=30.0)
+    q[2] = 0
+    x = m.sess.attend(q, n_tokens=2)["x"]
+    m.grow(k, v, 2)
+    torch.cuda.synchronize()
+    _check_attend(m, q, x, 2, [400, 333])
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 4, 128), (16, 1, 64)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("at", [2, 5])
+def test_attend_with_bad_values_behind(heads, bad, at):
+    """NaN and infinities behind a row's position leave it alone, in its own page and group of rows too; rows that
+    see them show them. Rows nobody wrote hold NaN throughout."""
+    m = Coded([37, 112, 15], 8, "e4m3", heads, seed=10)
+    T = 8
+    q, k, v = m.rows(T)
+    m.sess.append(None, k, v, n_tokens=T, rope=None)
+    good = m.sess.attend(q, n_tokens=T)["x"]
+    k, v = k.clone(), v.clone()
+    k[at::T] = float("nan")
+    v[at::T] = bad
+    m.sess.append(None, k, v, n_tokens=T, rope=None)
+    x = m.sess.attend(q, n_tokens=T)["x"]
+    torch.cuda.synchronize()
+    for s in range(m.S):
+        _eq(x[T * s:T * s + at], good[T * s:T * s + at], s)
+        assert torch.isnan(x[T * s + at:T * (s + 1)]).all()
+    v = torch.where(torch.isfinite(v), v, bad)
+    k = torch.where(torch.isnan(k), 0, k)  # the row's key is a number: its value shows
+    m.sess.append(None, k, v, n_tokens=T, rope=None)
+    x = m.sess.attend(q, n_tokens=T)["x"]
+    torch.cuda.synchronize()
+    for s in range(m.S):
+        _eq(x[T * s:T * s + at], good[T * s:T * s + at], s)
+        assert not torch.isfinite(x[T * s + at:T * (s + 1)]).any()
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_steps(code):
+    """Forty steps of changing widths, some rows of which are not kept: lengths, codes and attention throughout."""
+    m = Coded([3, 47, 16], 200, code, (8, 2, 64), 2, max_new=20, seed=12)
+    r, lens = np.random.RandomState(3), [3, 47, 16]
+    for step in range(40):
+        T = int(r.choice([1, 1, 1, 2, 5, 16, 20]))
+        keep = T if r.rand() < 0.7 else int(r.randint(1, T + 1))
+        if lens[0] + T > 190:
+            break
+        _append_rows(m, T, 1.0)  # (rows that are replaced)
+        q, k, v = _append_rows(m, T)
+        x = m.sess.attend(q, n_tokens=T)["x"]
+        if step % 4 == 0:
+            old = m.k, m.v
+            m.k, m.v = list(m.k), list(m.v)
+            m.grow(k, v, T)
+            torch.cuda.synchronize()
+            _check_attend(m, q, x, T, lens)
+            m.k, m.v = old
+        rows = [s * T + i for s in range(3) for i in range(keep)]
+        m.grow(k[rows], v[rows], keep)
+        m.sess.advance(keep)
+        lens = [n + keep for n in lens]
+        assert m.sess.lengths() == lens
+    torch.cuda.synchronize()
+    m.check(lens)
+
+
+def test_attend_of_layers_and_fewer_tokens():
+    """Layers one by one, fewer tokens than were appended, an output of the caller's: the same bits."""
+    m = Coded([700, 33, 512], 6, "int8", (8, 2, 128), layers=5, seed=11)
+    q, k, v = _append_rows(m, 6)
+    a = m.sess.attend(q, n_tokens=6)["x"]
+    _eq(m.sess.attend(q, n_tokens=6)["x"], a)
+    out = torch.empty_like(a)
+    assert m.sess.attend(q, n_tokens=6, x_out=out)["x"] is out
+    _eq(out, a)
+    m.grow(k, v, 6)
+    for l in range(5):
+        b = m.sess.attend(q[:, l:l + 1].contiguous(), n_tokens=6, layer=l, n_layers=1)["x"]
+        torch.cuda.synchronize()
+        _check_attend(m, q[:, l:l + 1], b, 6, [700, 33, 512], layers=[l])
+    two = torch.cat([q[6 * s:6 * s + 2] for s in range(3)])
+    x = m.sess.attend(two, n_tokens=2)["x"]
+    torch.cuda.synchronize()
+    _check_attend(m, two, x, 2, [700, 33, 512])
+
+
+def test_pages_beyond_4_gib():
+    """Codes more than 2^32 bytes, open pages more than 2^31 bytes behind their buffers' beginnings."""
+    heads, layers = (32, 8, 128), 5
+    from paper_2601_08670_amd.session import PcedSession
+    m = Coded([40, 20], 20, "e4m3", heads, layers, max_new=20, seed=13)
+    n = 60000
+    far = PcedSession(n_layers=layers, n_q_heads=32, n_kv_heads=8, head_dim=128, vocab=500, dtype="bf16", max_queries=1,
+                      max_seqs=7000, max_pages=n, max_pages_per_seq=m.table.shape[1], device=DEV, kv8="e4m3", max_new=20)
+    assert far.k_codes.numel() > 2 ** 32 and far.k_open.numel() * 2 > 2 ** 31
+    table = np.where(m.table >= 0, n - 1 - m.table, -1).astype(np.int32)
+    far.load([1], m.lens, m.k, m.v, [0.5], beta=[0.5], page_table=table)
+    q, k, v = m.rows(20)
+    for s in (m.sess, far):
+        s.append(None, k, v, n_tokens=20)
+    a, b = (s.attend(q, n_tokens=20)["x"] for s in (m.sess, far))
+    torch.cuda.synchronize()
+    _eq(a, b)
+    for s in (m.sess, far):
+        s.advance(20)
+    for l in (0, layers - 1):
+        for x, y in zip(m.sess.read_cache(0, l, 0, 60), far.read_cache(0, l, 0, 60)):
+            _eq(x, y)
+
+
+def test_streams_and_graphs():
+    """A captured step replays on new rows, between eager steps of its own stream and others."""
+    m = Coded([200, 15, 31], 4, "e4m3", (8, 2, 64), 2, seed=14)
+    other = Coded([90, 40], 4, "int8", (8, 2, 64), 2, seed=15)
+    T = 3
+    q, k, v = m.rows(T)
+    out, rope = torch.empty_like(q), (10000.0, 64, False)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        m.sess.append(q, k, v, n_tokens=T, rope=rope, q_out=out)
+        x = m.sess.attend(out, n_tokens=T)["x"]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.sess.append(q, k, v, n_tokens=T, rope=rope, q_out=out)
+        m.sess.attend(out, n_tokens=T, x_out=x)
+    for i in range(3):
+        q2, k2, v2 = m.rows(T)
+        q.copy_(q2), k.copy_(k2), v.copy_(v2)
+        x.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        got = x.clone()
+        o = other.rows(1)
+        other.sess.append(*o)
+        other.sess.attend(o[0])
+        want = m.sess.attend(m.sess.append(q, k, v, n_tokens=T, rope=rope), n_tokens=T)["x"]
+        torch.cuda.synchronize()
+        _eq(got, want, i)
+
+
+def test_profile_counts():
+    m = Coded([300, 40], 1, "e4m3", (8, 2, 64), seed=16)
+    m.sess.ctx.pced_profile_enable(True)
+    q, k, v = m.rows(1)
+    m.sess.attend(m.sess.append(q, k, v))
+    torch.cuda.synchronize()
+    p = m.sess.ctx.pced_profile_read()
+    assert p["append"]["launches"] == 1 and p["attn"]["launches"] == 1 and p["attn"]["bytes"] > 0
+
+
+def test_session_refusals():
+    from paper_2601_08670_amd import _lib
+    from paper_2601_08670_amd.session import PcedSession
+    m, twin = Coded([40, 20], 4, "e4m3", max_new=2), Model([40, 20], 4)
+    q, k, v = m.rows(3)
+    with pytest.raises(_lib.PcedError, match="CAPACITY"):
+        m.sess.append(q, k, v, n_tokens=3)
+    q, k, v = m.rows(1)
+    with pytest.raises(_lib.PcedError, match="STATE"):
+        m.sess.attend(q)
+    m.sess.append(q, k, v)
+    for kw in (dict(select=(2, 1, 1)), dict(want=("pages",))):
+        with pytest.raises(ValueError):
+            m.sess.attend(q, **kw)
+    with pytest.raises(ValueError):
+        m.sess.attend(q.float())
+    with pytest.raises(_lib.PcedError, match="UNSUPPORTED"):
+        m.sess.ctx.pced_attend(0, 1, 1, q, None, torch.empty_like(q))
+    with pytest.raises(_lib.PcedError, match="UNSUPPORTED"):
+        m.sess.step(q, k, v, torch.empty(_lib.pced_lm_head_bytes(m.sess.cfg), dtype=torch.uint8, device=DEV))
+    with pytest.raises(_lib.PcedError, match="STATE"):
+        twin.sess.ctx.pced_attend_codes(0, 1, 1, q, torch.empty_like(q))
+    with pytest.raises(_lib.PcedError, match="INVALID"):
+        m.sess.read_cache(0, 0, 30, 20)
+    base = dict(n_layers=1, n_q_heads=8, n_kv_heads=2, head_dim=64, vocab=500, max_queries=1, max_seqs=2, max_pages=4,
+                max_pages_per_seq=2, device=DEV)
+    for kw in (dict(dtype="f32", kv8="e4m3"), dict(dtype="bf16", kv8="int4"), dict(dtype="bf16", kv8="int8", max_new=0)):
+        with pytest.raises(ValueError):
+            PcedSession(**base, **kw)
