@@ -665,6 +665,51 @@ pced_status pced_adjust_logits(pced_ctx* ctx, const float* logits, const pced_ad
 pced_status pced_fuse_adjusted(pced_ctx* ctx, const float* logits, int32_t refresh_beta, const pced_adjust* adjust,
                                int32_t* tokens_out, const pced_step_out* extra, hipStream_t stream);
 
+/*
+ * Sampling: a token per query, drawn from the softmax of its scores at a temperature. The paper's choice
+ * is the highest score (Eq. 3); here, for query b with S(v) = max_k s_hat_k(v) over its adjusted logits (Eq. 2),
+ * T its temperature and s_max its highest score:
+ *     candidates: tokens whose score is a number above -inf that the mask leaves open, in falling order of
+ *                 score, the lower token first among equals; weights w(v) = exp((S(v) - s_max) / T)
+ *     top_k       keeps the first top_k of them (<= 0: all)
+ *     top_p       of those, the shortest beginning that holds at least top_p of their weight (>= 1: all)
+ *     min_p       of those, the tokens with S(v) >= s_max + T ln min_p, that is w(v) >= min_p (<= 0: all)
+ *     the token is the first, in that order, at which the running sum of what is kept exceeds uniform[b] times
+ *     its total
+ * The first candidate is always kept. T <= 0 (or NaN) is Eq. 3's choice. Eq. 2 is in fp32; weights come from
+ * fp64 and are summed exactly, as multiples of 2^-(62 - ceil(log2 V)) (those below half of that
+ * weigh nothing, and are never drawn), so that equal inputs give equal outputs. uniform is cut to [0, 1 - 2^-24], NaN
+ * counts as 0. All pointers are device memory, read when the call runs.
+ */
+typedef struct pced_sampling {
+  const float* temperature;  /* [B]                                  */
+  const int32_t* top_k;      /* [B] or NULL: no such cut, each       */
+  const float* top_p;
+  const float* min_p;
+} pced_sampling;
+
+/* Optional device outputs; any NULL member is skipped. */
+typedef struct pced_sample_out {
+  int32_t* winner;           /* [B] expert (1..N_b) with the token's highest score    */
+  float* score;              /* [B] the token's fused score                           */
+  float* logprob;            /* [B] ln of its weight over the weight of what was kept */
+  int32_t* kept;             /* [B] how many tokens were kept                         */
+  float* beta_used;          /* [sum N_b] beta_k used                                 */
+} pced_sample_out;
+
+/*
+ * Stage entry: the sampled tokens of the loaded batch.
+ *   logits        device [S][V] fp32, rows in load order
+ *   refresh_beta  as for pced_fuse; from the logits as given
+ *   adjust        adjustments of the logits, or NULL
+ *   uniform       device [B] random numbers in [0, 1), one per query
+ *   tokens_out    device [B]; -1 where a query has no candidate (winner 0, score and logprob -inf, kept 0)
+ * Errors: as pced_fuse_adjusted.
+ */
+pced_status pced_sample(pced_ctx* ctx, const float* logits, int32_t refresh_beta, const pced_adjust* adjust,
+                        const pced_sampling* sampling, const float* uniform, int32_t* tokens_out,
+                        const pced_sample_out* extra, hipStream_t stream);
+
 /* Kernel timing with HIP events attached to each kernel dispatch (start when
  * the kernel begins, stop when it completes). Classes: */
 enum {

@@ -28,7 +28,7 @@ EXPORTED = ("pced_pool_bytes", "pced_lm_head_bytes", "pced_pack_lm_head", "pced_
             "pced_stream_read", "pced_append", "pced_advance", "pced_summary_bytes", "pced_bind_summary",
             "pced_summarize", "pced_attend", "pced_adjust_logits", "pced_fuse_adjusted",
             "pced_codes_bytes", "pced_scales_bytes", "pced_open_bytes", "pced_load_codes", "pced_append_codes", "pced_attend_codes",
-            "pced_read_codes")
+            "pced_read_codes", "pced_sample")
 
 
 class PcedError(RuntimeError):
@@ -83,6 +83,14 @@ class pced_adjust(ctypes.Structure):
                 ("mask_row", ctypes.c_int64), ("n_history", ctypes.c_int32), ("n_bias", ctypes.c_int32)]
 
 
+class pced_sampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class pced_sample_out(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("winner", "score", "logprob", "kept", "beta_used")]
+
+
 class pced_profile(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64 * 13), ("total_ms", ctypes.c_double * 13),
                 ("bytes", ctypes.c_double * 13), ("flops", ctypes.c_double * 13)]
@@ -135,6 +143,8 @@ def load_library() -> ctypes.CDLL:
         "pced_attend": (I, [P, I, I, I, P, ctypes.POINTER(pced_select), P, P, V]),
         "pced_adjust_logits": (I, [P, P, ctypes.POINTER(pced_adjust), P, V]),
         "pced_fuse_adjusted": (I, [P, P, I, ctypes.POINTER(pced_adjust), P, ctypes.POINTER(pced_step_out), V]),
+        "pced_sample": (I, [P, P, I, ctypes.POINTER(pced_adjust), ctypes.POINTER(pced_sampling), P, P,
+                            ctypes.POINTER(pced_sample_out), V]),
         "pced_codes_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config)]),
         "pced_scales_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config)]),
         "pced_open_bytes": (ctypes.c_size_t, [ctypes.POINTER(pced_config), I]),
@@ -452,6 +462,15 @@ class Context:
                 setattr(so, name, t.data_ptr())
         _check(self.lib.pced_fuse_adjusted(self.handle, _ptr(logits), int(refresh_beta), ctypes.byref(adjust),
                                            _ptr(tokens_out), ctypes.byref(so), _stream(stream)))
+
+    def pced_sample(self, logits, refresh_beta, adjust: Optional[pced_adjust], sampling: pced_sampling, uniform,
+                    tokens_out, extra: Optional[dict] = None, stream=None):
+        """extra: outputs (winner, score, logprob, kept, beta_used)."""
+        so = pced_sample_out(**{n: _ptr(t) for n, t in extra.items() if t is not None}) if extra else None
+        _check(self.lib.pced_sample(self.handle, _ptr(logits), int(refresh_beta),
+                                    None if adjust is None else ctypes.byref(adjust), ctypes.byref(sampling),
+                                    _ptr(uniform), _ptr(tokens_out), None if so is None else ctypes.byref(so),
+                                    _stream(stream)))
 
     def pced_get_lengths(self, n_seqs):
         out = (ctypes.c_int32 * n_seqs)()

@@ -15,8 +15,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-I", os.path.join(ROOT, "include"), "-I", CSRC]
-SOURCES = ["pced_kernels.hip", "pced_layer.hip", "pced_cache8.hip", "pced_api.cpp", "pced_layer_api.cpp",
-           "pced_cache8_api.cpp"]
+SOURCES = ["pced_kernels.hip", "pced_layer.hip", "pced_cache8.hip", "pced_sample.hip", "pced_api.cpp",
+           "pced_layer_api.cpp", "pced_cache8_api.cpp", "pced_sample_api.cpp"]
 # rocBLAS: the many-row decoder projections' GEMMs
 LINK = ["-L/opt/rocm/lib", "-Wl,-rpath,/opt/rocm/lib", "-lrocblas"]
 

@@ -177,6 +177,10 @@ Layout make_layout(const pced_config& c) {
   L.pf_part_ml = take(2 * PR * c.n_kv_heads * kPrefillParts * G * 2 * 4);  // (bf16 states: pf_part_acc holds twice as many)
   L.pf_proj_elems = std::max(PR * max_cols, (size_t)kLmRowsPad * L.part_cols);
   L.pf_proj = take(L.pf_proj_elems * 4);
+  // sampling: a query's bins and its list of tokens (scores and experts: the logits' place, which has a
+  // row for every query's amateur and one for its first expert)
+  L.smp_bins = take(B * sizeof(SampleBins));
+  L.smp_list = take(B * c.vocab * 4);
   L.total = o;
   return L;
 }

@@ -32,7 +32,7 @@ struct Layout {
   size_t chunk_info, seg, nparts, work_pages, prev_tok, beta, part_acc, part_ml, x, logits,
       rho, x_packed, fuse_part, lse_part, jsd_part, syn_q, syn_k, syn_v, dec_h, dec_a, dec_act, dec_ss, dec_rho, dec_part,
       rope, pf_len0, pf_pt, pf_tok, pf_glen0, pf_gpt, pf_nparts, pf_rho, pf_h, pf_a, pf_act, pf_ss, pf_q, pf_x, pf_part_acc, pf_part_ml, pf_proj,
-      stage_bytes, total;
+      smp_bins, smp_list, stage_bytes, total;
   int packed_rows;      // rows x_packed holds
   int pf_rows;          // rows of one prefill chunk (sequences x suffix tokens)
   size_t pf_proj_cols;  // slices x columns per row of the prefill projection partials
@@ -170,6 +170,8 @@ void advance(pced_ctx* c, int n, bool by_rows);
 
 FuseArgs fuse_args(pced_ctx* c, const float* logits, int32_t* tokens_out, int tok_stride, const pced_step_out* extra,
                    int nblk);
+// The device form of a caller's adjustments.
+pced_status adjust_args(const pced_ctx* c, const pced_adjust* d, AdjustArgs* out);
 // Dynamic beta from `logits`, summed, ready for a later launch.
 pced_status run_beta(pced_ctx* c, const float* logits, hipStream_t st);
 

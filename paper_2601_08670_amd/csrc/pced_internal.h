@@ -196,6 +196,41 @@ struct AdjustArgs {
   int rows_per_block;       // (set by launch_adjust)
 };
 
+// Sampling (see pced_sample). A query's candidates are divided by their distance below the highest score into
+// kSampleBins bins of equal width, the highest first; what a bin holds is counted and its weights are summed, as
+// whole multiples of 2^-shift, so that the order of the additions leaves no trace.
+constexpr int kSampleBins = 2048;
+struct SampleBins {
+  unsigned long long mass[kSampleBins];
+  uint32_t count[kSampleBins];
+  unsigned long long floor_mass;  // of the candidates that min_p keeps
+  uint32_t floor_count;
+  uint32_t listed;                // tokens in the query's list
+};
+static_assert(sizeof(SampleBins) % 16 == 0, "cleared in 16-byte stores");
+struct SampleArgs {
+  float* scores;            // [B][V]; -inf where no expert scores the token
+  int32_t* who;             // [B][V] the best expert
+  const float* part;        // [B][nblk][2] the slices' largest and smallest candidate
+  SampleBins* bins;         // [B]
+  int32_t* list;            // [B][V] tokens of the bins that hold a cut
+  const float* temperature; // [B] each; the filters' are optional
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniform;
+  int32_t* tokens_out;      // [B]
+  int32_t* prev_tok;        // [B]
+  int32_t* winner;          // optional [B] each
+  float* score;
+  float* logprob;
+  int32_t* kept;
+  float* beta_used;         // optional [sum N], with the betas as used
+  const float* beta;
+  const int32_t* query_exp0;
+  int V, nblk, shift;
+};
+
 // MoE / PoE aggregation (the alternatives to Eq. 3's max): per-expert
 // log-sum-exp of the contrastive logits c_k = (1 + beta_k) s_k - beta_k s_0,
 // then per vocabulary slice the aggregated score and its best two tokens.
@@ -440,6 +475,11 @@ int adjusted_slice(int V, int n_queries, int num_cus);
 // k_fuse_adjusted (a.nblk slices) then k_fuse_final
 hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_queries, hipStream_t st,
                                 const Timing* tm = nullptr, const Timing* tm_merge = nullptr);
+// k_fuse_scores (a.nblk slices), which also clears p.bins
+hipError_t launch_fuse_scores(const FuseArgs& a, const AdjustArgs& d, const SampleArgs& p, int n_queries, hipStream_t st,
+                              const Timing* tm = nullptr);
+// pced_sample.hip: from the scores to the tokens
+hipError_t launch_sample(const SampleArgs& p, int n_queries, int num_cus, hipStream_t st, const Timing* tm = nullptr);
 hipError_t launch_adjust(const AdjustArgs& a, int n_queries, int max_rows, int num_cus, hipStream_t st);
 // vocabulary tokens per work-group of the stand-alone fuse (1024, or 512 for few queries)
 int fuse_slice(int V, int n_queries, int num_cus);

@@ -2406,8 +2406,10 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a) {
 // of which a history names most, start first. Bound: what a block does one after the
 // other (lists, first rows, sweep, listed tokens), with HBM behind it: 16 queries of 17
 // rows of 151936 tokens, half of them open, 46 us for 166 MB (3.6 TB/s).
-template <bool VEC, int SW>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 ? (VEC ? 3 : 2) : 4))) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
+// STORE: the slice's scores and experts go to scores and who ([query][V]; -inf and 0 where no expert scores
+// the token), and their largest and smallest candidate's score to part.
+template <bool VEC, int SW, bool STORE>
+__device__ __forceinline__ void fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, float* scores, int32_t* who_out) {
 #pragma clang fp contract(off)
   constexpr int RI = SW / 256, NB = 4;
   __shared__ AdjustLds<SW> lds;
@@ -2458,6 +2460,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 
   lists.end(d, vb, lds, [&](int u) {
     const uint32_t bit = 1u << (u & 31);
     if (atomicOr(&tbits[u >> 5], bit) & bit) return;  // (listed before)
+    if (STORE) tbest[u] = 0;
     if (!(open_tokens(d, b, (vb + u) & ~3) >> (u & 3) & 1)) return;
     tlist[atomicAdd(&tcount, 1)] = (uint16_t)u;
     tbest[u] = 0;
@@ -2548,6 +2551,43 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 
     }
   }
   __syncthreads();
+  if constexpr (STORE) {
+    float hi = kNegInf, lo = -kNegInf;
+#pragma unroll
+    for (int i = 0; i < RI; ++i) {
+      const int u = threadIdx.x + 256 * i;
+      float y = sbest[0][u];
+      int k = sk[0][u];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const float yw = sbest[w][u];
+        if (yw > y) { y = yw; k = sk[w][u]; }
+      }
+      if (tbits[u >> 5] >> (u & 31) & 1) {
+        const unsigned long long w = tbest[u];
+        const uint32_t key = (uint32_t)(w >> 32);
+        y = __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+        k = w == 0 ? 0 : (int)~(uint32_t)w;
+      }
+      if (k == 0) y = kNegInf;
+      else { hi = fmaxf(hi, y); lo = fminf(lo, y); }
+      if (vb + u < a.V) {
+        scores[(size_t)b * a.V + vb + u] = y;
+        who_out[(size_t)b * a.V + vb + u] = k;
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) { hi = fmaxf(hi, __shfl_xor(hi, o)); lo = fminf(lo, __shfl_xor(lo, o)); }
+    __shared__ float range[4][2];
+    if (lane == 0) { range[wave][0] = hi; range[wave][1] = lo; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int w = 1; w < 4; ++w) { hi = fmaxf(hi, range[w][0]); lo = fminf(lo, range[w][1]); }
+      *(float2*)(a.part + 2 * ((size_t)b * a.nblk + slice)) = make_float2(hi, lo);
+    }
+    return;
+  }
   Top2 cand{kNegInf, 0x7FFFFFFF, 0, kNegInf, 0x7FFFFFFF};
 #pragma unroll
   for (int i = 0; i < RI; ++i) {
@@ -2580,6 +2620,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 
     p[0] = r.v1; p[1] = __int_as_float(r.i1); p[2] = __int_as_float(r.k1);
     p[3] = r.v2; p[4] = __int_as_float(r.i2);
   }
+}
+
+template <bool VEC, int SW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 ? (VEC ? 3 : 2) : 4))) void k_fuse_adjusted(FuseArgs a, AdjustArgs d) {
+  fuse_adjusted<VEC, SW, false>(a, d, nullptr, nullptr);
+}
+
+// The first launch of pced_sample: scores of every token (see fuse_adjusted). The query's bins start at zero.
+template <bool VEC, int SW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 ? (VEC ? 3 : 2) : 4))) void k_fuse_scores(FuseArgs a, AdjustArgs d, SampleArgs p) {
+  uint4* z = (uint4*)(p.bins + blockIdx.x);
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < (int)(sizeof(SampleBins) / 16); i += 256 * gridDim.y)
+    z[i] = make_uint4(0, 0, 0, 0);
+  fuse_adjusted<VEC, SW, true>(a, d, p.scores, p.who);
 }
 
 // One block per query: merges the vocabulary slices' candidates and writes
@@ -4211,6 +4265,16 @@ hipError_t launch_fuse_adjusted(const FuseArgs& a, const AdjustArgs& d, int n_qu
                   : (vec ? run(k_fuse_adjusted<true, 256>) : run(k_fuse_adjusted<false, 256>));
   if (e != hipSuccess) return e;
   return go(k_fuse_final, dim3(n_queries), dim3(kFuseBlock), 0, st, t0(tm_merge), t1(tm_merge), a);
+}
+
+hipError_t launch_fuse_scores(const FuseArgs& a, const AdjustArgs& d, const SampleArgs& p, int n_queries, hipStream_t st,
+                              const Timing* tm) {
+  const int per = (a.V + a.nblk - 1) / a.nblk;
+  const bool vec = a.V % 4 == 0 && (uintptr_t)a.logits % 16 == 0;
+  auto run = [&](auto kernel) { return go(kernel, dim3(n_queries, a.nblk), dim3(256), 0, st, t0(tm), t1(tm), a, d, p); };
+  return per > 512   ? (vec ? run(k_fuse_scores<true, 1024>) : run(k_fuse_scores<false, 1024>))
+         : per > 256 ? (vec ? run(k_fuse_scores<true, 512>) : run(k_fuse_scores<false, 512>))
+                     : (vec ? run(k_fuse_scores<true, 256>) : run(k_fuse_scores<false, 256>));
 }
 
 hipError_t launch_adjust(const AdjustArgs& a0, int n_queries, int max_rows, int num_cus, hipStream_t st) {

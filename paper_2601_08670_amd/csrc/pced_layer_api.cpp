@@ -188,7 +188,8 @@ pced_status run_attend(pced_ctx* c, AttendArgs a, bool select, hipStream_t st) {
   return PCED_OK;
 }
 
-// The device form of a caller's adjustments
+}  // namespace
+namespace pced {
 pced_status adjust_args(const pced_ctx* c, const pced_adjust* d, AdjustArgs* out) {
   if (!d) return fail(PCED_ERR_INVALID_ARG, "adjust is NULL");
   constexpr int kMaxList = 1 << 30;  // (the kernels' places in a list are 32-bit)
@@ -217,8 +218,7 @@ pced_status adjust_args(const pced_ctx* c, const pced_adjust* d, AdjustArgs* out
   *out = a;
   return PCED_OK;
 }
-
-}  // namespace
+}  // namespace pced
 
 extern "C" {
 

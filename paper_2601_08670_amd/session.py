@@ -71,6 +71,29 @@ class Adjust:
         self.struct = _lib.pced_adjust(mask_row=row, n_history=size("history"), n_bias=size("bias_token"), **ptr)
 
 
+class Sampling:
+    """A batch's sampling settings (pced_sampling) with the device tensors they are in: temperature [B] float32,
+    and optionally top_k [B] int32, top_p and min_p [B] float32."""
+
+    DTYPES = dict(temperature="float32", top_k="int32", top_p="float32", min_p="float32")
+
+    def __init__(self, n_queries, device, **tensors):
+        torch = _torch()
+        unknown = set(tensors) - set(self.DTYPES)
+        if unknown:
+            raise ValueError(f"unknown settings {sorted(unknown)}")
+        self.n_queries, self.device = n_queries, device
+        self.tensors = {k: t for k, t in tensors.items() if t is not None}
+        if "temperature" not in self.tensors:
+            raise ValueError("no temperature")
+        for name, t in self.tensors.items():
+            if t.dtype != getattr(torch, self.DTYPES[name]) or t.shape != (n_queries,) or not t.is_contiguous():
+                raise ValueError(f"{name}: {self.DTYPES[name]} [{n_queries}], contiguous")
+            if t.device != device:
+                raise ValueError(f"{name}: on {t.device}, the session is on {device}")
+        self.struct = _lib.pced_sampling(**{k: t.data_ptr() for k, t in self.tensors.items()})
+
+
 class PcedSession:
     """A context plus its two KV pools for one model geometry and capacity.
 
@@ -366,6 +389,38 @@ class PcedSession:
             out[name] = like(self._out_like[name])
         self.ctx.pced_fuse_adjusted(logits, refresh_beta, self._adjust(adjust), out["tokens"], out)
         return out
+
+    # --------------------------------------------------------------- sampling
+    def sampling(self, **tensors):
+        """The loaded batch's sampling settings (see Sampling) for sample."""
+        return Sampling(self.B, self.device, **tensors)
+
+    def sample(self, logits, sampling, uniform, adjust=None, refresh_beta=False,
+               want=("winner", "score", "logprob", "kept", "beta_used")):
+        """pced_sample: a token per query, drawn with uniform [B] (float32) from [S][V] logits, adjusted if ``adjust``
+        is given, and the wanted outputs."""
+        self._on_device()
+        torch = _torch()
+        self._logits(logits, "logits")
+        if sampling.n_queries != self.B:
+            raise ValueError("the settings are another batch's")
+        if sampling.device != self.device:
+            raise ValueError(f"the settings are on {sampling.device}, the session is on {self.device}")
+        if uniform.dtype != torch.float32 or uniform.shape != (self.B,) or not uniform.is_contiguous():
+            raise ValueError(f"uniform: float32 [{self.B}], contiguous")
+        self._here(uniform, "uniform")
+        out = {"tokens": torch.empty_like(self._out_like["winner"])}
+        for name in want:
+            like = self._SAMPLE_LIKE.get(name)
+            if like is None:
+                raise ValueError(f"unknown output {name}")
+            out[name] = torch.empty_like(self._out_like[like])
+        extra = {name: out[name] for name in want}
+        self.ctx.pced_sample(logits, refresh_beta, None if adjust is None else self._adjust(adjust), sampling.struct,
+                             uniform, out["tokens"], extra)
+        return out
+
+    _SAMPLE_LIKE = dict(winner="winner", score="top1", logprob="top1", kept="winner", beta_used="beta_used")
 
     def lengths(self):
         return self.ctx.pced_get_lengths(self.S)
