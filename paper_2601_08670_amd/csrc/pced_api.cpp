@@ -180,7 +180,7 @@ Layout make_layout(const pced_config& c) {
   // sampling: a query's bins and its list of tokens (scores and experts: the logits' place, which has a
   // row for every query's amateur and one for its first expert)
   L.smp_bins = take(B * sizeof(SampleBins));
-  L.smp_list = take(B * c.vocab * 4);
+  L.smp_list = take(B * c.vocab * 8);
   L.total = o;
   return L;
 }

@@ -206,6 +206,9 @@ struct SampleBins {
   unsigned long long floor_mass;  // of the candidates that min_p keeps
   uint32_t floor_count;
   uint32_t listed;                // tokens in the query's list
+  double rate;                    // log2(e) / T
+  float top;                      // the highest score; -inf: no candidate
+  float inv;                      // bins per unit of score
 };
 static_assert(sizeof(SampleBins) % 16 == 0, "cleared in 16-byte stores");
 struct SampleArgs {
@@ -213,7 +216,7 @@ struct SampleArgs {
   int32_t* who;             // [B][V] the best expert
   const float* part;        // [B][nblk][2] the slices' largest and smallest candidate
   SampleBins* bins;         // [B]
-  int32_t* list;            // [B][V] tokens of the bins that hold a cut
+  unsigned long long* list; // [B][V] scores and tokens of the bins that hold a cut (see order_of)
   const float* temperature; // [B] each; the filters' are optional
   const int32_t* top_k;
   const float* top_p;

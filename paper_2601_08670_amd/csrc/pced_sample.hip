@@ -20,44 +20,11 @@ constexpr int kSampleList = 1024;  // tokens that one block puts in order by com
 
 typedef unsigned long long u64;
 
-// What a query's settings and the range of its scores say
+// A query's softmax: how scores become bins and weights (SampleBins holds it for the later launches)
 struct Softmax {
-  float top;       // the highest score; -inf: no candidate
-  float inv;       // bins per unit of score
-  double rate;     // log2(e) / T
-  double floor;    // the lowest score that min_p keeps
-  bool greedy, has_floor;
+  float top, inv;
+  double rate;
 };
-// by all of the block's threads; ends with a barrier
-template <int NT>
-__device__ __forceinline__ Softmax softmax_of(const SampleArgs& a, int b) {
-  __shared__ float red[2][NT / 64];
-  float hi = kNegInf, lo = -kNegInf;
-  for (int i = threadIdx.x; i < a.nblk; i += NT) {
-    const float2 x = *(const float2*)(a.part + 2 * ((size_t)b * a.nblk + i));
-    hi = fmaxf(hi, x.x);
-    lo = fminf(lo, x.y);
-  }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) { hi = fmaxf(hi, __shfl_xor(hi, o)); lo = fminf(lo, __shfl_xor(lo, o)); }
-  if ((threadIdx.x & 63) == 0) { red[0][threadIdx.x >> 6] = hi; red[1][threadIdx.x >> 6] = lo; }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) { hi = fmaxf(hi, red[0][w]); lo = fminf(lo, red[1][w]); }
-  Softmax s;
-  s.top = hi;
-  const float T = a.temperature[b];
-  s.greedy = !(T > 0.f);
-  s.rate = s.greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)T;
-  // beyond shift + 1 octaves the weights are 0: no need to tell those tokens apart
-  const double reach = (a.shift + 1) / s.rate;
-  const float span = (float)fmin((double)hi - (double)lo, fmin(reach, 3.0e38));
-  s.inv = span > 0.f ? (float)kSampleBins / span : 0.f;  // (NaN where the highest is infinite: 0)
-  const float mp = a.min_p ? a.min_p[b] : 0.f;
-  s.has_floor = mp > 0.f && !s.greedy;
-  s.floor = s.has_floor ? (double)hi + (double)T * log((double)mp) : 0.0;
-  return s;
-}
 // (grows with the distance from the highest score: a product of it with one number)
 __device__ __forceinline__ int bin_of(const Softmax& s, float x) {
   const float d = x == s.top ? 0.f : s.top - x;
@@ -68,33 +35,100 @@ __device__ __forceinline__ u64 weight_of(const Softmax& s, float x, int shift) {
   const double e = shift - ((double)s.top - (double)x) * s.rate;
   return e >= -1.0 ? (u64)rint(exp2(e)) : 0ull;  // (inf - x: 0)
 }
+// A score and its token as a number: fp32 order as unsigned order, and of equal scores the lower token higher
+__device__ __forceinline__ u64 order_of(float x, int v) {
+  const uint32_t u = __float_as_uint(x + 0.f);  // (-0 counts as 0)
+  return (u64)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~v;
+}
+__device__ __forceinline__ float score_in(u64 key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
+}
+__device__ __forceinline__ int token_in(u64 key) { return (int)~(uint32_t)key; }
 
-// A block's part of a query's tokens into the bins: counted in LDS, then added to the query's.
-constexpr int kBinThreads = 512;
+// The tokens of a block's part of a query's row, kTokens per thread at a time, the first of them
+// loaded before anything else: the settings, the slices' ranges and the bins come from other dies'
+// launches, 1 us away, and so do the scores.
+constexpr int kBinThreads = 512, kTokens = 8;
+struct Part {
+  const float* x;
+  int v0, v1;
+  float y[kTokens];
+  __device__ __forceinline__ Part(const SampleArgs& a, int b) {
+    x = a.scores + (size_t)b * a.V;
+    const int per = ((a.V + (int)gridDim.x - 1) / (int)gridDim.x + 3) & ~3;
+    v0 = blockIdx.x * per;
+    v1 = min(a.V, v0 + per);
+    load(v0);
+  }
+  __device__ __forceinline__ int token(int v, int i) const { return v + i * kBinThreads + (int)threadIdx.x; }
+  __device__ __forceinline__ void load(int v) {
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      const int t = token(v, i);
+      y[i] = t < v1 ? x[t] : kNegInf;
+    }
+  }
+};
+
+// A block's part of a query's tokens into the bins: counted in LDS, then added to the query's. Bound: the way of
+// the settings and scores, the atomics' turns in LDS, the flush (16 queries of 151936 tokens: see launch_sample).
 __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
+  constexpr int NW = kBinThreads / 64;
   __shared__ u64 mass[kSampleBins];
   __shared__ uint32_t count[kSampleBins];
+  __shared__ float red[2][NW];
   __shared__ u64 fm;
   __shared__ uint32_t fc;
   const int b = blockIdx.y, tid = threadIdx.x;
-  const int per = ((a.V + (int)gridDim.x - 1) / (int)gridDim.x + 3) & ~3;
-  const int v0 = blockIdx.x * per, v1 = min(a.V, v0 + per);
+  Part part(a, b);
+  const float T = a.temperature[b], mp = a.min_p ? a.min_p[b] : 0.f;
+  float hi = kNegInf, lo = -kNegInf;
+  for (int i = tid; i < a.nblk; i += kBinThreads) {
+    const float2 x = *(const float2*)(a.part + 2 * ((size_t)b * a.nblk + i));
+    hi = fmaxf(hi, x.x);
+    lo = fminf(lo, x.y);
+  }
   for (int i = tid; i < kSampleBins; i += kBinThreads) { mass[i] = 0; count[i] = 0; }
   if (tid == 0) { fm = 0; fc = 0; }
-  const Softmax s = softmax_of<kBinThreads>(a, b);  // (ends with a barrier)
-  const float* x = a.scores + (size_t)b * a.V;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) { hi = fmaxf(hi, __shfl_xor(hi, o)); lo = fminf(lo, __shfl_xor(lo, o)); }
+  if ((tid & 63) == 0) { red[0][tid >> 6] = hi; red[1][tid >> 6] = lo; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { hi = fmaxf(hi, red[0][w]); lo = fminf(lo, red[1][w]); }
+  const bool greedy = !(T > 0.f), has_floor = mp > 0.f && !greedy;
+  Softmax s;
+  s.top = hi;
+  s.rate = greedy ? 1.4426950408889634 : 1.4426950408889634 / (double)T;
+  // beyond shift + 1 octaves the weights are 0: no need to tell those tokens apart
+  const float span = (float)fmin((double)hi - (double)lo, fmin((a.shift + 1) / s.rate, 3.0e38));
+  s.inv = span > 0.f ? (float)kSampleBins / span : 0.f;  // (NaN where the highest is infinite: 0)
+  const double floor = has_floor ? (double)hi + (double)T * log((double)mp) : 0.0;
+  SampleBins* q = a.bins + b;
+  if (blockIdx.x == 0 && tid == 0) {
+    q->rate = s.rate;
+    q->top = s.top;
+    q->inv = s.inv;
+  }
   u64 my_mass = 0;
   uint32_t my_count = 0;
-  for (int v = v0 + tid; v < v1; v += kBinThreads) {
-    const float y = x[v];
-    if (!(y > kNegInf)) continue;
-    const u64 w = weight_of(s, y, a.shift);
-    const int bin = bin_of(s, y);
-    atomicAdd(&count[bin], 1u);
-    if (w) atomicAdd(&mass[bin], w);
-    if (s.has_floor && (double)y >= s.floor) { my_mass += w; ++my_count; }
+  for (int v = part.v0;;) {
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      const float y = part.y[i];
+      if (!(y > kNegInf)) continue;
+      const u64 w = weight_of(s, y, a.shift);
+      const int bin = bin_of(s, y);
+      atomicAdd(&count[bin], 1u);
+      if (w) atomicAdd(&mass[bin], w);
+      if (has_floor && (double)y >= floor) { my_mass += w; ++my_count; }
+    }
+    v += kTokens * kBinThreads;
+    if (v >= part.v1) break;
+    part.load(v);
   }
-  if (s.has_floor) {
+  if (has_floor) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
       my_mass += __shfl_xor(my_mass, o);
@@ -103,7 +137,6 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
     if ((tid & 63) == 0 && my_count) { atomicAdd(&fm, my_mass); atomicAdd(&fc, my_count); }
   }
   __syncthreads();
-  SampleBins* q = a.bins + b;
   for (int i = tid; i < kSampleBins; i += kBinThreads) {
     if (!count[i]) continue;
     atomicAdd(&q->count[i], count[i]);
@@ -141,119 +174,170 @@ __device__ __forceinline__ int bin_at(const Sums& s, double t) {
   }
   return lo;
 }
-// by all of the block's threads
+// By all of the block's threads: each has PER neighbouring bins, and the one whose bin a cut falls into says so.
 template <int NT>
-__device__ __forceinline__ Cuts cuts_of(const SampleArgs& a, int b, Sums& s) {
-  constexpr int PER = kSampleBins / NT;
+struct Scan {
+  static constexpr int PER = kSampleBins / NT;
   static_assert(PER * NT == kSampleBins, "");
-  __shared__ u64 wm[NT / 64];
-  __shared__ uint32_t wc[NT / 64];
-  __shared__ Cuts cuts;
-  const SampleBins* q = a.bins + b;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  u64 m[PER], ms = 0;
-  uint32_t n[PER], ns = 0;
+  u64 m[PER];
+  uint32_t n[PER];
+  Softmax s;
+  float T, p, mp, u;
+  int k;
+  u64 floor_mass;
+  uint32_t floor_count;
+  // the loads, ahead of everything else
+  __device__ __forceinline__ Scan(const SampleArgs& a, int b) {
+    const SampleBins* q = a.bins + b;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) { m[i] = q->mass[PER * tid + i]; n[i] = q->count[PER * tid + i]; }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) { ms += m[i]; ns += n[i]; }
-  u64 rm = ms;
-  uint32_t rn = ns;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 x = __shfl_up(rm, o);
-    const uint32_t y = (uint32_t)__shfl_up((int)rn, o);
-    if (lane >= o) { rm += x; rn += y; }
+    for (int i = 0; i < PER; ++i) { m[i] = q->mass[PER * threadIdx.x + i]; n[i] = q->count[PER * threadIdx.x + i]; }
+    s = Softmax{q->top, q->inv, q->rate};
+    floor_mass = q->floor_mass;
+    floor_count = q->floor_count;
+    T = a.temperature[b];
+    k = a.top_k ? a.top_k[b] : 0;
+    p = a.top_p ? a.top_p[b] : 1.f;
+    mp = a.min_p ? a.min_p[b] : 0.f;
+    u = a.uniform[b];
   }
-  if (lane == 63) { wm[wave] = rm; wc[wave] = rn; }
-  __syncthreads();
+  __device__ __forceinline__ Cuts cuts(const SampleArgs& a, Sums& sums) {
+    __shared__ u64 wm[NT / 64];
+    __shared__ uint32_t wc[NT / 64];
+    __shared__ int s_bk, s_p0, s_p1, s_t0, s_t1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    u64 ms = 0;
+    uint32_t ns = 0;
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w)
-    if (w < wave) { rm += wm[w]; rn += wc[w]; }
-  rm -= ms;
-  rn -= ns;
+    for (int i = 0; i < PER; ++i) { ms += m[i]; ns += n[i]; }
+    u64 rm = ms;
+    uint32_t rn = ns;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    s.mass[PER * tid + i] = rm;
-    s.count[PER * tid + i] = rn;
-    rm += m[i];
-    rn += n[i];
-  }
-  if (tid == NT - 1) { s.mass[kSampleBins] = rm; s.count[kSampleBins] = rn; }
-  __syncthreads();
-  if (tid == 0) {
-    Cuts c;
-    const uint32_t N = s.count[kSampleBins];
-    const float T = a.temperature[b];
+    for (int o = 1; o < 64; o <<= 1) {
+      const u64 x = __shfl_up(rm, o);
+      const uint32_t y = (uint32_t)__shfl_up((int)rn, o);
+      if (lane >= o) { rm += x; rn += y; }
+    }
+    if (lane == 63) { wm[wave] = rm; wc[wave] = rn; }
+    __syncthreads();
+    u64 M = 0;
+    uint32_t N = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < wave) { rm += wm[w]; rn += wc[w]; }
+      M += wm[w];
+      N += wc[w];
+    }
+    u64 at_m[PER + 1];
+    uint32_t at_n[PER + 1];
+    at_m[0] = rm - ms;
+    at_n[0] = rn - ns;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      at_m[i + 1] = at_m[i] + m[i];
+      at_n[i + 1] = at_n[i] + n[i];
+      sums.mass[PER * tid + i] = at_m[i];
+      sums.count[PER * tid + i] = at_n[i];
+    }
+    if (tid == 0) { sums.mass[kSampleBins] = M; sums.count[kSampleBins] = N; }
     const bool greedy = !(T > 0.f);
-    const int k = a.top_k ? a.top_k[b] : 0;
-    const float mp = a.min_p ? a.min_p[b] : 0.f;
+    Cuts c;
     c.none = N == 0;
     c.n_k = greedy ? 1u : k > 0 ? min((uint32_t)k, N) : N;
-    c.p = a.top_p ? a.top_p[b] : 1.f;
-    c.has_p = c.p < 1.f && !greedy;
-    c.p = fmaxf(c.p, 0.f);
-    const float u = a.uniform[b];
+    c.has_p = p < 1.f && !greedy;
+    c.p = fmaxf(p, 0.f);
     c.u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
     c.has_floor = mp > 0.f && !greedy;
-    c.floor_count = max(q->floor_count, 1u);          // the highest stays whatever min_p says
-    c.floor_mass = max(q->floor_mass, (u64)1 << a.shift);
-    int lo = 0, hi = kSampleBins - 1;                  // the bin of rank n_k - 1
-    while (lo < hi) {
-      const int x = (lo + hi) >> 1;
-      if (s.count[x + 1] >= c.n_k) hi = x;
-      else lo = x + 1;
-    }
-    c.bk = lo;
-    // all of the bin, or a bin without weight: its sum is known
-    c.k_open = s.count[lo + 1] != c.n_k && s.mass[lo] != s.mass[lo + 1];
-    c.mass_k = s.count[lo + 1] == c.n_k ? s.mass[lo + 1] : s.mass[lo];
-    const u64 k0 = c.k_open ? s.mass[lo] : c.mass_k, k1 = c.k_open ? s.mass[lo + 1] : c.mass_k;
-    u64 m0 = k0, m1 = k1;                              // what is kept weighs between these
+    c.floor_count = max(floor_count, 1u);              // the highest stays whatever min_p says
+    c.floor_mass = max(floor_mass, (u64)1 << a.shift);
+    c.bk = c.t0 = c.t1 = 0;
     c.p0 = 1;
     c.p1 = 0;
+    c.k_open = false;
+    c.mass_k = 0;
+    if (c.none) {  // uniform
+      __syncthreads();
+      return c;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)                      // the bin of rank n_k - 1
+      if (at_n[i] < c.n_k && c.n_k <= at_n[i + 1]) s_bk = PER * tid + i;
+    __syncthreads();
+    c.bk = s_bk;
+    const u64 b0 = sums.mass[c.bk], b1 = sums.mass[c.bk + 1];
+    const bool whole = sums.count[c.bk + 1] == c.n_k;
+    // all of the bin, or a bin without weight: its sum is known
+    c.k_open = !whole && b0 != b1;
+    c.mass_k = whole ? b1 : b0;
+    const u64 k0 = c.k_open ? b0 : c.mass_k, k1 = c.k_open ? b1 : c.mass_k;
+    u64 m0 = k0, m1 = k1;                              // what is kept weighs between these
     if (c.has_p) {
-      c.p0 = bin_at<false>(s, (double)c.p * (double)k0);
-      c.p1 = bin_at<false>(s, (double)c.p * (double)k1);
-      m0 = min(m0, s.mass[c.p0]);
-      m1 = min(m1, s.mass[c.p1 + 1]);
+      const double t0 = (double)c.p * (double)k0, t1 = (double)c.p * (double)k1;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const double x = (double)at_m[i], y = (double)at_m[i + 1];
+        const bool first = i == 0 && tid == 0;
+        if (y >= t0 && (x < t0 || first)) s_p0 = PER * tid + i;
+        if (y >= t1 && (x < t1 || first)) s_p1 = PER * tid + i;
+      }
+      __syncthreads();
+      c.p0 = s_p0;
+      c.p1 = s_p1;
+      m0 = min(m0, sums.mass[c.p0]);
+      m1 = min(m1, sums.mass[c.p1 + 1]);
     }
     if (c.has_floor) { m0 = min(m0, c.floor_mass); m1 = min(m1, c.floor_mass); }
-    c.t0 = bin_at<true>(s, (double)c.u * (double)m0);
-    c.t1 = bin_at<true>(s, (double)c.u * (double)m1);
-    cuts = c;
+    const double t0 = (double)c.u * (double)m0, t1 = (double)c.u * (double)m1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const double x = (double)at_m[i], y = (double)at_m[i + 1];
+      if (x <= t0 && t0 < y) s_t0 = PER * tid + i;
+      if (x <= t1 && t1 < y) s_t1 = PER * tid + i;
+    }
+    __syncthreads();
+    c.t0 = s_t0;
+    c.t1 = s_t1;
+    return c;
   }
-  __syncthreads();
-  return cuts;
-}
+};
 
 // The tokens of the bins that hold a cut or the token, in any order.
 __global__ __launch_bounds__(kBinThreads) void k_sample_list(SampleArgs a) {
   __shared__ Sums sums;
+  __shared__ uint32_t s_n, s_base;
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-  const int per = ((a.V + (int)gridDim.x - 1) / (int)gridDim.x + 3) & ~3;
-  const int v0 = blockIdx.x * per, v1 = min(a.V, v0 + per);
-  if (v0 >= v1) return;
-  const Softmax s = softmax_of<kBinThreads>(a, b);
-  const Cuts c = cuts_of<kBinThreads>(a, b, sums);
+  Part part(a, b);
+  Scan<kBinThreads> scan(a, b);
+  const Softmax s = scan.s;
+  const Cuts c = scan.cuts(a, sums);
   if (c.none) return;
-  const float* x = a.scores + (size_t)b * a.V;
-  for (int v = v0 + tid; v - tid < v1; v += kBinThreads) {
-    const float y = v < v1 ? x[v] : kNegInf;
-    const bool mine = y > kNegInf && wanted(c, bin_of(s, y));
-    const u64 m = __ballot(mine);
-    if (!m) continue;
+  for (int v = part.v0; v < part.v1; v += kTokens * kBinThreads) {
+    if (v > part.v0) part.load(v);
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    // a place in the list per wave and block: one global atomic, 1 us and more away
+    u64 m[kTokens];
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      const float y = part.y[i];
+      m[i] = __ballot(y > kNegInf && wanted(c, bin_of(s, y)));
+      mine += (uint32_t)__popcll(m[i]);
+    }
     uint32_t at = 0;
-    if (lane == 0) at = atomicAdd(&a.bins[b].listed, (uint32_t)__popcll(m));
-    at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
-    if (mine) a.list[(size_t)b * a.V + at + __popcll(m & (((u64)1 << lane) - 1))] = v;
+    if (lane == 0 && mine) at = atomicAdd(&s_n, mine);
+    __syncthreads();
+    if (tid == 0 && s_n) s_base = atomicAdd(&a.bins[b].listed, s_n);
+    __syncthreads();
+    if (mine) {
+      at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + s_base;
+      u64* list = a.list + (size_t)b * a.V;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) {
+        if (m[i] >> lane & 1) list[at + __popcll(m[i] & (((u64)1 << lane) - 1))] = order_of(part.y[i], part.token(v, i));
+        at += (uint32_t)__popcll(m[i]);
+      }
+    }
   }
-}
-
-// fp32 order as unsigned order, and of equal scores the lower token higher
-__device__ __forceinline__ u64 order_of(float x, int v) {
-  const uint32_t u = __float_as_uint(x + 0.f);  // (-0 counts as 0)
-  return (u64)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~v;
 }
 
 constexpr int kTokenThreads = 1024;
@@ -265,22 +349,18 @@ struct Found {
 // Long lists: the token of bin `bin` at which the count reaches r (1 on; MODE 0), or the sum reaches (1) or
 // passes (2) t, by its key's digits from the highest on, those that all of the bin's keys share left out.
 template <int MODE>
-__device__ __forceinline__ Found search(const SampleArgs& a, int b, const Softmax& s, const Sums& sums, int n, int bin,
-                                        uint32_t r, double t) {
+__device__ __forceinline__ Found search(const SampleArgs& a, const u64* list, const Softmax& s, const Sums& sums, int n,
+                                        int bin, uint32_t r, double t) {
   __shared__ u64 hm[256], s_key[2];
   __shared__ uint32_t hc[256];
   __shared__ int s_digit;
   const int tid = threadIdx.x;
-  const float* x = a.scores + (size_t)b * a.V;
-  const int32_t* list = a.list + (size_t)b * a.V;
   if (tid == 0) { s_key[0] = ~(u64)0; s_key[1] = 0; }
   __syncthreads();
   u64 all = ~(u64)0, any = 0;
   for (int i = tid; i < n; i += kTokenThreads) {
-    const int v = list[i];
-    const float y = x[v];
-    if (bin_of(s, y) != bin) continue;
-    const u64 k = order_of(y, v);
+    const u64 k = list[i];
+    if (bin_of(s, score_in(k)) != bin) continue;
     all &= k;
     any |= k;
   }
@@ -294,10 +374,9 @@ __device__ __forceinline__ Found search(const SampleArgs& a, int b, const Softma
     for (int i = tid; i < 256; i += kTokenThreads) { hm[i] = 0; hc[i] = 0; }
     __syncthreads();
     for (int i = tid; i < n; i += kTokenThreads) {
-      const int v = list[i];
-      const float y = x[v];
+      const u64 k = list[i];
+      const float y = score_in(k);
       if (bin_of(s, y) != bin) continue;
-      const u64 k = order_of(y, v);
       if (sh < 56 && (k >> (sh + 8)) != (f.key >> (sh + 8))) continue;
       atomicAdd(&hc[k >> sh & 255], 1u);
       atomicAdd(&hm[k >> sh & 255], weight_of(s, y, a.shift));
@@ -337,34 +416,46 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
   __shared__ Sums sums;
   __shared__ u64 key[kSampleList], weight[kSampleList];
   __shared__ uint16_t bins[kSampleList];
-  __shared__ u64 s_mass_k, s_p_mass, s_mass;
-  __shared__ uint32_t s_p_count, s_count;
+  __shared__ u64 s_mass_k, s_p_mass;
+  __shared__ uint32_t s_p_count;
   const int b = blockIdx.x, tid = threadIdx.x;
+  const u64* list = a.list + (size_t)b * a.V;
+  const int n = (int)a.bins[b].listed;
+  const u64 entry = tid < a.V ? list[tid] : 0;  // (as far as it is one)
+  Scan<kTokenThreads> scan(a, b);
   if (a.beta_used) {
     const int e1 = a.query_exp0[b + 1];
     for (int e = a.query_exp0[b] + tid; e < e1; e += kTokenThreads) a.beta_used[e] = a.beta[e];
   }
-  const Softmax s = softmax_of<kTokenThreads>(a, b);
-  const Cuts c = cuts_of<kTokenThreads>(a, b, sums);
-  const float* x = a.scores + (size_t)b * a.V;
-  auto write = [&](int v, uint32_t kept, u64 mass) {  // one thread
-    const float y = v >= 0 ? x[v] : kNegInf;
+  const Softmax s = scan.s;
+  const bool few = n <= kSampleList;
+  const float y = score_in(entry);
+  int bin = -1;
+  u64 w = 0;
+  if (few && tid < n) {
+    bin = bin_of(s, y);
+    w = weight_of(s, y, a.shift);
+    key[tid] = entry;
+    weight[tid] = w;
+    bins[tid] = (uint16_t)bin;
+  }
+  const Cuts c = scan.cuts(a, sums);  // (ends with a barrier)
+  auto write = [&](int v, float x, uint32_t kept, u64 mass) {  // one thread
     a.tokens_out[b] = v;
     a.prev_tok[b] = v;
     if (a.winner) a.winner[b] = v >= 0 ? a.who[(size_t)b * a.V + v] : 0;
-    if (a.score) a.score[b] = y;
+    if (a.score) a.score[b] = x;
     if (a.kept) a.kept[b] = (int32_t)kept;
     if (a.logprob) {
       // ln of the weight over the sum: the weight's exponent as it is, not as rounded to 2^-shift
-      const double z = y == s.top ? 0.0 : ((double)y - (double)s.top) * s.rate;
+      const double z = x == s.top ? 0.0 : ((double)x - (double)s.top) * s.rate;
       a.logprob[b] = v >= 0 ? (float)((z - (log2((double)mass) - a.shift)) * 0.6931471805599453) : kNegInf;
     }
   };
   if (c.none) {
-    if (tid == 0) write(-1, 0, 0);
+    if (tid == 0) write(-1, kNegInf, 0, 0);
     return;
   }
-  const int n = (int)a.bins[b].listed;
   // what all three filters keep, once top_k's sum and top_p's cut are known
   auto keep = [&](u64 mass_k, uint32_t p_count, u64 p_mass, uint32_t* count, u64* mass) {
     *count = c.n_k;
@@ -372,64 +463,62 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
     if (c.has_p && p_count < *count) { *count = p_count; *mass = p_mass; }
     if (c.has_floor && c.floor_count < *count) { *count = c.floor_count; *mass = c.floor_mass; }
   };
-  if (n > kSampleList) {
+  uint32_t count;
+  u64 mass;
+  if (!few) {
     u64 mass_k = c.mass_k;
     if (c.k_open) {
-      const Found f = search<0>(a, b, s, sums, n, c.bk, c.n_k, 0.0);
-      mass_k = f.mass + weight_of(s, x[(int)~(uint32_t)f.key], a.shift);
+      const Found f = search<0>(a, list, s, sums, n, c.bk, c.n_k, 0.0);
+      mass_k = f.mass + weight_of(s, score_in(f.key), a.shift);
     }
-    uint32_t p_count = 0, count;
-    u64 p_mass = 0, mass;
+    uint32_t p_count = 0;
+    u64 p_mass = 0;
     if (c.has_p) {
       const double t = (double)c.p * (double)mass_k;
-      const Found f = search<1>(a, b, s, sums, n, bin_at<false>(sums, t), 0, t);
+      const Found f = search<1>(a, list, s, sums, n, bin_at<false>(sums, t), 0, t);
       p_count = f.rank + 1;
-      p_mass = f.mass + weight_of(s, x[(int)~(uint32_t)f.key], a.shift);
+      p_mass = f.mass + weight_of(s, score_in(f.key), a.shift);
     }
     keep(mass_k, p_count, p_mass, &count, &mass);
     const double t = (double)c.u * (double)mass;
-    const Found f = search<2>(a, b, s, sums, n, bin_at<true>(sums, t), 0, t);
-    if (tid == 0) write((int)~(uint32_t)f.key, count, mass);
+    const Found f = search<2>(a, list, s, sums, n, bin_at<true>(sums, t), 0, t);
+    if (tid == 0) write(token_in(f.key), score_in(f.key), count, mass);
     return;
   }
-  int v = -1, bin = -1;
-  u64 mine = 0, w = 0;
-  if (tid < n) {
-    v = a.list[(size_t)b * a.V + tid];
-    const float y = x[v];
-    bin = bin_of(s, y);
-    key[tid] = mine = order_of(y, v);
-    weight[tid] = w = weight_of(s, y, a.shift);
-    bins[tid] = (uint16_t)bin;
-  }
-  __syncthreads();
-  // the tokens before each: those of the bins before, and those of its bin with a higher key
-  u64 before = 0;
+  // The tokens before each: those of the bins before, and those of its bin with a higher key. 2^lg
+  // neighbouring threads take a token together.
+  int lg = 0;
+  while (lg < 6 && (n << (lg + 1)) <= kTokenThreads) ++lg;
+  const int i = tid >> lg, step = 1 << lg;
+  u64 before = 0, mine = 0;
   uint32_t rank = 0;
-  if (tid < n) {
-    before = sums.mass[bin];
-    rank = sums.count[bin];
-    for (int j = 0; j < n; ++j)
+  if (i < n) {
+    mine = key[i];
+    bin = bins[i];
+    for (int j = tid & (step - 1); j < n; j += step)
       if (bins[j] == bin && key[j] > mine) { before += weight[j]; ++rank; }
+  }
+  for (int o = 1; o < step; o <<= 1) {
+    before += __shfl_xor(before, o);
+    rank += (uint32_t)__shfl_xor((int)rank, o);
+  }
+  const bool one = i < n && (tid & (step - 1)) == 0;
+  if (one) {
+    w = weight[i];
+    before += sums.mass[bin];
+    rank += sums.count[bin];
     if (c.k_open && rank + 1 == c.n_k) s_mass_k = before + w;
   }
   __syncthreads();
   const u64 mass_k = c.k_open ? s_mass_k : c.mass_k;
-  if (tid < n && c.has_p) {
+  if (c.has_p) {  // uniform
     const double t = (double)c.p * (double)mass_k;
-    if ((double)(before + w) >= t && ((double)before < t || rank == 0)) { s_p_count = rank + 1; s_p_mass = before + w; }
+    if (one && (double)(before + w) >= t && ((double)before < t || rank == 0)) { s_p_count = rank + 1; s_p_mass = before + w; }
+    __syncthreads();
   }
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t count;
-    u64 mass;
-    keep(mass_k, s_p_count, s_p_mass, &count, &mass);
-    s_count = count;
-    s_mass = mass;
-  }
-  __syncthreads();
-  const double t = (double)c.u * (double)s_mass;
-  if (tid < n && (double)before <= t && t < (double)(before + w)) write(v, s_count, s_mass);
+  keep(mass_k, s_p_count, s_p_mass, &count, &mass);
+  const double t = (double)c.u * (double)mass;
+  if (one && (double)before <= t && t < (double)(before + w)) write(token_in(mine), score_in(mine), count, mass);
 }
 
 }  // namespace

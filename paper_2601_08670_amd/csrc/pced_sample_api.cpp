@@ -42,7 +42,7 @@ pced_status pced_sample(pced_ctx* c, const float* logits, int32_t refresh_beta, 
   a.who = (int32_t*)(a.scores + (size_t)c->B * V);
   a.part = f.part;
   a.bins = c->at<SampleBins>(c->lay.smp_bins);
-  a.list = c->at<int32_t>(c->lay.smp_list);
+  a.list = c->at<unsigned long long>(c->lay.smp_list);
   a.temperature = sampling->temperature;
   a.top_k = sampling->top_k;
   a.top_p = sampling->top_p;

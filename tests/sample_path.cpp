@@ -21,7 +21,7 @@ hipError_t launch_fuse_scores(const FuseArgs& a, const AdjustArgs& d, const Samp
   const size_t n = (size_t)B * p.V * 4;
   return note("fuse_scores", a.nblk, d.mask != nullptr, inside(p.scores, n, l.logits, l.rho), inside(p.who, n, l.logits, l.rho),
               (char*)p.scores + n <= (char*)p.who, inside(p.bins, B * sizeof(SampleBins), l.smp_bins, l.smp_list),
-              inside(p.list, n, l.smp_list, l.total), inside(p.part, (size_t)B * a.nblk * 8, l.fuse_part, l.lse_part));
+              inside(p.list, 2 * n, l.smp_list, l.total), inside(p.part, (size_t)B * a.nblk * 8, l.fuse_part, l.lse_part));
 }
 hipError_t launch_sample(const SampleArgs& p, int B, int, hipStream_t, const Timing*) {
   return note("sample", B, p.shift, p.nblk, p.top_k != nullptr, p.kept != nullptr);
