@@ -3,6 +3,8 @@
 #include "pced_code8.h"
 #include "pced_device.h"
 
+#include <type_traits>
+
 namespace pced {
 namespace {
 
@@ -113,28 +115,69 @@ constexpr float kLowest8 = -3.402823466e38f;  // the softmax's first reference (
 struct Item8 {
   int s, h, l, tok0, nt, len;  // nt new tokens from tok0 on; len: tokens before the call's
 };
-__device__ __forceinline__ Item8 item8(const Attend8Args& a, uint32_t item) {
+// group i of sequence s, and the (layer, kv-head) number lh of the launch
+__device__ __forceinline__ Item8 item8(const Attend8Args& a, int s, int i, uint32_t lh) {
   Item8 r;
-  r.h = item % (uint32_t)a.n_kv_heads;
-  item /= (uint32_t)a.n_kv_heads;
+  r.s = s;
   r.l = 0;
+  r.h = lh;
   if (a.launch_layers > 1) {
-    r.l = item % (uint32_t)a.launch_layers;
-    item /= (uint32_t)a.launch_layers;
+    r.l = lh / (uint32_t)a.n_kv_heads;
+    r.h = lh - r.l * a.n_kv_heads;
   }
-  const uint32_t g = item + a.group0;
-  r.s = g;
-  r.tok0 = 0;
-  if (a.seq_groups > 1) {
-    r.s = g / (uint32_t)a.seq_groups;
-    r.tok0 = (g - r.s * a.seq_groups) * a.gt;
-  }
+  r.tok0 = i * a.gt;
   r.nt = min(a.gt, a.n_tokens - r.tok0);
-  r.len = a.len0[r.s] + a.t;
+  r.len = a.len0[s] + a.t;
   return r;
 }
 // pages that an item's tokens see
 __device__ __forceinline__ int pages8(const Item8& it) { return (it.len + it.tok0 + it.nt - 1) / kPage + 1; }
+// pages of a part of sequence s: as few parts as a.part_pages allows, of equal length
+__device__ __forceinline__ int part8(const Attend8Args& a, int s) {
+  const int pages = (a.len0[s] + a.t + a.n_tokens - 1) / kPage + 1, n = (pages + a.part_pages - 1) / a.part_pages;
+  return (pages + n - 1) / n;
+}
+
+// The item and part of a block. Only parts that some token sees have blocks: the sequences' lengths are far
+// apart, and blocks without work would take turns with the others and leave the eight dies uneven shares. A wave
+// counts the sequences' parts, 64 sequences at a time, up to the block's. Work-groups go to the dies in turn; the
+// token groups of one (sequence, part, layer, kv-head) go to one die and follow each other there, so that its L2 has
+// their pages.
+__device__ __forceinline__ bool block8(const Attend8Args& a, Item8& it, uint32_t& item, int& part) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t heads = (uint32_t)a.launch_layers * a.n_kv_heads;
+  uint32_t u = blockIdx.x, i = 0;
+  if (a.n_groups > 1) {
+    const uint32_t r = u >> 3, k = r / (uint32_t)a.n_groups;
+    i = r - k * a.n_groups;
+    u = (u & 7) + 8 * k;
+  }
+  const uint32_t sp = u / heads, lh = u - sp * heads;
+  if (sp >= (uint32_t)a.seq_parts) return false;
+  int s = sp, before = 0;
+  part = 0;
+  for (int base = 0; a.seq_parts > a.launch_seqs; base += 64) {  // (sp is below the sum of all)
+    int n = 0;
+    if (base + lane < a.launch_seqs) {
+      const int pages = (a.len0[a.seq0 + base + lane] + a.t + a.n_tokens - 1) / kPage + 1;
+      n = (pages + a.part_pages - 1) / a.part_pages;
+    }
+    int run = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(run, o); if (lane >= o) run += x; }
+    const uint64_t past = __ballot((int)sp < before + run);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      s = base + at;
+      part = (int)sp - before - __builtin_amdgcn_readlane(run, at) + __builtin_amdgcn_readlane(n, at);
+      break;
+    }
+    before += __builtin_amdgcn_readlane(run, 63);
+  }
+  item = ((uint32_t)s * a.n_groups + i) * heads + lh;
+  it = item8(a, a.seq0 + s, a.group0 + i, lh);
+  return true;
+}
 
 // Where query row (token i of the group, q-head g) begins in q and x, in elements
 __device__ __forceinline__ size_t qrow8(const Attend8Args& a, const Item8& it, int i, int g, int D) {
@@ -146,185 +189,98 @@ __device__ __forceinline__ void store_x4_bf16(void* x, size_t at, f32x4 o) {
   *(uint2*)((uint16_t*)x + at) = make_uint2(__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q));
 }
 
+__device__ __forceinline__ f16x8 join8h(uint2 a, uint2 b) { return __builtin_bit_cast(f16x8, u32x4{a.x, a.y, b.x, b.y}); }
+__device__ __forceinline__ float lane_f(float x, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+// Powers of two that put the largest of a wave's V scales (a lane's is the upper half of `scale`) into [2^6, 2^7), and back
+struct VScale {
+  float down, up;
+  __device__ __forceinline__ explicit VScale(uint32_t scale) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) scale = max(scale, (uint32_t)__shfl_xor((int)scale, o));
+    const uint32_t e = max(__builtin_amdgcn_readfirstlane((int)scale) >> 23, 18);  // (scales are 2^-109 to 2^120)
+    down = __builtin_bit_cast(float, (260 - e) << 23);
+    up = __builtin_bit_cast(float, (e - 6) << 23);
+  }
+};
+
 __device__ __forceinline__ bf16x8 join8(uint2 a, uint2 b) { return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y}); }
 
-// One block of 4 waves per (item, part of its pages): as k_attend, but the columns of both
-// products are the q-heads of a kv-head for up to 16 NC / G new tokens, so that those share
-// a page's way into registers, and the pages come as codes: a page's K product is summed over
-// codes and then scaled, its softmax weights are scaled by V's scale before they meet V's codes. Codes
-// are exact in bf16, so nothing is rounded on the way that k_attend does not round.
-// The pages that were complete before the call lie before every new token: no mask. The pages
-// behind them are 16-bit tiles, one at a time, masked by each column's own position. There, V of tokens behind
-// the group's last counts as 0 (unwritten rows hold anything); V of the group's own later
-// tokens is written, but may be inf or NaN, whose product with a weight of 0 is not 0: if it is,
-// the page is taken token by token.
-template <int CODE, int D, int NC>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NC == 1 ? 2 : 1, 4))) void k_attend8(Attend8Args a) {
-  constexpr int NU = D / 32, NW = D / 64, NJ = D / 16;  // 16-bit units, code units, 16-dim output blocks
-  constexpr int DP = D + 4;
-  __shared__ __align__(16) float sacc[4][16 * NC][DP];
-  __shared__ float sm[4][16 * NC], sl[4][16 * NC];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 15, quad = lane >> 4;
-  // Work-groups go to the eight dies in turn. The token groups of one (sequence, layer, kv-head) go to
-  // one die and follow each other there: its L2 then has the pages.
-  uint32_t item, part;
-  if (a.seq_groups == 1) {
-    item = blockIdx.x / (uint32_t)a.parts;
-    part = blockIdx.x - item * a.parts;
-  } else {
-    const uint32_t s0 = (uint32_t)a.group0 / a.seq_groups, per = (uint32_t)a.seq_groups * a.parts;
-    const uint32_t r = blockIdx.x >> 3, k = r / per, rest = r - k * per;
-    const uint32_t pair = (blockIdx.x & 7) + 8 * k;  // (layer, kv-head, sequence)
-    const uint32_t heads = (uint32_t)a.launch_layers * a.n_kv_heads;
-    const uint32_t lh = pair / a.launch_seqs, s = pair - lh * a.launch_seqs;
-    part = rest / a.seq_groups;
-    const uint32_t i = rest - part * a.seq_groups, g = (s0 + s) * a.seq_groups + i - a.group0;
-    if (lh >= heads || g >= (uint32_t)a.n_groups) return;
-    item = g * heads + lh;
-  }
-  const Item8 it = item8(a, item);
-  const int total = pages8(it), full = it.len / kPage;
-  const int c0 = part * a.part_pages, c1 = min(total, c0 + a.part_pages);
-  if (c0 >= c1) return;
-  const int G = a.group, cols = it.nt * G;
-  const int layer = a.layer + it.l;
-  const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
-  const int cnt = min(c1, full) - c0;  // pages of codes (<= 0: none)
-  // the wave's u-th page of codes is page u / 2 * 8 + 2 wave + u % 2 of the part; ids and scales one per lane
-  const int my_page = c0 + min(lane / 2 * 8 + 2 * wave + lane % 2, max(cnt, 1) - 1);
-  const int my_phys = max(pt[my_page], 0);
-  const uint32_t my_scale = cnt > 0 ? a.c.scales[((size_t)layer * a.n_kv_heads + it.h) * a.c.max_pages + my_phys] : 0u;
+// A wave's part of an item: NC tiles of 16 columns (a column is a q-head of one of the group's new tokens), each
+// with an online softmax. As in k_attend the products are
+//   S^T[16 tok x 16 cols] = K[16 x D] Q^T,   O^T[D x 16 cols] += V^T[D x tok] P^T,
+// and the softmax's reference (in log2 units) moves only when a score exceeds it by 8, so that weights stay within
+// 2^8. Codes are exact in bf16 and in fp16: a page's K product is summed over codes and scaled behind; its softmax
+// weights are scaled by V's scale and rounded to fp16 (relative error 2^-11, an eighth of a bf16 result's own) before they
+// meet V's codes. Powers of two keep the weights in fp16's range: the largest V scale of the wave's pages counts as
+// 2^6 to 2^7, so that a weight is below 2^15, and what is lost below 2^-14 is at most 2^-31 of that page's V.
+// (As the sum of two bf16, with twice the products, a question of 24 tokens took 111 us instead of 94.)
+template <int D, int NC>
+struct Columns {
+  static constexpr int NU = D / 32, NJ = D / 16;  // 16-byte units of a bf16 tile per lane, 16-dim output blocks
   u32x4 q[NC][NU];
-  int lim[NC];  // the column's own position
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const int cc = min(16 * n + col, cols - 1), i = cc / G;
-    const uint16_t* row = (const uint16_t*)a.q + qrow8(a, it, i, cc - i * G, D) + 8 * quad;
-    lim[n] = it.len + it.tok0 + i;
-#pragma unroll
-    for (int u = 0; u < NU; ++u) q[n][u] = *(const u32x4*)(row + 32 * u);
-  }
   f32x4 acc[NC][NJ];
   float m[NC], lsum[NC];
+  int lim[NC];  // the column's own position
+  __device__ __forceinline__ void begin(const Attend8Args& a, const Item8& it) {
+    const int col = threadIdx.x & 15, quad = (threadIdx.x & 63) >> 4, G = a.group;
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    m[n] = kLowest8;
-    lsum[n] = 0.f;
+    for (int n = 0; n < NC; ++n) {
+      const int cc = min(16 * n + col, it.nt * G - 1), i = cc / G;
+      const uint16_t* row = (const uint16_t*)a.q + qrow8(a, it, i, cc - i * G, D) + 8 * quad;
+      lim[n] = it.len + it.tok0 + i;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < NU; ++u) q[n][u] = *(const u32x4*)(row + 32 * u);
+      m[n] = kLowest8;
+      lsum[n] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
   }
-  // moves column tile n's reference where a score exceeds it by `lead`
-  auto refer = [&](int n, float top) __attribute__((always_inline)) {
-    if (__any(top > m[n] + a.lead)) {
+  __device__ __forceinline__ void refer(int n, float top) {
+    if (__any(top > m[n] + 8.f)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m[n], top), alpha = m[n] == mn ? 1.f : __builtin_amdgcn_exp2f((m[n] - mn) * a.scale_log2);
+      const float mn = fmaxf(m[n], top), alpha = m[n] == mn ? 1.f : __builtin_amdgcn_exp2f(m[n] - mn);
       m[n] = mn;
       lsum[n] *= alpha;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[n][j] *= alpha;
     }
-  };
-
-  // ------------------------------------------------ pages of codes, two at a time
-  struct Regs {
-    u32x4 k[2][NW], v[2][NW];
-  };
-  const size_t tile = (size_t)kPage * D;
-  auto load = [&](int u, Regs& r) __attribute__((always_inline)) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const size_t at = (((size_t)layer * a.c.max_pages + __builtin_amdgcn_readlane(my_phys, u + b)) * a.n_kv_heads + it.h) * tile;
-      const u32x4* kp = (const u32x4*)(a.c.k_codes + at) + lane;
-      const u32x4* vp = (const u32x4*)(a.c.v_codes + at) + lane;
-#pragma unroll
-      for (int j = 0; j < NW; ++j) r.k[b][j] = kp[64 * j];
-#pragma unroll
-      for (int j = 0; j < NW; ++j) r.v[b][j] = vp[64 * j];
-    }
-  };
-  auto work = [&](int i, Regs& r) __attribute__((always_inline)) {
-    const int u = 2 * i, k0 = 2 * wave + 8 * i;  // first page in lanes, and in the part
-    f32x4 sc[2][NC];
-    float vs[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint32_t s2 = (uint32_t)__builtin_amdgcn_readlane((int)my_scale, u + b);
-      const float ks = bf2f(s2 & 0xFFFFu);
-      vs[b] = bf2f(s2 >> 16);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) sc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < NU; ++x) {
-        const u32x4& w = r.k[b][x >> 1];
-        const bf16x8 kk = join8(decode4<CODE>(w[2 * (x & 1)]), decode4<CODE>(w[2 * (x & 1) + 1]));
-#pragma unroll
-        for (int n = 0; n < NC; ++n)
-          sc[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, __builtin_bit_cast(bf16x8, q[n][x]), sc[b][n], 0, 0, 0);
-      }
-#pragma unroll
-      for (int n = 0; n < NC; ++n) sc[b][n] *= ks;
-    }
-    if (k0 + 1 >= cnt) {  // uniform: the batch's second slot is past the part's pages
-#pragma unroll
-      for (int n = 0; n < NC; ++n) sc[1][n] = f32x4{kNegInf, kNegInf, kNegInf, kNegInf};
-    }
-    bf16x8 hi[NC], lo[NC];
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      float top = kNegInf;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) top = fmaxf(top, fmaxf(fmaxf(sc[b][n][0], sc[b][n][1]), fmaxf(sc[b][n][2], sc[b][n][3])));
-      refer(n, top);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f((sc[b][n][e] - m[n]) * a.scale_log2);
-        lsum[n] += (p[0] + p[1]) + (p[2] + p[3]);
-        // a weight goes in as the sum of two bf16 (relative error 2^-17; the matrix cores are idle anyway)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = p[e] * vs[b];
-          hi[n][4 * b + e] = (__bf16)x;
-          lo[n][4 * b + e] = (__bf16)(x - (float)hi[n][4 * b + e]);
-        }
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const bf16x8 vv = join8(decode4<CODE>(r.v[0][j >> 2][j & 3]), decode4<CODE>(r.v[1][j >> 2][j & 3]));
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, hi[n], acc[n][j], 0, 0, 0);
-        acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, lo[n], acc[n][j], 0, 0, 0);
-      }
-    }
-  };
-  if (cnt > 2 * wave) {
-    const int nb = (cnt - 2 * wave + 7) / 8;
-    Regs ra, rb;
-    load(0, ra);
-    int i = 0;
-    for (; i + 2 < nb; i += 2) {
-      load(2 * (i + 1), rb);
-      work(i, ra);
-      load(2 * (i + 2), ra);
-      work(i + 1, rb);
-    }
-    if (nb - i == 2) {
-      load(2 * (i + 1), rb);
-      work(i, ra);
-      work(i + 1, rb);
-    } else {
-      work(i, ra);
-    }
   }
-
-  // --------------------------------- the pages behind, one at a time, in 16 bits
-  for (int p = max(c0, full) + wave; p < c1; p += 4) {
-    const size_t at = (((size_t)layer * a.c.open_pages + it.s * a.c.ring + p % a.c.ring) * a.n_kv_heads + it.h) * tile;
+  // tile n's weights for two pages' scores (sums over codes), times V's scales
+  __device__ __forceinline__ f16x8 weights(int n, const f32x4 (&sc)[2], const float (&kc)[2], const float (&vs)[2]) {
+    float top = kNegInf;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) top = fmaxf(top, kc[b] * fmaxf(fmaxf(sc[b][0], sc[b][1]), fmaxf(sc[b][2], sc[b][3])));
+    refer(n, top);
+    f16x8 w;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e], kc[b], -m[n]));
+      lsum[n] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * b + e] = (_Float16)(p[e] * vs[b]);
+    }
+    return w;
+  }
+  __device__ __forceinline__ void unscale(float f) {
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[n][j] *= f;
+  }
+  // A page behind the complete ones: a 16-bit tile, masked by each column's own position. V of tokens behind the
+  // group's last counts as 0 (unwritten rows hold anything); V of the group's own later tokens is written, but
+  // may be inf or NaN, whose product with a weight of 0 is not 0: the columns that see it get it one by one.
+  __device__ __forceinline__ void open_page(const Attend8Args& a, const Item8& it, int p) {
+    const int lane = threadIdx.x & 63, quad = lane >> 4;
+    const size_t at = (((size_t)(a.layer + it.l) * a.c.open_pages + it.s * a.c.ring + p % a.c.ring) * a.n_kv_heads + it.h) *
+                      (size_t)(kPage * D);
     const u32x4* kp = (const u32x4*)(a.c.k_open + at) + lane;
     const u32x4* vp = (const u32x4*)(a.c.v_open + at) + lane;
     u32x4 k[NU], v[NU];
@@ -342,14 +298,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NC == 1 ? 2
     };
     const int first = it.len + it.tok0, end = first + it.nt - 1;
     keep(v, end);
-    bool odd = false;  // some inf or NaN that not all of the group's tokens see
+    // inf and NaN that not all of the group's tokens see: out, and in again where they are seen
+    bool odd = false;
     if (kPage * p + kPage - 1 > first) {
 #pragma unroll
       for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) odd |= t0 + (e & 3) > first && (el16(v[u], e) & 0x7F80u) == 0x7F80u;
+        for (int e = 0; e < 8; ++e) {
+          const bool bad = t0 + (e & 3) > first && (el16(v[u], e) & 0x7F80u) == 0x7F80u;
+          odd |= bad;
+          if (bad) v[u][e >> 1] &= ~(0xFFFFu << (16 * (e & 1)));
+        }
       odd = __any(odd);
     }
+    float x[NC][4];
     s16x4 hi[NC], lo[NC];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -360,73 +322,181 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NC == 1 ? 2
       float top = kNegInf;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (t0 + e > lim[n]) sc[e] = kNegInf;
+        sc[e] = t0 + e > lim[n] ? kNegInf : sc[e] * a.scale_log2;
         top = fmaxf(top, sc[e]);
       }
       refer(n, top);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f((sc[e] - m[n]) * a.scale_log2);
-        lsum[n] += x;
-        const __bf16 h = (__bf16)x;
+        x[n][e] = __builtin_amdgcn_exp2f(sc[e] - m[n]);
+        lsum[n] += x[n][e];
+        const __bf16 h = (__bf16)x[n][e];
         hi[n][e] = __builtin_bit_cast(short, h);
-        lo[n][e] = __builtin_bit_cast(short, (__bf16)(x - (float)h));
+        lo[n][e] = __builtin_bit_cast(short, (__bf16)(x[n][e] - (float)h));
       }
     }
     auto tokens4 = [](const u32x4& w, int half) { return __builtin_bit_cast(s16x4, half ? make_uint2(w[2], w[3]) : make_uint2(w[0], w[1])); };
-    if (!odd) {
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const s16x4 vv = tokens4(v[j >> 1], j & 1);
+    for (int j = 0; j < NJ; ++j) {
+      const s16x4 vv = tokens4(v[j >> 1], j & 1);
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-          acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, hi[n], acc[n][j], 0, 0, 0);
-          acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, lo[n], acc[n][j], 0, 0, 0);
-        }
+      for (int n = 0; n < NC; ++n) {
+        acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, hi[n], acc[n][j], 0, 0, 0);
+        acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, lo[n], acc[n][j], 0, 0, 0);
       }
-    } else {
-      for (int i = 0; i < it.nt; ++i) {  // each token's columns see V up to it
-        u32x4 w[NU];
+    }
+    if (!odd) return;
+    const uint16_t* tile = (const uint16_t*)a.c.v_open + at;
+#pragma unroll 1
+    for (int t = max(first + 1 - kPage * p, 0); t < kPage && kPage * p + t <= end; ++t) {
+      const int from = (lane & 15) + 16 * (t >> 2);  // where the token's weights are
 #pragma unroll
-        for (int u = 0; u < NU; ++u) w[u] = v[u];
-        keep(w, first + i);
+      for (int n = 0; n < NC; ++n) {
+        const float mine = (t & 3) == 0 ? x[n][0] : (t & 3) == 1 ? x[n][1] : (t & 3) == 2 ? x[n][2] : x[n][3];
+        const float w = __shfl(mine, from);
+        const bool sees = kPage * p + t <= lim[n];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const s16x4 vv = tokens4(w[j >> 1], j & 1);
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
-          for (int n = 0; n < NC; ++n) {
-            f32x4 o = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, hi[n], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            o = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vv, lo[n], o, 0, 0, 0);
-            if (lim[n] == first + i) acc[n][j] += o;
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t y = tile[vswz(t, 16 * j + 4 * quad + e)];
+            acc[n][j][e] += sees && (y & 0x7F80u) == 0x7F80u ? w * bf2f(y) : 0.f;
           }
-        }
       }
     }
   }
-
-  // -------------------------------------------------------- the waves' states
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
+  __device__ __forceinline__ void sum(int n) {
     lsum[n] += __shfl_xor(lsum[n], 16);
     lsum[n] += __shfl_xor(lsum[n], 32);
+  }
+};
+
+// One block of W waves per (item, part of its pages), whose waves take pairs of pages in turn, all columns each, and
+// are merged in LDS. The pages that were complete before the call lie before every new token: no mask. A wave holds
+// the ids and scales of its pages one per lane and loads a pair of pages while it works on the one before.
+// Bound: HBM for a token (33 sequences, 16 layers of 8 heads: 232 us, 5.9 TB/s, as much as a plain read of memory reaches; a
+// layer of it 18.1 us, half of which is the launch, a first page and the merge of the waves; 9 books of 100 000 tokens and their
+// query: 216 us); for a question of 24 tokens (17 sequences of 5000, int8, 7 heads each: 84 us) the instructions of
+// decoding, softmax and products, which a SIMD issues one after another.
+template <int CODE, int D, int NC, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 4))) void k_attend8(Attend8Args a) {
+  constexpr int NU = D / 32, NW = D / 64, NJ = D / 16;  // 16-bit units, code units, 16-dim output blocks
+  constexpr int DP = D + 4;
+  __shared__ __align__(16) float sacc[W][16 * NC][DP];
+  __shared__ float sm[W][16 * NC], sl[W][16 * NC];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  uint32_t item;
+  int part;
+  Item8 it;
+  if (!block8(a, it, item, part)) return;
+  const int total = pages8(it), full = it.len / kPage;
+  const int size = part8(a, it.s), c0 = part * size, c1 = min(total, c0 + size);
+  if (c0 >= c1) return;
+  const int G = a.group, cols = it.nt * G;
+  const int layer = a.layer + it.l;
+  const int32_t* pt = a.page_table + (size_t)it.s * a.maxpps;
+  const int cnt = min(c1, full) - c0;  // pages of codes (<= 0: none)
+  // the wave's u-th page of codes is page u / 2 * 2 W + 2 wave + u % 2 of the part; ids and scales one per lane
+  const int my_page = c0 + min(lane / 2 * (2 * W) + 2 * wave + lane % 2, max(cnt, 1) - 1);
+  const int my_phys = max(pt[my_page], 0);
+  const uint32_t my_scale = cnt > 0 ? a.c.scales[((size_t)layer * a.n_kv_heads + it.h) * a.c.max_pages + my_phys] : 0u;
+  Columns<D, NC> C;
+  C.begin(a, it);
+  struct Regs {
+    u32x4 k[2][NW], v[2][NW];
+  };
+  const VScale vx(my_scale);
+  const float my_kc = bf2f(my_scale & 0xFFFFu) * a.scale_log2, my_vs = bf2f(my_scale >> 16) * vx.down;
+  const size_t tile = (size_t)kPage * D;
+  auto load = [&](int u, Regs& r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const size_t at = (((size_t)layer * a.c.max_pages + __builtin_amdgcn_readlane(my_phys, u + b)) * a.n_kv_heads + it.h) * tile;
+      const u32x4* kp = (const u32x4*)(a.c.k_codes + at) + lane;
+      const u32x4* vp = (const u32x4*)(a.c.v_codes + at) + lane;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) r.k[b][j] = kp[64 * j];
+#pragma unroll
+      for (int j = 0; j < NW; ++j) r.v[b][j] = vp[64 * j];
+    }
+  };
+  auto work = [&](int i, Regs& r) __attribute__((always_inline)) {
+    const int u = 2 * i, k0 = 2 * wave + 2 * W * i;  // first page in lanes, and in the part
+    f32x4 sc[NC][2];
+    float kc[2], vs[2];  // a page's scales: K's with log2(e) / sqrt(D), V's
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      kc[b] = lane_f(my_kc, u + b);
+      vs[b] = lane_f(my_vs, u + b);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) sc[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NU; ++x) {
+        const u32x4& w = r.k[b][x >> 1];
+        const bf16x8 kk = join8(decode4<CODE>(w[2 * (x & 1)]), decode4<CODE>(w[2 * (x & 1) + 1]));
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+          sc[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, __builtin_bit_cast(bf16x8, C.q[n][x]), sc[n][b], 0, 0, 0);
+      }
+    }
+    if (k0 + 1 >= cnt) {  // uniform: the pair's second slot is past the part's pages
+#pragma unroll
+      for (int n = 0; n < NC; ++n) sc[n][1] = f32x4{kNegInf, kNegInf, kNegInf, kNegInf};
+    }
+    f16x8 wt[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) wt[n] = C.weights(n, sc[n], kc, vs);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const f16x8 vv = join8h(decode4h<CODE>(r.v[0][j >> 2][j & 3]), decode4h<CODE>(r.v[1][j >> 2][j & 3]));
+#pragma unroll
+      for (int n = 0; n < NC; ++n) C.acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, wt[n], C.acc[n][j], 0, 0, 0);
+    }
+  };
+  if (cnt > 2 * wave) {
+    const int nb = (cnt - 2 * wave + 2 * W - 1) / (2 * W);
+    Regs ra, rb;
+    load(0, ra);
+    int i = 0;
+    for (; i + 2 < nb; i += 2) {
+      load(2 * (i + 1), rb);
+      work(i, ra);
+      load(2 * (i + 2), ra);
+      work(i + 1, rb);
+    }
+    if (nb - i == 2) {
+      load(2 * (i + 1), rb);
+      work(i, ra);
+      work(i + 1, rb);
+    } else {
+      work(i, ra);
+    }
+    C.unscale(vx.up);
+  }
+#pragma unroll 1
+  for (int p = max(c0, full) + wave; p < c1; p += W) C.open_page(a, it, p);
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    C.sum(n);
     const int cc = 16 * n + col;
     if (cc < cols) {
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) *(f32x4*)&sacc[wave][cc][16 * j + 4 * quad] = acc[n][j];
-      if (quad == 0) { sm[wave][cc] = m[n]; sl[wave][cc] = lsum[n]; }
+      for (int j = 0; j < NJ; ++j) *(f32x4*)&sacc[wave][cc][16 * j + 4 * quad] = C.acc[n][j];
+      if (quad == 0) { sm[wave][cc] = C.m[n]; sl[wave][cc] = C.lsum[n]; }
     }
   }
   __syncthreads();
-  for (int e = tid; e < cols * (D / 4); e += 256) {
+  for (int e = tid; e < cols * (D / 4); e += 64 * W) {
     const int cc = e / (D / 4), d = e % (D / 4) * 4;
     float mm = sm[0][cc];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) mm = fmaxf(mm, sm[w][cc]);
+    for (int w = 1; w < W; ++w) mm = fmaxf(mm, sm[w][cc]);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float den = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = exp2f((sm[w][cc] - mm) * a.scale_log2);  // (a wave without pages: l = 0 and m = kLowest8)
+    for (int w = 0; w < W; ++w) {
+      const float f = exp2f(sm[w][cc] - mm);  // (a wave without pages: l = 0 and m = kLowest8)
       den += f * sl[w][cc];
       o += f * *(const f32x4*)&sacc[w][cc][d];
     }
@@ -441,41 +511,61 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NC == 1 ? 2
   }
 }
 
-// The merge of an item's parts (see k_attend_merge), a block per item and 1024 of its outputs
+// The merge of an item's parts (see k_attend_merge): a block per item and 8 of its columns, of each of which a
+// wave takes half, or (SPREAD: many parts, few columns) a block per column, whose 256 / (D / 4) groups of threads take the
+// parts in turn and meet in LDS.
+template <bool SPREAD>
 __global__ __launch_bounds__(256) void k_attend8_merge(Attend8Args a) {
-  const uint32_t item = blockIdx.x;
-  const Item8 it = item8(a, item);
-  const int G = a.group, D = a.head_dim, stride = a.gt * G;
-  const int n = (pages8(it) + a.part_pages - 1) / a.part_pages;
-  const int e = blockIdx.y * 256 + threadIdx.x;
-  const int cc = e / (D / 4), d = e % (D / 4) * 4;
-  if (cc >= it.nt * G) return;
+  __shared__ f32x4 so[SPREAD ? 256 : 1];
+  __shared__ float2 sml[SPREAD ? 256 : 1];
+  const uint32_t item = blockIdx.x, heads = (uint32_t)a.launch_layers * a.n_kv_heads;
+  const uint32_t g = item / heads, s = g / (uint32_t)a.n_groups;
+  const Item8 it = item8(a, a.seq0 + s, a.group0 + g - s * a.n_groups, item - g * heads);
+  const int G = a.group, D = a.head_dim, stride = a.gt * G, lanes = D / 4, groups = 256 / lanes;
+  const int size = part8(a, it.s), n = (pages8(it) + size - 1) / size;
+  const int grp = threadIdx.x / lanes, d = threadIdx.x % lanes * 4;
+  const int cc = SPREAD ? blockIdx.y : blockIdx.y * groups + grp;
+  if (cc >= it.nt * G) return;  // (SPREAD: the whole block)
   const size_t w0 = (size_t)item * a.parts * stride + cc;
+  const int step = SPREAD ? groups : 1;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float mm = kLowest8, den = 0.f;
-  for (int j0 = 0; j0 < n; j0 += 8) {  // (slots past the last part read it again and weigh nothing)
+  for (int j0 = SPREAD ? grp : 0; j0 < n; j0 += 8 * step) {  // (slots past the last part read it again and weigh nothing)
     f32x4 v[8];
     float2 ml[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const size_t w = w0 + (size_t)min(j0 + j, n - 1) * stride;
+      const size_t w = w0 + (size_t)min(j0 + j * step, n - 1) * stride;
       v[j] = *(const f32x4*)(a.part_acc + w * D + d);
       ml[j] = *(const float2*)(a.part_ml + 2 * w);
     }
     float top = mm;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
-    const float r = mm == top ? 1.f : exp2f((mm - top) * a.scale_log2);
+    const float r = mm == top ? 1.f : exp2f(mm - top);
     mm = top;
     den *= r;
     o *= r;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (j0 + j < n) {
-        const float f = exp2f((ml[j].x - mm) * a.scale_log2);
+      if (j0 + j * step < n) {
+        const float f = exp2f(ml[j].x - mm);
         den += f * ml[j].y;
         o += f * v[j];
       }
+  }
+  if constexpr (SPREAD) {
+    so[threadIdx.x] = o;
+    sml[threadIdx.x] = make_float2(mm, den);
+    __syncthreads();
+    if (grp > 0) return;
+    for (int x = 1; x < groups && x < n; ++x) {
+      const float2 ml = sml[x * lanes + threadIdx.x];
+      const float top = fmaxf(mm, ml.x), f0 = exp2f(mm - top), f1 = exp2f(ml.x - top);
+      mm = top;
+      den = f0 * den + f1 * ml.y;
+      o = f0 * o + f1 * so[x * lanes + threadIdx.x];
+    }
   }
   const int i = cc / G;
   store_x4_bf16(a.x_out, qrow8(a, it, i, cc - i * G, D) + d, o / den);
@@ -542,26 +632,27 @@ hipError_t launch_load8(const LoadArgs& a0, const Cache8Args& c, int n_items, hi
   return c.code == kE4m3 ? run(k_load8<kE4m3, 64>) : run(k_load8<kInt8, 64>);
 }
 
-hipError_t launch_attend8(const Attend8Args& a0, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
-  Attend8Args a = a0;
-  const size_t items = (size_t)a.n_groups * a.launch_layers * a.n_kv_heads;
-  a.launch_seqs = (a.group0 + a.n_groups - 1) / a.seq_groups - a.group0 / a.seq_groups + 1;
-  const size_t pairs = (size_t)a.launch_seqs * a.launch_layers * a.n_kv_heads;
-  const size_t blocks = (a.seq_groups == 1 ? items : (pairs + 7) / 8 * 8 * a.seq_groups) * a.parts;
+hipError_t launch_attend8(const Attend8Args& a, hipStream_t st, const Timing* tm, const Timing* tm_merge) {
+  const size_t heads = (size_t)a.launch_layers * a.n_kv_heads, units = a.seq_parts * heads;
+  const size_t items = (size_t)a.launch_seqs * a.n_groups * heads;
+  const size_t blocks = a.n_groups == 1 ? units : (units + 7) / 8 * 8 * a.n_groups;
   if (blocks > 0x7FFFFFFFu) return hipErrorInvalidValue;
-  auto run = [&](auto kernel) { return go(kernel, dim3((unsigned)blocks), dim3(256), 0, st, t0(tm), t1(tm), a); };
-  auto tiles = [&](auto one, auto two) { return a.tiles == 1 ? run(one) : run(two); };
-  hipError_t e;
-  if (a.head_dim == 128) {
-    e = a.c.code == kE4m3 ? tiles(k_attend8<kE4m3, 128, 1>, k_attend8<kE4m3, 128, 2>)
-                          : tiles(k_attend8<kInt8, 128, 1>, k_attend8<kInt8, 128, 2>);
-  } else {
-    e = a.c.code == kE4m3 ? tiles(k_attend8<kE4m3, 64, 1>, k_attend8<kE4m3, 64, 2>)
-                          : tiles(k_attend8<kInt8, 64, 1>, k_attend8<kInt8, 64, 2>);
-  }
+  auto run = [&](auto kernel) { return go(kernel, dim3((unsigned)blocks), dim3(64 * a.waves), 0, st, t0(tm), t1(tm), a); };
+  auto pick = [&](auto code, auto dim) {
+    constexpr int CODE = decltype(code)::value, D = decltype(dim)::value;
+    if (a.tiles == 1) return a.waves == 8 ? run(k_attend8<CODE, D, 1, 8>) : run(k_attend8<CODE, D, 1, 4>);
+    return run(k_attend8<CODE, D, 2, 4>);
+  };
+  using E = std::integral_constant<int, kE4m3>;
+  using I = std::integral_constant<int, kInt8>;
+  auto dims = [&](auto code) {
+    return a.head_dim == 128 ? pick(code, std::integral_constant<int, 128>{}) : pick(code, std::integral_constant<int, 64>{});
+  };
+  const hipError_t e = a.c.code == kE4m3 ? dims(E{}) : dims(I{});
   if (e != hipSuccess || a.parts == 1) return e;
-  const dim3 grid((unsigned)items, (a.gt * a.group * (a.head_dim / 4) + 255) / 256);
-  return go(k_attend8_merge, grid, dim3(256), 0, st, t0(tm_merge), t1(tm_merge), a);
+  const int cols = a.gt * a.group, per = 1024 / a.head_dim;  // columns of a block
+  auto merge = [&](auto kernel, int y) { return go(kernel, dim3((unsigned)items, y), dim3(256), 0, st, t0(tm_merge), t1(tm_merge), a); };
+  return a.parts > 8 && items * cols < 4096 ? merge(k_attend8_merge<true>, cols) : merge(k_attend8_merge<false>, (cols + per - 1) / per);
 }
 
 hipError_t launch_read8(const ReadCacheArgs& a, const Cache8Args& c, int len, hipStream_t st) {

@@ -47,23 +47,52 @@ pced_status check_new(const pced_ctx* c, int n_tokens) {
   return PCED_OK;
 }
 
-// How a launch of pced_attend_codes divides its work (see attend_plan): parts of the items' pages,
-// and the workspace that their states take.
+// How pced_attend_codes divides its work: sequences, groups per sequence and layers per launch, pages per part, and
+// the workspace that the parts' states take.
 struct Plan8 {
-  int parts, part_pages;
-  size_t ml, bytes;
+  int seqs, groups, layers, part_pages;
+  int parts;         // of the longest sequence
+  size_t ml, bytes;  // (offset of the second array)
 };
-Plan8 plan8(const pced_ctx* c, const Attend8Args& a, int max_pages, int groups, int layers, int min_part) {
-  Plan8 p{};
-  const size_t items = (size_t)groups * layers * a.n_kv_heads, cols = (size_t)a.gt * a.group;
-  const size_t want = std::max<size_t>(1, 2 * (size_t)c->num_cus / items);
-  p.part_pages = std::min(std::max<int>({min_part, ceil_div(ceil_div(max_pages, (long)want), 8) * 8, 8}), kAttendPart);
-  p.parts = ceil_div(max_pages, p.part_pages);
-  if (p.parts > 1) {
-    p.ml = align_up(items * p.parts * cols * a.head_dim * 4);
-    p.bytes = p.ml + align_up(items * p.parts * cols * 8);
+void size_plan(Plan8* p, const Attend8Args& a, int max_pages) {
+  const size_t cols = (size_t)a.gt * a.group;
+  p->parts = ceil_div(max_pages, p->part_pages);
+  const size_t states = (size_t)p->seqs * p->groups * p->layers * a.n_kv_heads * p->parts * cols;
+  p->ml = p->parts > 1 ? align_up(states * a.head_dim * 4) : 0;
+  p->bytes = p->parts > 1 ? p->ml + align_up(states * 8) : 0;
+}
+// pages: of every sequence. The waves of a work-group hold kWavePages page numbers each.
+//
+// Parts. Splitting a sequence costs a second launch and the states' way through memory (about 4 us), so sequences of
+// up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.6 us, split 10.0), and so do longer ones where they keep
+// every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 45). Otherwise parts are as short as one
+// work-group per CU allows (5 x up to 250 pages: 48 pages 14.1 us, 32 pages 15.6, 96 pages 16.3), 32 pages at least.
+bool plan8(const pced_ctx* c, const Attend8Args& a, const std::vector<int>& pages, int groups, Plan8* out) {
+  const int most = 4 * kWavePages, S = (int)pages.size();
+  const int max_pages = *std::max_element(pages.begin(), pages.end());
+  const double per = (double)groups * a.n_layers * a.n_kv_heads;  // work-groups for a part of a sequence
+  int part = most;
+  if (max_pages > 96 && S * per <= c->num_cus) {
+    long sum = 0;
+    for (int x : pages) sum += x;
+    for (part = (int)std::min<double>(most, std::max(32., std::ceil(sum * per / c->num_cus / 8) * 8)); part < most; part += 8) {
+      long n = 0;
+      for (int x : pages) n += ceil_div(x, part);
+      if (n * per <= c->num_cus) break;
+    }
   }
-  return p;
+  Plan8 p{S, groups, a.n_layers, part, 0, 0, 0};
+  size_plan(&p, a, max_pages);
+  while (p.bytes > c->lay.part_acc_bytes) {
+    if (p.layers > 1) p.layers = (p.layers + 1) / 2;
+    else if (p.seqs > 1) p.seqs = (p.seqs + 1) / 2;
+    else if (p.groups > 1) p.groups = (p.groups + 1) / 2;
+    else if (p.part_pages < most) p.part_pages = std::min(2 * p.part_pages, most);
+    else return false;
+    size_plan(&p, a, max_pages);
+  }
+  *out = p;
+  return true;
 }
 
 }  // namespace
@@ -162,43 +191,45 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   a.group = c->G;
   a.head_dim = cfg.head_dim;
   a.maxpps = cfg.max_pages_per_seq;
-  a.tiles = n_tokens * c->G <= 16 ? 1 : 2;
-  const int most = 16 * a.tiles / c->G;  // tokens that the tiles hold
-  a.seq_groups = ceil_div(n_tokens, most);
-  a.gt = ceil_div(n_tokens, a.seq_groups);
+  // Two tiles share a page's loads and decoding, one leaves room for more waves: 33 sequences of 82 pages on average,
+  // 8 heads, e4m3: 8 columns 17.0 us (two tiles 18.7), 32 columns 21.3 (21.8), 64 columns 33.2 (31.5), 256 columns 103 (92);
+  // int8, 256 columns 145 (120).
+  a.tiles = n_tokens * c->G <= 32 ? 1 : 2;
+  const int groups = ceil_div(n_tokens, 16 * a.tiles / c->G);  // per sequence
+  a.gt = ceil_div(n_tokens, groups);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cfg.head_dim));
-  a.lead = 8.f / a.scale_log2;
-  int max_pages = 0;
-  for (int s = 0; s < c->S; ++s) max_pages = std::max(max_pages, (c->len[s] + n_tokens - 1) / kPage + 1);
-  // as many layers and groups per launch as the workspace takes
-  const int all = c->S * a.seq_groups;
-  int groups = all, layers = n_layers, min_part = 8;
-  Plan8 p = plan8(c, a, max_pages, groups, layers, min_part);
-  while (p.bytes > c->lay.part_acc_bytes) {
-    if (layers > 1) layers = (layers + 1) / 2;
-    else if (groups > 1) groups = (groups + 1) / 2;
-    else if (p.parts > 1 && p.part_pages < kAttendPart) min_part = 2 * p.part_pages;
-    else return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
-    p = plan8(c, a, max_pages, groups, layers, min_part);
-  }
+  std::vector<int> pages(c->S);
+  for (int s = 0; s < c->S; ++s) pages[s] = (c->len[s] + n_tokens - 1) / kPage + 1;
+  Plan8 p{};
+  if (!plan8(c, a, pages, groups, &p)) return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
+  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 x 128 pages, 8 heads:
+  // 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or parts are short
+  // (9 x 256 pages of 1500: 217 us, eight waves 228).
+  a.waves = a.tiles == 1 && p.parts == 1 && (double)c->S * groups * n_layers * cfg.n_kv_heads <= 2. * c->num_cus ? 8 : 4;
   char* ws = c->at<char>(c->lay.part_acc);
   a.part_acc = (float*)ws;
   a.part_ml = (float*)(ws + p.ml);
   a.parts = p.parts;
   a.part_pages = p.part_pages;
-  double tokens = 0;  // seen, per layer and kv-head
-  for (int s = 0; c->prof && s < c->S; ++s) tokens += c->len[s] + n_tokens;
-  for (int l = 0; l < n_layers; l += layers) {
+  for (int l = 0; l < n_layers; l += p.layers) {
     a.layer = layer + l;
-    a.launch_layers = std::min(layers, n_layers - l);
-    for (int g = 0; g < all; g += groups) {
-      a.group0 = g;
-      a.n_groups = std::min(groups, all - g);
-      const double part = tokens * a.n_groups / all * a.launch_layers * cfg.n_kv_heads * cfg.head_dim;
-      ProfScope ps(c, PCED_PROF_ATTN, part * 2, part * 4 * c->G * n_tokens);
-      ProfScope pm(c, PCED_PROF_COMBINE, 0, 0);
-      if (p.parts == 1) pm.drop();
-      HIP_OK(launch_attend8(a, st, ps.timing(), pm.timing()));
+    a.launch_layers = std::min(p.layers, n_layers - l);
+    for (a.seq0 = 0; a.seq0 < c->S; a.seq0 += p.seqs) {
+      a.launch_seqs = std::min(p.seqs, c->S - a.seq0);
+      a.seq_parts = 0;
+      double tokens = 0;  // seen, per layer and kv-head
+      for (int s = a.seq0; s < a.seq0 + a.launch_seqs; ++s) {
+        a.seq_parts += ceil_div(pages[s], p.part_pages);
+        tokens += c->len[s] + n_tokens;
+      }
+      for (a.group0 = 0; a.group0 < groups; a.group0 += p.groups) {
+        a.n_groups = std::min(p.groups, groups - a.group0);
+        const double part = tokens * a.n_groups / groups * a.launch_layers * cfg.n_kv_heads * cfg.head_dim;
+        ProfScope ps(c, PCED_PROF_ATTN, part * 2, part * 4 * c->G * n_tokens);
+        ProfScope pm(c, PCED_PROF_COMBINE, 0, 0);
+        if (p.parts == 1) pm.drop();
+        HIP_OK(launch_attend8(a, st, ps.timing(), pm.timing()));
+      }
     }
   }
   return PCED_OK;

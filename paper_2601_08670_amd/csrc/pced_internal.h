@@ -395,9 +395,10 @@ struct Cache8Args {
   uint16_t* v_open;
   int code, ring, open_pages, max_pages;
 };
+constexpr int kWavePages = 64;  // pages of codes that a wave of k_attend8 takes, at most: one per lane
 // Attention of new tokens over caches in 8 bits (see pced_attend_codes). An item is a group of gt
-// consecutive new tokens of a sequence (seq_groups of them per sequence), a layer and a kv-head; a launch takes
-// n_groups groups from group0 on and launch_layers layers from `layer` on.
+// consecutive new tokens of a sequence, a layer and a kv-head; a launch takes launch_seqs sequences from seq0 on, of
+// each n_groups groups from group0 on, and launch_layers layers from `layer` on.
 struct Attend8Args {
   Cache8Args c;
   const void* q;            // [S * n_tokens][n_layers][Hq][D]
@@ -406,12 +407,13 @@ struct Attend8Args {
   const int32_t* page_table;
   float* part_acc;          // [item][parts][gt * G][D]
   float* part_ml;           // [item][parts][gt * G][2]
-  int t, n_tokens, gt, seq_groups, group0, n_groups, layer0, n_layers, layer, launch_layers;
-  int n_q_heads, n_kv_heads, group, head_dim, maxpps, tiles;  // tiles: 16-column tiles of a group's query rows
-  int parts, part_pages;    // parts of an item's pages, and pages per part
-  int launch_seqs;          // sequences of the launch's groups (set by launch_attend8)
+  int t, n_tokens, gt, seq0, launch_seqs, group0, n_groups, layer0, n_layers, layer, launch_layers;
+  int n_q_heads, n_kv_heads, group, head_dim, maxpps;
+  int tiles;                // 16-column tiles for a group's query rows: 1 or 2
+  int waves;                // of a work-group: 4 or 8 (one tile, one part)
+  int parts, part_pages;    // parts of an item's pages, and pages per part, at most
+  int seq_parts;            // parts of all of the launch's sequences
   float scale_log2;         // log2(e) / sqrt(D)
-  float lead;               // difference of scores that makes a weight of 2^8
 };
 // Summaries of the complete pages of every sequence from token len - behind on, all layers.
 struct SummaryArgs {

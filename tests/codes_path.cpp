@@ -20,11 +20,12 @@ hipError_t launch_append8(const AppendRowsArgs& a, const Cache8Args& c, hipStrea
 hipError_t launch_attend8(const Attend8Args& a, hipStream_t, const Timing*, const Timing*) {
   if (a.parts > 1) {
     // what the launch's items use, as the kernels index it
-    const size_t states = (size_t)a.n_groups * a.launch_layers * a.n_kv_heads * a.parts * a.gt * a.group;
+    const size_t states = (size_t)a.launch_seqs * a.n_groups * a.launch_layers * a.n_kv_heads * a.parts * a.gt * a.group;
     note("acc", (long)(uintptr_t)a.part_acc, (long)((uintptr_t)a.part_acc + states * a.head_dim * 4));
     note("ml", (long)(uintptr_t)a.part_ml, (long)((uintptr_t)a.part_ml + states * 8));
   }
-  return note("attend_codes", a.layer, a.launch_layers, a.group0, a.n_groups, a.parts, a.part_pages, a.gt, a.tiles);
+  note("attend_split", a.parts, a.part_pages, a.gt, a.tiles, a.seq_parts);
+  return note("attend_codes", a.layer, a.launch_layers, a.seq0, a.launch_seqs, a.group0, a.n_groups);
 }
 hipError_t launch_read8(const ReadCacheArgs& a, const Cache8Args&, int len, hipStream_t) {
   return note("read_codes", a.seq, a.layer, a.start, a.count, len);

@@ -201,17 +201,20 @@ def test_every_size_fits(codes_host, heads, layers, lens, n):
     b = Codes(codes_host, lens, n, n_q_heads=heads[0], n_kv_heads=heads[1], head_dim=heads[2], n_layers=layers)
     assert b.status == OK and b.append(n, rope=None) == OK and b.attend(n) == OK, b.error()
     begin, end, seen, G = codes_host.room_begin(b.ctx), codes_host.room_end(b.ctx), set(), heads[0] // heads[1]
-    for l, nl, g, ng, parts, part_pages, gt, tiles in b.calls("attend_codes"):
-        cells = {(i, j) for i in range(l, l + nl) for j in range(g, g + ng)}
+    splits = b.calls("attend_split")
+    for (l, nl, s, ns, g, ng, *_), (parts, part_pages, gt, tiles, seq_parts, *_) in zip(b.calls("attend_codes"), splits):
+        cells = {(i, j, k) for i in range(l, l + nl) for j in range(s, s + ns) for k in range(g, g + ng)}
         assert cells and not cells & seen
         seen |= cells
-        assert parts * part_pages >= -(-(max(lens) + n) // 16) and part_pages <= 256
-        assert 1 <= gt and gt * G <= 16 * tiles
+        pages = [(x + n - 1) // 16 + 1 for x in lens]
+        assert parts == -(-max(pages) // part_pages) and part_pages % 8 == 0 and part_pages <= 256
+        assert seq_parts == sum(-(-x // part_pages) for x in pages[s:s + ns])
+        assert 1 <= gt and gt * G <= 16 * tiles and tiles in (1, 2)
         groups = -(-n // gt)
     spans = sorted((c[0], c[1]) for name in ("acc", "ml") for c in b.calls(name))
     for x, y in spans:
         assert begin <= x < y <= end
-    assert seen == {(i, j) for i in range(layers) for j in range(groups * len(lens))}
+    assert seen == {(i, j, k) for i in range(layers) for j in range(len(lens)) for k in range(groups)}
 
 
 def test_struct_matches_the_header(tmp_path):

@@ -208,12 +208,15 @@ def _check_attend(m, q, x, T, lens, layers=None):
                     want = C.attend(qq, kk, vv)
                     # a score's fp32 sum of D products, its block's scale and the difference of scores are off by at
                     # most (D + 6) 2^-24 times the sum of the products' sizes; a weight's relative error is at most that
-                    # of scores (twice, with the reference's), of exp2 (2^-22), of its product with V's scale (2^-24)
-                    # and of its two bf16 parts (2^-17), in numerator and sum; the fp32 sums over n tokens and over
-                    # the parts' states add (n + 64) 2^-24 to each; the result is rounded to bf16 once (half a step:
-                    # 2^-8)
+                    # of scores (twice, with the reference's) and of exp2 (2^-22), in numerator and sum; in the
+                    # numerator that of its product with V's scale (2^-24) and of the rounding of that to fp16: 2^-11,
+                    # or, below 2^-14, 2^-25 absolute. A part's products are scaled so that its largest V scale lies
+                    # in [2^6, 2^7) and the softmax's sum is at least 1 in its units: n tokens' 2^-25 are n 2^-31 of
+                    # the largest scale, times a code of at most M, which is (1 + 2^-6) max |V| at most. The fp32 sums
+                    # over n tokens and over the parts' states add (n + 64) 2^-24 to each; the result is rounded to
+                    # bf16 once (half a step: 2^-8)
                     ds = (m.d + 6) * 2.0 ** -24 * (np.abs(qq) @ np.abs(kk).T).max() / np.sqrt(m.d)
-                    rel = 2 * (2 * ds + 2.0 ** -22 + 2.0 ** -24 + 2.0 ** -17) + 2 * (n + 64) * 2.0 ** -24
+                    rel = 2 * (2 * ds + 2.0 ** -22) + 2.0 ** -24 + 2.0 ** -11 + n * 2.0 ** -30 + 2 * (n + 64) * 2.0 ** -24
                     tol = half * np.abs(want) + rel * (1 + half) * np.abs(vv).max()
                     err = np.abs(got[s * T + i, at, h * G:(h + 1) * G] - want) - tol
                     assert (err <= 0).all(), (s, i, l, h, float(err.max()))
