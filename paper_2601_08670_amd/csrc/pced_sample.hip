@@ -49,7 +49,7 @@ __device__ __forceinline__ int token_in(u64 key) { return (int)~(uint32_t)key; }
 // The tokens of a block's part of a query's row, kTokens per thread at a time, the first of them
 // loaded before anything else: the settings, the slices' ranges and the bins come from other dies'
 // launches, 1 us away, and so do the scores.
-constexpr int kBinThreads = 512, kTokens = 8;
+constexpr int kBinThreads = 512, kTokens = 10;
 struct Part {
   const float* x;
   int v0, v1;
@@ -524,8 +524,11 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs& a, int n_queries, int num_cus, hipStream_t st, const Timing* tm) {
-  const long want = std::max(1L, 2L * num_cus / n_queries), most = std::max(1, a.V / 2048);
-  const dim3 grid((unsigned)std::min({want, most, 64L}), n_queries);
+  // a work-group per compute unit, none below 1024 tokens, and at most 32 per query, since each adds its bins to
+  // the query's (k_sample_bins, 512 threads, 16 queries of 151936 tokens, us at 8 / 16 / 32 / 64 / 128 per query: 17.5 /
+  // 14.2 / 15.6 / 21.6 / 34.2; one of 128256: 13.9 / 8.8 / 6.2 / 6.1 / 6.9)
+  const long parts = std::min({(long)num_cus / n_queries, (a.V + 1023L) / 1024, 32L});
+  const dim3 grid((unsigned)std::max(1L, parts), n_queries);
   hipError_t e = go(k_sample_bins, grid, dim3(kBinThreads), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;
   e = go(k_sample_list, grid, dim3(kBinThreads), 0, st, nullptr, nullptr, a);
