@@ -375,7 +375,7 @@ struct Columns {
 // are merged in LDS. The pages that were complete before the call lie before every new token: no mask. A wave holds
 // the ids and scales of its pages one per lane and loads a pair of pages while it works on the one before.
 // Bound: HBM for a token (33 sequences, 16 layers of 8 heads: 232 us, 5.9 TB/s, as much as a plain read of memory reaches; a
-// layer of it 18.1 us, half of which is the launch, a first page and the merge of the waves; 9 books of 100 000 tokens and their
+// layer of it 18.1 us, half of which is the launch, a first page and the merge of the waves; 8 books of up to 131 072 tokens and their
 // query: 216 us); for a question of 24 tokens (17 sequences of 5000, int8, 7 heads each: 84 us) the instructions of
 // decoding, softmax and products, which a SIMD issues one after another.
 template <int CODE, int D, int NC, int W>

@@ -202,9 +202,9 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   for (int s = 0; s < c->S; ++s) pages[s] = (c->len[s] + n_tokens - 1) / kPage + 1;
   Plan8 p{};
   if (!plan8(c, a, pages, groups, &p)) return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
-  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 x 128 pages, 8 heads:
+  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 sequences of up to 128 pages, 8 heads:
   // 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or parts are short
-  // (9 x 256 pages of 1500: 217 us, eight waves 228).
+  // (8 books of up to 8192 pages, in parts of 256: 217 us, eight waves 228).
   a.waves = a.tiles == 1 && p.parts == 1 && (double)c->S * groups * n_layers * cfg.n_kv_heads <= 2. * c->num_cus ? 8 : 4;
   char* ws = c->at<char>(c->lay.part_acc);
   a.part_acc = (float*)ws;
