@@ -61,23 +61,30 @@ void size_plan(Plan8* p, const Attend8Args& a, int max_pages) {
   p->ml = p->parts > 1 ? align_up(states * a.head_dim * 4) : 0;
   p->bytes = p->parts > 1 ? p->ml + align_up(states * 8) : 0;
 }
-// pages: of every sequence. The waves of a work-group hold kWavePages page numbers each.
+// The pages that n new tokens of sequence s end in, and all before
+int pages_of(const pced_ctx* c, int s, int n) { return (c->len[s] + n - 1) / kPage + 1; }
+
+// The waves of a work-group hold kWavePages page numbers each.
 //
 // Parts. Splitting a sequence costs a second launch and the states' way through memory (about 4 us), so sequences of
 // up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.6 us, split 10.0), and so do longer ones where they keep
 // every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 45). Otherwise parts are as short as one
 // work-group per CU allows (5 x up to 250 pages: 48 pages 14.1 us, 32 pages 15.6, 96 pages 16.3), 32 pages at least.
-bool plan8(const pced_ctx* c, const Attend8Args& a, const std::vector<int>& pages, int groups, Plan8* out) {
-  const int most = 4 * kWavePages, S = (int)pages.size();
-  const int max_pages = *std::max_element(pages.begin(), pages.end());
+bool plan8(const pced_ctx* c, const Attend8Args& a, int groups, Plan8* out) {
+  const int most = 4 * kWavePages, S = c->S;
+  int max_pages = 0;
+  long sum = 0;
+  for (int s = 0; s < S; ++s) {
+    const int x = pages_of(c, s, a.n_tokens);
+    max_pages = std::max(max_pages, x);
+    sum += x;
+  }
   const double per = (double)groups * a.n_layers * a.n_kv_heads;  // work-groups for a part of a sequence
   int part = most;
   if (max_pages > 96 && S * per <= c->num_cus) {
-    long sum = 0;
-    for (int x : pages) sum += x;
     for (part = (int)std::min<double>(most, std::max(32., std::ceil(sum * per / c->num_cus / 8) * 8)); part < most; part += 8) {
       long n = 0;
-      for (int x : pages) n += ceil_div(x, part);
+      for (int s = 0; s < S; ++s) n += ceil_div(pages_of(c, s, a.n_tokens), part);
       if (n * per <= c->num_cus) break;
     }
   }
@@ -198,10 +205,8 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   const int groups = ceil_div(n_tokens, 16 * a.tiles / c->G);  // per sequence
   a.gt = ceil_div(n_tokens, groups);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cfg.head_dim));
-  std::vector<int> pages(c->S);
-  for (int s = 0; s < c->S; ++s) pages[s] = (c->len[s] + n_tokens - 1) / kPage + 1;
   Plan8 p{};
-  if (!plan8(c, a, pages, groups, &p)) return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
+  if (!plan8(c, a, groups, &p)) return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
   // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 sequences of up to 128 pages, 8 heads:
   // 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or parts are short
   // (8 books of up to 8192 pages, in parts of 256: 217 us, eight waves 228).
@@ -219,7 +224,7 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
       a.seq_parts = 0;
       double tokens = 0;  // seen, per layer and kv-head
       for (int s = a.seq0; s < a.seq0 + a.launch_seqs; ++s) {
-        a.seq_parts += ceil_div(pages[s], p.part_pages);
+        a.seq_parts += ceil_div(pages_of(c, s, n_tokens), p.part_pages);
         tokens += c->len[s] + n_tokens;
       }
       for (a.group0 = 0; a.group0 < groups; a.group0 += p.groups) {

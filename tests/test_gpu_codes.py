@@ -242,6 +242,8 @@ ATTENDS = [
     ((12, 1, 128), 1, [129, 5], 4),
     ((8, 2, 64), 1, [6000, 1], 1),
     ((8, 2, 64), 1, [4500, 17], 20),
+    ((4, 4, 64), 3, [33, 5, 40] * 15, 1),
+    ((4, 4, 64), 3, [4200] + [17, 3, 30] * 7, 1),
 ]
 
 
@@ -270,6 +272,22 @@ def test_attend_sharp_scores_and_uneven_blocks(code):
     m.grow(k, v, 2)
     torch.cuda.synchronize()
     _check_attend(m, q, x, 2, [400, 333])
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("size", [2.0 ** -115, 2.0 ** 110])
+@pytest.mark.parametrize("T", [1, 9])
+def test_attend_values_of_any_size(code, size, T):
+    """Values at both ends of the scales' range: each cache's own size decides how its weights are held."""
+    m = Coded([200, 300, 70], T, code, (8, 2, 64), seed=21)
+    m.v[1] *= size
+    m.v[2][:, :48] *= size  # (the rest, and the new rows, as they are)
+    m.load()
+    q, k, v = _append_rows(m, T)
+    x = m.sess.attend(q, n_tokens=T)["x"]
+    m.grow(k, v, T)
+    torch.cuda.synchronize()
+    _check_attend(m, q, x, T, [200, 300, 70])
 
 
 @pytest.mark.parametrize("heads", [(4, 2, 64), (4, 4, 128), (16, 1, 64)])
