@@ -209,6 +209,7 @@ struct SampleBins {
   double rate;                    // log2(e) / T
   float top;                      // the highest score; -inf: no candidate
   float inv;                      // bins per unit of score
+  uint32_t done[4];               // work-groups that have listed their tokens: [0]
 };
 static_assert(sizeof(SampleBins) % 16 == 0, "cleared in 16-byte stores");
 struct SampleArgs {

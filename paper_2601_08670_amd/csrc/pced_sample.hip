@@ -4,7 +4,7 @@
 // w = exp((s - s_max) / T). Every filter keeps a prefix of that order, so that three numbers say what is
 // kept, and the token is where the running sum of the kept weights passes u times their total. No sort: the
 // order is first known by bins (k_sample_bins), which place each cut and the token within one bin or a few;
-// only those bins' tokens are listed (k_sample_list) and put in order (k_sample_token).
+// only those bins' tokens are listed and put in order (k_sample_list).
 // Weights are whole numbers, rint(w 2^shift) with shift + log2 V <= 62: their sums are exact, so they are the
 // same whatever the order of the atomics, and every comparison is made with the same numbers. A weight below
 // 2^-shift-1 (2^-45 at 150000 tokens) counts as 0. w comes from fp64: an error of 2^-24 in each of 10^5 weights
@@ -46,14 +46,16 @@ __device__ __forceinline__ float score_in(u64 key) {
 }
 __device__ __forceinline__ int token_in(u64 key) { return (int)~(uint32_t)key; }
 
-// The tokens of a block's part of a query's row, kTokens per thread at a time, the first of them
+// The tokens of a block's part of a query's row, N per thread at a time, the first of them
 // loaded before anything else: the settings, the slices' ranges and the bins come from other dies'
 // launches, 1 us away, and so do the scores.
-constexpr int kBinThreads = 512, kTokens = 10;
+constexpr int kBinThreads = 512, kListThreads = 1024;
+template <int NT, int N>
 struct Part {
+  static constexpr int kStep = NT * N;
   const float* x;
   int v0, v1;
-  float y[kTokens];
+  float y[N];
   __device__ __forceinline__ Part(const SampleArgs& a, int b) {
     x = a.scores + (size_t)b * a.V;
     const int per = ((a.V + (int)gridDim.x - 1) / (int)gridDim.x + 3) & ~3;
@@ -61,10 +63,10 @@ struct Part {
     v1 = min(a.V, v0 + per);
     load(v0);
   }
-  __device__ __forceinline__ int token(int v, int i) const { return v + i * kBinThreads + (int)threadIdx.x; }
+  __device__ __forceinline__ int token(int v, int i) const { return v + i * NT + (int)threadIdx.x; }
   __device__ __forceinline__ void load(int v) {
 #pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int t = token(v, i);
       y[i] = t < v1 ? x[t] : kNegInf;
     }
@@ -74,14 +76,14 @@ struct Part {
 // A block's part of a query's tokens into the bins: counted in LDS, then added to the query's. Bound: the way of
 // the settings and scores, the atomics' turns in LDS, the flush (16 queries of 151936 tokens: see launch_sample).
 __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
-  constexpr int NW = kBinThreads / 64;
+  constexpr int NW = kBinThreads / 64, N = 10;
   __shared__ u64 mass[kSampleBins];
   __shared__ uint32_t count[kSampleBins];
   __shared__ float red[2][NW];
   __shared__ u64 fm;
   __shared__ uint32_t fc;
   const int b = blockIdx.y, tid = threadIdx.x;
-  Part part(a, b);
+  Part<kBinThreads, N> part(a, b);
   const float T = a.temperature[b], mp = a.min_p ? a.min_p[b] : 0.f;
   float hi = kNegInf, lo = -kNegInf;
   for (int i = tid; i < a.nblk; i += kBinThreads) {
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
   uint32_t my_count = 0;
   for (int v = part.v0;;) {
 #pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
+    for (int i = 0; i < N; ++i) {
       const float y = part.y[i];
       if (!(y > kNegInf)) continue;
       const u64 w = weight_of(s, y, a.shift);
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
       if (w) atomicAdd(&mass[bin], w);
       if (has_floor && (double)y >= floor) { my_mass += w; ++my_count; }
     }
-    v += kTokens * kBinThreads;
+    v += part.kStep;
     if (v >= part.v1) break;
     part.load(v);
   }
@@ -300,47 +302,6 @@ struct Scan {
   }
 };
 
-// The tokens of the bins that hold a cut or the token, in any order.
-__global__ __launch_bounds__(kBinThreads) void k_sample_list(SampleArgs a) {
-  __shared__ Sums sums;
-  __shared__ uint32_t s_n, s_base;
-  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-  Part part(a, b);
-  Scan<kBinThreads> scan(a, b);
-  const Softmax s = scan.s;
-  const Cuts c = scan.cuts(a, sums);
-  if (c.none) return;
-  for (int v = part.v0; v < part.v1; v += kTokens * kBinThreads) {
-    if (v > part.v0) part.load(v);
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-    // a place in the list per wave and block: one global atomic, 1 us and more away
-    u64 m[kTokens];
-    uint32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
-      const float y = part.y[i];
-      m[i] = __ballot(y > kNegInf && wanted(c, bin_of(s, y)));
-      mine += (uint32_t)__popcll(m[i]);
-    }
-    uint32_t at = 0;
-    if (lane == 0 && mine) at = atomicAdd(&s_n, mine);
-    __syncthreads();
-    if (tid == 0 && s_n) s_base = atomicAdd(&a.bins[b].listed, s_n);
-    __syncthreads();
-    if (mine) {
-      at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + s_base;
-      u64* list = a.list + (size_t)b * a.V;
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i) {
-        if (m[i] >> lane & 1) list[at + __popcll(m[i] & (((u64)1 << lane) - 1))] = order_of(part.y[i], part.token(v, i));
-        at += (uint32_t)__popcll(m[i]);
-      }
-    }
-  }
-}
-
-constexpr int kTokenThreads = 1024;
 struct Found {
   u64 key;        // of the token at the cut
   u64 mass;       // of the tokens before it, in all
@@ -358,7 +319,7 @@ __device__ __forceinline__ Found search(const SampleArgs& a, const u64* list, co
   if (tid == 0) { s_key[0] = ~(u64)0; s_key[1] = 0; }
   __syncthreads();
   u64 all = ~(u64)0, any = 0;
-  for (int i = tid; i < n; i += kTokenThreads) {
+  for (int i = tid; i < n; i += kListThreads) {
     const u64 k = list[i];
     if (bin_of(s, score_in(k)) != bin) continue;
     all &= k;
@@ -371,9 +332,9 @@ __device__ __forceinline__ Found search(const SampleArgs& a, const u64* list, co
   Found f{s_key[0], sums.mass[bin], sums.count[bin]};
   for (int sh = 56; sh >= 0; sh -= 8) {
     if (!(differ >> sh & 255)) continue;  // (the digit is in f.key already)
-    for (int i = tid; i < 256; i += kTokenThreads) { hm[i] = 0; hc[i] = 0; }
+    for (int i = tid; i < 256; i += kListThreads) { hm[i] = 0; hc[i] = 0; }
     __syncthreads();
-    for (int i = tid; i < n; i += kTokenThreads) {
+    for (int i = tid; i < n; i += kListThreads) {
       const u64 k = list[i];
       const float y = score_in(k);
       if (bin_of(s, y) != bin) continue;
@@ -411,23 +372,20 @@ __device__ __forceinline__ Found search(const SampleArgs& a, const u64* list, co
   return f;
 }
 
-// One block per query: the exact cuts, and the token.
-__global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
-  __shared__ Sums sums;
+// The exact cuts, and the token, by one block, from the bins' sums, the cuts and the whole list.
+__device__ __forceinline__ void sample_token(const SampleArgs& a, int b, const Softmax& s, const Cuts& c, const Sums& sums) {
   __shared__ u64 key[kSampleList], weight[kSampleList];
   __shared__ uint16_t bins[kSampleList];
   __shared__ u64 s_mass_k, s_p_mass;
   __shared__ uint32_t s_p_count;
-  const int b = blockIdx.x, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const u64* list = a.list + (size_t)b * a.V;
-  const int n = (int)a.bins[b].listed;
+  const int n = (int)__hip_atomic_load(&a.bins[b].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const u64 entry = tid < a.V ? list[tid] : 0;  // (as far as it is one)
-  Scan<kTokenThreads> scan(a, b);
   if (a.beta_used) {
     const int e1 = a.query_exp0[b + 1];
-    for (int e = a.query_exp0[b] + tid; e < e1; e += kTokenThreads) a.beta_used[e] = a.beta[e];
+    for (int e = a.query_exp0[b] + tid; e < e1; e += kListThreads) a.beta_used[e] = a.beta[e];
   }
-  const Softmax s = scan.s;
   const bool few = n <= kSampleList;
   const float y = score_in(entry);
   int bin = -1;
@@ -439,7 +397,7 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
     weight[tid] = w;
     bins[tid] = (uint16_t)bin;
   }
-  const Cuts c = scan.cuts(a, sums);  // (ends with a barrier)
+  __syncthreads();
   auto write = [&](int v, float x, uint32_t kept, u64 mass) {  // one thread
     a.tokens_out[b] = v;
     a.prev_tok[b] = v;
@@ -452,7 +410,7 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
       a.logprob[b] = v >= 0 ? (float)((z - (log2((double)mass) - a.shift)) * 0.6931471805599453) : kNegInf;
     }
   };
-  if (c.none) {
+  if (c.none) {  // uniform
     if (tid == 0) write(-1, kNegInf, 0, 0);
     return;
   }
@@ -488,7 +446,7 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
   // The tokens before each: those of the bins before, and those of its bin with a higher key. 2^lg
   // neighbouring threads take a token together.
   int lg = 0;
-  while (lg < 6 && (n << (lg + 1)) <= kTokenThreads) ++lg;
+  while (lg < 6 && (n << (lg + 1)) <= kListThreads) ++lg;
   const int i = tid >> lg, step = 1 << lg;
   u64 before = 0, mine = 0;
   uint32_t rank = 0;
@@ -521,6 +479,55 @@ __global__ __launch_bounds__(kTokenThreads) void k_sample_token(SampleArgs a) {
   if (one && (double)before <= t && t < (double)(before + w)) write(token_in(mine), score_in(mine), count, mass);
 }
 
+// The tokens of the bins that hold a cut or the token into the query's list, in any order; the block that
+// is the last to do so finds the token.
+__global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
+  __shared__ Sums sums;
+  __shared__ uint32_t s_n, s_base, s_done;
+  constexpr int N = 5;
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  Part<kListThreads, N> part(a, b);
+  Scan<kListThreads> scan(a, b);
+  const Softmax s = scan.s;
+  const Cuts c = scan.cuts(a, sums);
+  for (int v = part.v0; v < part.v1 && !c.none; v += part.kStep) {
+    if (v > part.v0) part.load(v);
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    // a place in the list per wave and block: one global atomic, 1 us and more away
+    u64 m[N];
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = part.y[i];
+      m[i] = __ballot(y > kNegInf && wanted(c, bin_of(s, y)));
+      mine += (uint32_t)__popcll(m[i]);
+    }
+    uint32_t at = 0;
+    if (lane == 0 && mine) at = atomicAdd(&s_n, mine);
+    __syncthreads();
+    if (tid == 0 && s_n) s_base = atomicAdd(&a.bins[b].listed, s_n);
+    __syncthreads();
+    if (mine) {
+      at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + s_base;
+      u64* list = a.list + (size_t)b * a.V;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (m[i] >> lane & 1) list[at + __popcll(m[i] & (((u64)1 << lane) - 1))] = order_of(part.y[i], part.token(v, i));
+        at += (uint32_t)__popcll(m[i]);
+      }
+    }
+  }
+  // The block's entries (ordered by the barrier) are released, and the others' acquired, by one thread: as a launch
+  // of its own the rest took 2 us more for one query of 32000 tokens (10.5 us with it), as much for 16 of 151936;
+  // a fence by every thread writes the caches back once per wave: 20 us.
+  __syncthreads();
+  if (tid == 0) s_done = __hip_atomic_fetch_add(&a.bins[b].done[0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (s_done != gridDim.x - 1) return;
+  sample_token(a, b, s, c, sums);
+}
+
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs& a, int n_queries, int num_cus, hipStream_t st, const Timing* tm) {
@@ -531,9 +538,7 @@ hipError_t launch_sample(const SampleArgs& a, int n_queries, int num_cus, hipStr
   const dim3 grid((unsigned)std::max(1L, parts), n_queries);
   hipError_t e = go(k_sample_bins, grid, dim3(kBinThreads), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;
-  e = go(k_sample_list, grid, dim3(kBinThreads), 0, st, nullptr, nullptr, a);
-  if (e != hipSuccess) return e;
-  return go(k_sample_token, dim3(n_queries), dim3(kTokenThreads), 0, st, nullptr, t1(tm), a);
+  return go(k_sample_list, grid, dim3(kListThreads), 0, st, nullptr, t1(tm), a);
 }
 
 }  // namespace pced
