@@ -594,9 +594,9 @@ size_t pced_open_bytes(const pced_config* cfg, int32_t max_new);
  * fp32 contexts.
  */
 pced_status pced_load_codes(pced_ctx* ctx, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
-                       const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
-                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
-                       const float* beta, hipStream_t stream);
+                            const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
+                            const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                            const float* beta, hipStream_t stream);
 
 /*
  * pced_append into a cache in 8 bits: the rows go into the open pages, K rotated, and pages that
@@ -604,21 +604,21 @@ pced_status pced_load_codes(pced_ctx* ctx, int32_t n_queries, const int32_t* n_e
  * Arguments and errors are those of pced_append; CAPACITY also for n_tokens > max_new.
  */
 pced_status pced_append_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
-                         const pced_rope* rope, void* q_out, hipStream_t stream);
+                              const pced_rope* rope, void* q_out, hipStream_t stream);
 
 /*
  * Attention of the new tokens over a cache in 8 bits, after pced_append_codes of the same layers: row (s, i)
  * attends to tokens 0 .. len_s + i, those of the pages that were complete at len_s as codes * scale, the others as
- * they were appended. Sums and softmax in fp32; arguments and errors are those of pced_attend
- * without sel.
+ * they were appended. Sums and softmax in fp32; the weights that meet codes are rounded to fp16 (relative 2^-11), those
+ * that meet appended rows to two bf16 (2^-17). Arguments and errors are those of pced_attend without sel.
  */
 pced_status pced_attend_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q, void* x_out,
-                         hipStream_t stream);
+                              hipStream_t stream);
 
 /* pced_read_cache of a cache in 8 bits: codes * scale, rounded to bf16, and the rows behind the last
  * complete page as they are. */
 pced_status pced_read_codes(pced_ctx* ctx, int32_t seq, int32_t layer, int32_t start, int32_t count, void* k_out,
-                       void* v_out, hipStream_t stream);
+                            void* v_out, hipStream_t stream);
 
 /*
  * Adjustments of a query's logits before a token is chosen. All pointers are device

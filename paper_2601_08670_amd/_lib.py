@@ -344,8 +344,8 @@ class Context:
         self._keep = [list(src_k), list(src_v), k_pool, v_pool]
 
     def pced_load_codes(self, n_experts: Sequence[int], cache_len: Sequence[int], src_k, src_v, code, max_new, k_codes,
-                   v_codes, scales, k_open, v_open, relevance, gamma=2.5, beta=None, page_table=None,
-                   reserve_tokens=0, stream=None):
+                        v_codes, scales, k_open, v_open, relevance, gamma=2.5, beta=None, page_table=None,
+                        reserve_tokens=0, stream=None):
         buffers = (k_codes, v_codes, scales, k_open, v_open)
         cache = pced_cache8(CODES[code], max_new, *[_ptr(t) for t in buffers])
         self._load(self.lib.pced_load_codes, n_experts, cache_len, src_k, src_v, (ctypes.byref(cache),), relevance, gamma,
@@ -435,7 +435,7 @@ class Context:
 
     def pced_append_codes(self, layer, n_layers, n_tokens, rows: pced_rows, rope: Optional[pced_rope], q_out, stream=None):
         status = self.lib.pced_append_codes(self.handle, layer, n_layers, n_tokens, ctypes.byref(rows),
-                                       None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream))
+                                            None if rope is None else ctypes.byref(rope), _ptr(q_out), _stream(stream))
         if status:
             _check(status)
 
@@ -446,7 +446,7 @@ class Context:
 
     def pced_read_codes(self, seq, layer, start, count, k_out, v_out, stream=None):
         _check(self.lib.pced_read_codes(self.handle, int(seq), int(layer), int(start), int(count), k_out.data_ptr(),
-                                   v_out.data_ptr(), _stream(stream)))
+                                        v_out.data_ptr(), _stream(stream)))
 
     def pced_adjust_logits(self, logits, adjust: pced_adjust, out, stream=None):
         _check(self.lib.pced_adjust_logits(self.handle, _ptr(logits), ctypes.byref(adjust), _ptr(out),

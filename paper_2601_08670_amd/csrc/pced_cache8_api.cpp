@@ -67,9 +67,10 @@ int pages_of(const pced_ctx* c, int s, int n) { return (c->len[s] + n - 1) / kPa
 // The waves of a work-group hold kWavePages page numbers each.
 //
 // Parts. Splitting a sequence costs a second launch and the states' way through memory (about 4 us), so sequences of
-// up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.6 us, split 10.0), and so do longer ones where they keep
-// every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 45). Otherwise parts are as short as one
-// work-group per CU allows (5 x up to 250 pages: 48 pages 14.1 us, 32 pages 15.6, 96 pages 16.3), 32 pages at least.
+// up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.6 us, split 10.0), and so do longer ones
+// where they keep every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 45). Otherwise
+// parts are as short as one work-group per CU allows (5 x up to 250 pages: 48 pages 14.1 us, 32 pages 15.6, 96 pages
+// 16.3), 32 pages at least.
 bool plan8(const pced_ctx* c, const Attend8Args& a, int groups, Plan8* out) {
   const int most = 4 * kWavePages, S = c->S;
   int max_pages = 0;
@@ -122,9 +123,9 @@ size_t pced_open_bytes(const pced_config* cfg, int32_t max_new) {
 }
 
 pced_status pced_load_codes(pced_ctx* c, int32_t n_queries, const int32_t* n_experts, const int32_t* cache_len,
-                       const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
-                       const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
-                       const float* beta, hipStream_t st) {
+                            const void* const* src_k, const void* const* src_v, const pced_cache8* cache,
+                            const int32_t* page_table, int32_t reserve_tokens, const float* relevance, float gamma,
+                            const float* beta, hipStream_t st) {
   pced_status r = check_ctx(c, false);
   if (r == PCED_OK) r = check_cache8(c, cache);
   if (r != PCED_OK) return r;
@@ -146,7 +147,7 @@ pced_status pced_load_codes(pced_ctx* c, int32_t n_queries, const int32_t* n_exp
 }
 
 pced_status pced_append_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const pced_rows* rows,
-                         const pced_rope* rope, void* q_out, hipStream_t st) {
+                              const pced_rope* rope, void* q_out, hipStream_t st) {
   pced_status r = check_loaded8(c);
   if (r != PCED_OK) return r;
   AppendRowsArgs a{};
@@ -170,7 +171,7 @@ pced_status pced_append_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
 }
 
 pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q, void* x_out,
-                         hipStream_t st) {
+                              hipStream_t st) {
   pced_status r = check_loaded8(c);
   if (r == PCED_OK) r = check_layers(c, layer, n_layers, n_tokens);
   if (r == PCED_OK) r = check_new(c, n_tokens);
@@ -206,10 +207,11 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   a.gt = ceil_div(n_tokens, groups);
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cfg.head_dim));
   Plan8 p{};
-  if (!plan8(c, a, groups, &p)) return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
-  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 sequences of up to 128 pages, 8 heads:
-  // 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or parts are short
-  // (8 books of up to 8192 pages, in parts of 256: 217 us, eight waves 228).
+  if (!plan8(c, a, groups, &p))
+    return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
+  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 sequences of up
+  // to 128 pages, 8 heads: 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or
+  // parts are short (8 books of up to 8192 pages, in parts of 256: 217 us, eight waves 228).
   a.waves = a.tiles == 1 && p.parts == 1 && (double)c->S * groups * n_layers * cfg.n_kv_heads <= 2. * c->num_cus ? 8 : 4;
   char* ws = c->at<char>(c->lay.part_acc);
   a.part_acc = (float*)ws;
@@ -241,7 +243,7 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
 }
 
 pced_status pced_read_codes(pced_ctx* c, int32_t seq, int32_t layer, int32_t start, int32_t count, void* k_out, void* v_out,
-                       hipStream_t st) {
+                            hipStream_t st) {
   pced_status r = check_loaded8(c);
   if (r != PCED_OK) return r;
   if (seq < 0 || seq >= c->S) return fail(PCED_ERR_INVALID_ARG, "seq %d not in [0, %d)", seq, c->S);

@@ -1,5 +1,5 @@
 // 8-bit codes of cache blocks (16 tokens of one layer and kv-head, K or V): encoding a
-// bf16 tile, decoding to bf16. See pced_cache8 in pced.h for the definition.
+// bf16 tile, decoding to bf16 and fp16. See pced_cache8 in pced.h for the definition.
 //
 // A tile of codes keeps the bf16 tile's order (kswz, vswz): a lane's 16-byte units 2j and
 // 2j + 1 of the bf16 tile are the two halves of its unit j of codes, so that both operands of

@@ -2627,7 +2627,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 
   fuse_adjusted<VEC, SW, false>(a, d, nullptr, nullptr);
 }
 
-// The first launch of pced_sample: scores of every token (see fuse_adjusted). The query's bins start at zero.
+// The first launch of pced_sample: scores of every token (see fuse_adjusted; 16 queries of 17 rows of 151936 tokens, half
+// of them open: 48.7 us, where k_fuse_adjusted, which stores no scores, takes 46). The query's bins start at zero.
 template <bool VEC, int SW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(SW == 1024 ? (VEC ? 3 : 2) : 4))) void k_fuse_scores(FuseArgs a, AdjustArgs d, SampleArgs p) {
   uint4* z = (uint4*)(p.bins + blockIdx.x);

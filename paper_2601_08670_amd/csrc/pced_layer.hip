@@ -304,7 +304,8 @@ __device__ __forceinline__ void append_rows(const AppendRowsArgs& a, const Cache
           u32x4 u[B][NU], w[NU / 2];
 #pragma unroll
           for (int x = 0; x < B; ++x) {
-            const u32x4* in = (const u32x4*)((const uint16_t*)(z == 1 ? a.vpool : a.kpool) + (tile0 + min(h0 + 4 * x, Hkv - 1)) * tile) + (tid & 63);
+            const uint16_t* rows = (const uint16_t*)(z == 1 ? a.vpool : a.kpool) + (tile0 + min(h0 + 4 * x, Hkv - 1)) * tile;
+            const u32x4* in = (const u32x4*)rows + (tid & 63);
 #pragma unroll
             for (int i = 0; i < NU; ++i) u[x][i] = in[64 * i];
           }
@@ -312,7 +313,8 @@ __device__ __forceinline__ void append_rows(const AppendRowsArgs& a, const Cache
           for (int x = 0; x < B; ++x) {
             const int h = h0 + 4 * x;
             if (h >= Hkv) break;
-            u32x4* out = (u32x4*)((z == 1 ? c.v_codes : c.k_codes) + (((size_t)(a.layer0 + l) * c.max_pages + cp) * Hkv + h) * tile) + (tid & 63);
+            const size_t at = (((size_t)(a.layer0 + l) * c.max_pages + cp) * Hkv + h) * tile;
+            u32x4* out = (u32x4*)((z == 1 ? c.v_codes : c.k_codes) + at) + (tid & 63);
             uint32_t sc;
             encode_tile<CODE, NU>(u[x], w, &sc);
 #pragma unroll

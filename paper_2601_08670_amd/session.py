@@ -187,7 +187,7 @@ class PcedSession:
             self.ctx.pced_load_caches(n_experts, cache_len, src_k, src_v, self.k_pool, self.v_pool, relevance, **batch)
         else:
             self.ctx.pced_load_codes(n_experts, cache_len, src_k, src_v, self.kv8, self.max_new, self.k_codes, self.v_codes,
-                                self.scales, self.k_open, self.v_open, relevance, **batch)
+                                     self.scales, self.k_open, self.v_open, relevance, **batch)
         # (shapes of fuse_adjusted's outputs: empty_like takes a third less time than a shape and a type)
         self._out_like = self.out_buffers(("winner", "top1", "top2", "beta_used"))
 
