@@ -676,7 +676,8 @@ pced_status pced_fuse_adjusted(pced_ctx* ctx, const float* logits, int32_t refre
  *     min_p       of those, the tokens with S(v) >= s_max + T ln min_p, that is w(v) >= min_p (<= 0: all)
  *     the token is the first, in that order, at which the running sum of what is kept exceeds uniform[b] times
  *     its total
- * The first candidate is always kept. T <= 0 (or NaN) is Eq. 3's choice. Eq. 2 is in fp32; weights come from
+ * The first candidate is always kept. T <= 0 (or NaN) is Eq. 3's choice, T = inf
+ * counts as the largest fp32 number. Eq. 2 is in fp32; weights come from
  * fp64 and are summed exactly, as multiples of 2^-(62 - ceil(log2 V)) (those below half of that
  * weigh nothing, and are never drawn), so that equal inputs give equal outputs. uniform is cut to [0, 1 - 2^-24], NaN
  * counts as 0. All pointers are device memory, read when the call runs.

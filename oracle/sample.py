@@ -32,7 +32,7 @@ def sample(S, temperature, u, top_k=0, top_p=1.0, min_p=0.0):
     if not order:
         return -1, -math.inf, 0
     greedy = not temperature > 0
-    T = np.longdouble(1.0 if greedy else temperature)
+    T = np.longdouble(1.0 if greedy else min(temperature, np.finfo(np.float32).max))
     s = S[order].astype(np.longdouble)
     with np.errstate(invalid="ignore"):
         z = np.where(s == s[0], np.longdouble(0), (s - s[0]) / T)

@@ -18,6 +18,8 @@ namespace {
 
 constexpr int kSampleList = 1024;  // tokens that one block puts in order by comparing all pairs
 
+constexpr float kMaxT = 3.402823466e38f;  // an infinite temperature counts as this (inf times min_p's ln 1 is no number)
+
 typedef unsigned long long u64;
 
 // A query's softmax: how scores become bins and weights (SampleBins holds it for the later launches)
@@ -85,7 +87,8 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
   __shared__ uint32_t fc;
   const int b = blockIdx.y, tid = threadIdx.x;
   Part<kBinThreads, N> part(a, b);
-  const float T = a.temperature[b], mp = a.min_p ? a.min_p[b] : 0.f;
+  const float given = a.temperature[b], mp = a.min_p ? a.min_p[b] : 0.f;
+  const float T = given > kMaxT ? kMaxT : given;  // (NaN stays)
   float hi = kNegInf, lo = -kNegInf;
   for (int i = tid; i < a.nblk; i += kBinThreads) {
     const float2 x = *(const float2*)(a.part + 2 * ((size_t)b * a.nblk + i));
@@ -520,9 +523,10 @@ __global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
       }
     }
   }
-  // The block's entries (ordered by the barrier) are released, and the others' acquired, by one thread: as a launch
+  // The block's entries (each wave waits for its own to arrive, then the barrier) are released, and the others' acquired, by one thread: as a launch
   // of its own the rest took 2 us more for one query of 32000 tokens (10.5 us with it), as much for 16 of 151936;
   // a fence by every thread writes the caches back once per wave: 20 us.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (tid == 0) s_done = __hip_atomic_fetch_add(&a.bins[b].done[0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();

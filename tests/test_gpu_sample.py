@@ -137,6 +137,18 @@ def test_extreme_settings():
             c.run(u, temperature=1.0, **cut)
 
 
+def test_infinite_temperature():
+    """With min_p = 1 the tokens of the highest score stay: their weight alone reaches it."""
+    x = _logits(2, 3000, 30)
+    x[1] = np.round(x[1])
+    c = Case(3000, [1], beta=0.0, logits=x)
+    for T in (math.inf, float(np.finfo(np.float32).max)):
+        for min_p in (1e-30, 1.0, 2.0, math.inf):
+            for u in (0.0, 0.5, 0.99):
+                c.run(u, temperature=T, min_p=min_p)
+                c.run(u, temperature=T, min_p=min_p, top_k=2, top_p=0.9)
+
+
 @pytest.mark.parametrize("vocab", [700, 4096, 40000])
 def test_infinities_and_nan(vocab):
     """NaN and -inf are no candidates, +inf is above all; rows of nothing else; the largest numbers."""
