@@ -258,6 +258,25 @@ def test_attend(code, heads, layers, lens, T):
     _check_attend(m, q, x, T, lens)
 
 
+# more than 64 columns (q-heads of a kv-head times new tokens), which a work-group's waves divide
+COLUMNS = [
+    ((28, 4, 128), 1, [200, 17, 4], 24),       # one group, six waves, the last one with a tile and a half
+    ((4, 4, 64), 2, [31, 300], 65),            # one column past 64
+    ((4, 4, 128), 1, [70, 16], 200),           # two groups, several open pages before a column's own
+    ((12, 1, 64), 1, [90, 48, 1], 31),         # groups of 16 and 15 tokens
+    ((16, 1, 128), 2, [257 * 16 - 3, 9], 13),  # parts that end inside a chunk of pages
+    ((8, 2, 128), 1, [48, 1] * 9, 24),
+    ((20, 4, 64), 1, [15, 63], 193),
+    ((4, 1, 128), 1, [5000, 2], 20),
+]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("heads,layers,lens,T", COLUMNS)
+def test_attend_of_many_columns(code, heads, layers, lens, T):
+    test_attend(code, heads, layers, lens, T)
+
+
 @pytest.mark.parametrize("code", CODES)
 def test_attend_sharp_scores_and_uneven_blocks(code):
     """Scores far apart, blocks whose scales differ by twenty orders, zero queries."""
