@@ -385,7 +385,7 @@ __device__ __forceinline__ void sample_token(const SampleArgs& a, int b, const S
   const int tid = threadIdx.x;
   const u64* list = a.list + (size_t)b * a.V;
   const int n = (int)__hip_atomic_load(&a.bins[b].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const u64 entry = tid < a.V ? list[tid] : 0;  // (as far as it is one)
+  const u64 entry = tid < a.V ? __hip_atomic_load(&list[tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;  // (as far as it is one)
   if (a.beta_used) {
     const int e1 = a.query_exp0[b + 1];
     for (int e = a.query_exp0[b] + tid; e < e1; e += kListThreads) a.beta_used[e] = a.beta[e];
@@ -428,6 +428,7 @@ __device__ __forceinline__ void sample_token(const SampleArgs& a, int b, const S
   uint32_t count;
   u64 mass;
   if (!few) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");  // the list by plain loads from here on
     u64 mass_k = c.mass_k;
     if (c.k_open) {
       const Found f = search<0>(a, list, s, sums, n, c.bk, c.n_k, 0.0);
@@ -485,7 +486,7 @@ __device__ __forceinline__ void sample_token(const SampleArgs& a, int b, const S
 
 // The tokens of the bins that hold a cut or the token into the query's list, in any order; the block that
 // is the last to do so finds the token. Bound: one wait after the other (bins and scores, a place in the list, the blocks'
-// turns, the list; one query of 32000 tokens 10.3 us, 16 of 151936 16.6).
+// turns, the list; one query of 32000 tokens 10.2 us, 16 of 151936 14.5).
 __global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
   __shared__ Sums sums;
   __shared__ uint32_t s_n, s_base, s_done;
@@ -518,17 +519,19 @@ __global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
       u64* list = a.list + (size_t)b * a.V;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (m[i] >> lane & 1) list[at + __popcll(m[i] & (((u64)1 << lane) - 1))] = order_of(part.y[i], part.token(v, i));
+        if (m[i] >> lane & 1) 
+          __hip_atomic_store(&list[at + __popcll(m[i] & (((u64)1 << lane) - 1))], order_of(part.y[i], part.token(v, i)), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
         at += (uint32_t)__popcll(m[i]);
       }
     }
   }
-  // The block's entries (each wave waits for its own to arrive, then the barrier) are released, and the others' acquired, by one thread: as a launch
-  // of its own the rest took 2 us more for one query of 32000 tokens (10.5 us with it), as much for 16 of 151936;
-  // a fence by every thread writes the caches back once per wave: 20 us.
+  // The entries are stored and loaded at agent scope, past the dies' own L2s: each wave waits until its own have arrived,
+  // the barrier puts that before the count, and no cache is written back or emptied (by one thread's release and acquire
+  // 1.2 us more for one query, 2.7 for 16 of 151936; by every thread's 20). As a launch of its own the rest took another 2 us.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (tid == 0) s_done = __hip_atomic_fetch_add(&a.bins[b].done[0], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0) s_done = __hip_atomic_fetch_add(&a.bins[b].done[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (s_done != gridDim.x - 1) return;
   sample_token(a, b, s, c, sums);
