@@ -60,8 +60,8 @@ struct Part {
   float y[N];
   __device__ __forceinline__ Part(const SampleArgs& a, int b) {
     x = a.scores + (size_t)b * a.V;
-    const int per = ((a.V + (int)gridDim.x - 1) / (int)gridDim.x + 3) & ~3;
-    v0 = blockIdx.x * per;
+    const int per = ((a.V + (int)gridDim.y - 1) / (int)gridDim.y + 3) & ~3;
+    v0 = blockIdx.y * per;
     v1 = min(a.V, v0 + per);
     load(v0);
   }
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
   __shared__ float red[2][NW];
   __shared__ u64 fm;
   __shared__ uint32_t fc;
-  const int b = blockIdx.y, tid = threadIdx.x;
+  const int b = blockIdx.x, tid = threadIdx.x;
   Part<kBinThreads, N> part(a, b);
   const float given = a.temperature[b], mp = a.min_p ? a.min_p[b] : 0.f;
   const float T = given > kMaxT ? kMaxT : given;  // (NaN stays)
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kBinThreads) void k_sample_bins(SampleArgs a) {
   s.inv = span > 0.f ? (float)kSampleBins / span : 0.f;  // (NaN where the highest is infinite: 0)
   const double floor = has_floor ? (double)hi + (double)T * log((double)mp) : 0.0;
   SampleBins* q = a.bins + b;
-  if (blockIdx.x == 0 && tid == 0) {
+  if (blockIdx.y == 0 && tid == 0) {
     q->rate = s.rate;
     q->top = s.top;
     q->inv = s.inv;
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
   __shared__ Sums sums;
   __shared__ uint32_t s_n, s_base, s_done;
   constexpr int N = 5;
-  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   Part<kListThreads, N> part(a, b);
   Scan<kListThreads> scan(a, b);
   const Softmax s = scan.s;
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(kListThreads) void k_sample_list(SampleArgs a) {
   __syncthreads();
   if (tid == 0) s_done = __hip_atomic_fetch_add(&a.bins[b].done[0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  if (s_done != gridDim.x - 1) return;
+  if (s_done != gridDim.y - 1) return;
   sample_token(a, b, s, c, sums);
 }
 
@@ -544,7 +544,7 @@ hipError_t launch_sample(const SampleArgs& a, int n_queries, int num_cus, hipStr
   // the query's (k_sample_bins, 512 threads, 16 queries of 151936 tokens, us at 8 / 16 / 32 / 64 / 128 per query: 17.5 /
   // 14.2 / 15.6 / 21.6 / 34.2; one of 128256: 13.9 / 8.8 / 6.2 / 6.1 / 6.9)
   const long parts = std::min({(long)num_cus / n_queries, (a.V + 1023L) / 1024, 32L});
-  const dim3 grid((unsigned)std::max(1L, parts), n_queries);
+  const dim3 grid(n_queries, (unsigned)std::max(1L, parts));
   hipError_t e = go(k_sample_bins, grid, dim3(kBinThreads), 0, st, t0(tm), nullptr, a);
   if (e != hipSuccess) return e;
   return go(k_sample_list, grid, dim3(kListThreads), 0, st, nullptr, t1(tm), a);
