@@ -609,8 +609,9 @@ pced_status pced_append_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, in
 /*
  * Attention of the new tokens over a cache in 8 bits, after pced_append_codes of the same layers: row (s, i)
  * attends to tokens 0 .. len_s + i, those of the pages that were complete at len_s as codes * scale, the others as
- * they were appended. Sums and softmax in fp32; the weights that meet codes are rounded to fp16 (relative 2^-11), those
- * that meet appended rows to two bf16 (2^-17). Arguments and errors are those of pced_attend without sel.
+ * they were appended. Sums and softmax in fp32; a weight, times V's scale where it meets codes, is held as the sum of two
+ * bf16 (relative 2^-17), whatever the scales of other pages. As in fp32, sums of weights times values beyond 2^128
+ * are infinite. Arguments and errors are those of pced_attend without sel.
  */
 pced_status pced_attend_codes(pced_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n_tokens, const void* q, void* x_out,
                               hipStream_t stream);

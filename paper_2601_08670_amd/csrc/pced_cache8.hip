@@ -190,34 +190,24 @@ __device__ __forceinline__ void store_x4_bf16(void* x, size_t at, f32x4 o) {
   *(uint2*)((uint16_t*)x + at) = make_uint2(__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q));
 }
 
-__device__ __forceinline__ f16x8 join8h(uint2 a, uint2 b) { return __builtin_bit_cast(f16x8, u32x4{a.x, a.y, b.x, b.y}); }
 __device__ __forceinline__ float lane_f(float x, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
-// Powers of two that put the largest of a wave's V scales (a lane's is the upper half of `scale`) into [2^6, 2^7), and back
-struct VScale {
-  float down, up;
-  __device__ __forceinline__ explicit VScale(uint32_t scale) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) scale = max(scale, (uint32_t)__shfl_xor((int)scale, o));
-    const uint32_t e = max(__builtin_amdgcn_readfirstlane((int)scale) >> 23, 18);  // (scales are 2^-109 to 2^120)
-    down = __builtin_bit_cast(float, (260 - e) << 23);
-    up = __builtin_bit_cast(float, (e - 6) << 23);
-  }
-};
-
 __device__ __forceinline__ bf16x8 join8(uint2 a, uint2 b) { return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y}); }
+
+// Two pages' weights as the sum of two bf16 each: relative 2^-17, with fp32's exponent
+struct Weights8 {
+  bf16x8 hi, lo;
+};
 
 // A wave's part of an item: NC tiles of 16 columns (a column is a q-head of one of the group's new tokens), each
 // with an online softmax. As in k_attend the products are
 //   S^T[16 tok x 16 cols] = K[16 x D] Q^T,   O^T[D x 16 cols] += V^T[D x tok] P^T,
 // and the softmax's reference (in log2 units) moves only when a score exceeds it by 8, so that weights stay within
-// 2^8. Codes are exact in bf16 and in fp16: a page's K product is summed over codes and scaled behind; its softmax
-// weights are scaled by V's scale and rounded to fp16 (relative error 2^-11, an eighth of a bf16 result's own) before they
-// meet V's codes. Powers of two keep the weights in fp16's range: the largest V scale of the wave's pages counts as
-// 2^6 to 2^7, so that a weight is below 2^15, and what is lost below 2^-14 is at most 2^-31 of that page's V.
-// (As the sum of two bf16, with twice the products, a question of 24 tokens took 111 us instead of 94.)
+// 2^8. Codes are exact in bf16: a page's K product is summed over codes and scaled behind; its softmax weights are
+// scaled by V's scale and meet V's codes as the sum of two bf16, which hold any weight and scale of fp32 to 2^-17, however
+// far apart the pages' scales lie.
 template <int D, int NC>
 struct Columns {
   static constexpr int NU = D / 32, NJ = D / 16;  // 16-byte units of a bf16 tile per lane, 16-dim output blocks
@@ -252,12 +242,12 @@ struct Columns {
     }
   }
   // tile n's weights for two pages' scores (sums over codes), times V's scales
-  __device__ __forceinline__ f16x8 weights(int n, const f32x4 (&sc)[2], const float (&kc)[2], const float (&vs)[2]) {
+  __device__ __forceinline__ Weights8 weights(int n, const f32x4 (&sc)[2], const float (&kc)[2], const float (&vs)[2]) {
     float top = kNegInf;
 #pragma unroll
     for (int b = 0; b < 2; ++b) top = fmaxf(top, kc[b] * fmaxf(fmaxf(sc[b][0], sc[b][1]), fmaxf(sc[b][2], sc[b][3])));
     refer(n, top);
-    f16x8 w;
+    Weights8 w;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       float p[4];
@@ -265,7 +255,11 @@ struct Columns {
       for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][e], kc[b], -m[n]));
       lsum[n] += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[4 * b + e] = (_Float16)(p[e] * vs[b]);
+      for (int e = 0; e < 4; ++e) {
+        const float x = p[e] * vs[b];
+        w.hi[4 * b + e] = (__bf16)x;
+        w.lo[4 * b + e] = (__bf16)(x - (float)w.hi[4 * b + e]);
+      }
     }
     return w;
   }
@@ -407,8 +401,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 4))) 
   struct Regs {
     u32x4 k[2][NW], v[2][NW];
   };
-  const VScale vx(my_scale);
-  const float my_kc = bf2f(my_scale & 0xFFFFu) * a.scale_log2, my_vs = bf2f(my_scale >> 16) * vx.down;
+  // A wave's 1024 tokens with weights up to 2^8 and codes up to 448 reach 2^27 times the largest V scale: from 2^100 on
+  // all are held 2^18 smaller, so that the sums stay finite until the end.
+  const bool vast = __any((my_scale >> 16) >= 0x7180u);
+  const float my_kc = bf2f(my_scale & 0xFFFFu) * a.scale_log2, my_vs = bf2f(my_scale >> 16) * (vast ? 0x1p-18f : 1.f);
   const size_t tile = (size_t)kPage * D;
   auto load = [&](int u, Regs& r) __attribute__((always_inline)) {
 #pragma unroll
@@ -445,14 +441,17 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 4))) 
 #pragma unroll
       for (int n = 0; n < NC; ++n) sc[n][1] = f32x4{kNegInf, kNegInf, kNegInf, kNegInf};
     }
-    f16x8 wt[NC];
+    Weights8 wt[NC];
 #pragma unroll
     for (int n = 0; n < NC; ++n) wt[n] = C.weights(n, sc[n], kc, vs);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const f16x8 vv = join8h(decode4h<CODE>(r.v[0][j >> 2][j & 3]), decode4h<CODE>(r.v[1][j >> 2][j & 3]));
+      const bf16x8 vv = join8(decode4<CODE>(r.v[0][j >> 2][j & 3]), decode4<CODE>(r.v[1][j >> 2][j & 3]));
 #pragma unroll
-      for (int n = 0; n < NC; ++n) C.acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv, wt[n], C.acc[n][j], 0, 0, 0);
+      for (int n = 0; n < NC; ++n) {
+        C.acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, wt[n].hi, C.acc[n][j], 0, 0, 0);
+        C.acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, wt[n].lo, C.acc[n][j], 0, 0, 0);
+      }
     }
   };
   if (cnt > 2 * wave) {
@@ -473,7 +472,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 4))) 
     } else {
       work(i, ra);
     }
-    C.unscale(vx.up);
+    if (vast) C.unscale(0x1p18f);
   }
 #pragma unroll 1
   for (int p = max(c0, full) + wave; p < c1; p += W) C.open_page(a, it, p);

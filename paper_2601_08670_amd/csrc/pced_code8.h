@@ -1,5 +1,5 @@
 // 8-bit codes of cache blocks (16 tokens of one layer and kv-head, K or V): encoding a
-// bf16 tile, decoding to bf16 and fp16. See pced_cache8 in pced.h for the definition.
+// bf16 tile, decoding to bf16. See pced_cache8 in pced.h for the definition.
 //
 // A tile of codes keeps the bf16 tile's order (kswz, vswz): a lane's 16-byte units 2j and
 // 2j + 1 of the bf16 tile are the two halves of its unit j of codes, so that both operands of
@@ -54,9 +54,6 @@ __device__ __forceinline__ void encode_tile(const u32x4 (&u)[NU], u32x4 (&c)[NU 
   }
 }
 
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 // Four codes as four bf16 (exactly: at most 8 significant bits)
 template <int CODE>
 __device__ __forceinline__ uint2 decode4(uint32_t w) {
@@ -67,22 +64,6 @@ __device__ __forceinline__ uint2 decode4(uint32_t w) {
   } else {
     lo = bf16x2{(__bf16)(float)(int8_t)w, (__bf16)(float)(int8_t)(w >> 8)};
     hi = bf16x2{(__bf16)(float)(int8_t)(w >> 16), (__bf16)(float)(int8_t)(w >> 24)};
-  }
-  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-}
-
-// Four codes as four fp16 (exactly)
-template <int CODE>
-__device__ __forceinline__ uint2 decode4h(uint32_t w) {
-  f16x2 lo, hi;
-  if constexpr (CODE == kE4m3) {
-    lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
-    hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
-  } else {
-    const uint32_t u = w ^ 0x80808080u;  // code + 128, as the low byte of 1024 + it
-    const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
-    lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
-    hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
   }
   return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
