@@ -270,8 +270,9 @@ struct Columns {
       for (int j = 0; j < NJ; ++j) acc[n][j] *= f;
   }
   // A page behind the complete ones: a 16-bit tile, masked by each column's own position. V of tokens behind the
-  // group's last counts as 0 (unwritten rows hold anything); V of the group's own later tokens is written, but
-  // may be inf or NaN, whose product with a weight of 0 is not 0: the columns that see it get it one by one.
+  // group's last counts as 0 (unwritten rows hold anything). V that is inf or NaN is kept out of the products, where
+  // columns that do not see it would get 0 times it, and those that do its products with two bf16, one of which may be 0 or
+  // negative: the columns that see it get it one by one, times the whole weight.
   __device__ __forceinline__ void open_page(const Attend8Args& a, const Item8& it, int p) {
     const int lane = threadIdx.x & 63, quad = lane >> 4;
     const size_t at = (((size_t)(a.layer + it.l) * a.c.open_pages + it.s * a.c.ring + p % a.c.ring) * a.n_kv_heads + it.h) *
@@ -291,21 +292,19 @@ struct Columns {
         for (int u = 0; u < NU; ++u) { w[u][e >> 1] &= mask; w[u][2 + (e >> 1)] &= mask; }
       }
     };
-    const int first = it.len + it.tok0, end = first + it.nt - 1;
+    const int end = it.len + it.tok0 + it.nt - 1;
     keep(v, end);
-    // inf and NaN that not all of the group's tokens see: out, and in again where they are seen
+    // inf and NaN: out, and in again where they are seen
     bool odd = false;
-    if (kPage * p + kPage - 1 > first) {
 #pragma unroll
-      for (int u = 0; u < NU; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool bad = t0 + (e & 3) > first && (el16(v[u], e) & 0x7F80u) == 0x7F80u;
-          odd |= bad;
-          if (bad) v[u][e >> 1] &= ~(0xFFFFu << (16 * (e & 1)));
-        }
-      odd = __any(odd);
-    }
+      for (int e = 0; e < 8; ++e) {
+        const bool bad = (el16(v[u], e) & 0x7F80u) == 0x7F80u;
+        odd |= bad;
+        if (bad) v[u][e >> 1] &= ~(0xFFFFu << (16 * (e & 1)));
+      }
+    odd = __any(odd);
     float x[NC][4];
     s16x4 hi[NC], lo[NC];
 #pragma unroll
@@ -343,7 +342,7 @@ struct Columns {
     if (!odd) return;
     const uint16_t* tile = (const uint16_t*)a.c.v_open + at;
 #pragma unroll 1
-    for (int t = max(first + 1 - kPage * p, 0); t < kPage && kPage * p + t <= end; ++t) {
+    for (int t = 0; t < kPage && kPage * p + t <= end; ++t) {
       const int from = (lane & 15) + 16 * (t >> 2);  // where the token's weights are
 #pragma unroll
       for (int n = 0; n < NC; ++n) {

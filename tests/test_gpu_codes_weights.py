@@ -133,3 +133,47 @@ def test_sharp_scores_and_uneven_blocks_weighted(code):
     m.grow(k, v, 2)
     torch.cuda.synchronize()
     _check_weighted(m, q, x, 2, [400, 333])
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 4, 128), (16, 1, 64)])
+@pytest.mark.parametrize("T", [1, 5, 21])
+def test_infinite_values_behind_the_complete_pages(heads, T):
+    """Infinities and NaN in some dimensions of rows that columns see: the weighted sum's own, and its other dimensions as
+    if they were 0."""
+    lens = [37, 127, 11]
+    m = Coded(lens, T, "int8", heads, seed=34)
+    q, k, v = m.rows(T)
+    r = np.random.RandomState(35)
+
+    def bad(x):
+        """x with one in forty values replaced."""
+        what = torch.from_numpy(r.choice([np.inf, -np.inf, np.nan], tuple(x.shape), p=[0.45, 0.45, 0.1])).to(x)
+        return torch.where(torch.from_numpy(r.rand(*x.shape) < 1 / 40).to(x.device), what, x)
+
+    v = bad(v)
+    for s, n in enumerate(lens):
+        m.v[s][:, n // 16 * 16:] = bad(m.v[s][:, n // 16 * 16:])
+    rows, new = m.v, v
+    out = []
+    for clean in (False, True):
+        zero = (lambda x: torch.where(torch.isfinite(x), x, 0)) if clean else (lambda x: x)
+        m.v, v = [zero(x) for x in rows], zero(new)
+        m.load()
+        m.sess.append(None, k, v, n_tokens=T, rope=None)
+        out.append(_f64(m.sess.attend(q, n_tokens=T)["x"]).reshape(m.S * T, m.hq, m.d))
+    m.v, v, G = rows, new, m.hq // m.hkv
+    m.grow(k, v, T)
+    ks, vs = m.values(lens)
+    seen = set()
+    for s in range(m.S):
+        for i in range(T):
+            n = lens[s] + i + 1
+            for h in range(m.hkv):
+                at = (s * T + i, slice(h * G, (h + 1) * G))
+                with np.errstate(invalid="ignore"):
+                    want = C.attend(_f64(q[s * T + i, 0, h * G:(h + 1) * G]), ks[s][0, :n, h], vs[s][0, :n, h])
+                odd = ~np.isfinite(want)
+                assert np.array_equal(out[0][at][odd], want[odd], equal_nan=True), (s, i, h)
+                assert np.array_equal(out[0][at][~odd], out[1][at][~odd]), (s, i, h)
+                seen |= set(map(str, want[odd]))
+    assert seen == {"inf", "-inf", "nan"}
