@@ -117,7 +117,13 @@ Layout make_layout(const pced_config& c) {
   const size_t page_bytes = (size_t)kPage * c.n_kv_heads * c.head_dim * es;
   L.stage_bytes = align_up(2 * std::max(page_bytes, std::min(kLoadStage / 2, page_bytes * c.max_pages_per_seq * c.n_layers)));
   L.part_acc_bytes = align_up(std::max(L.part_slots * G * c.head_dim * 4, L.stage_bytes));
-  L.part_acc = take(L.part_acc_bytes);
+  // Sampling's bins and lists of tokens lie there too, for no call uses both (scores and experts: in the logits' place,
+  // which has a row for every query's amateur and one for its first expert). PCED_AGG_MAX only.
+  const size_t bins = c.aggregation == PCED_AGG_MAX ? align_up(B * sizeof(SampleBins)) : 0;
+  const size_t lists = bins ? B * c.vocab * 8 : 0;
+  L.part_acc = take(std::max(L.part_acc_bytes, bins + lists));
+  L.smp_bins = L.part_acc;
+  L.smp_list = L.part_acc + bins;
   L.part_ml = take(2 * L.part_slots * G * 2 * 4);
   L.x = take((size_t)L.rows_pad * c.hidden * es);
   L.logits = take(S * c.vocab * 4);
@@ -177,10 +183,6 @@ Layout make_layout(const pced_config& c) {
   L.pf_part_ml = take(2 * PR * c.n_kv_heads * kPrefillParts * G * 2 * 4);  // (bf16 states: pf_part_acc holds twice as many)
   L.pf_proj_elems = std::max(PR * max_cols, (size_t)kLmRowsPad * L.part_cols);
   L.pf_proj = take(L.pf_proj_elems * 4);
-  // sampling: a query's bins and its list of tokens (scores and experts: the logits' place, which has a
-  // row for every query's amateur and one for its first expert)
-  L.smp_bins = take(B * sizeof(SampleBins));
-  L.smp_list = take(B * c.vocab * 8);
   L.total = o;
   return L;
 }
