@@ -25,7 +25,7 @@ __device__ __forceinline__ TileUnit tile_unit(int n, int D) {
 // are the tiles of whole kv-heads). A wave that holds the units of a complete page's tiles
 // encodes them; the units of a page behind the last complete one go to its place as they are, slots past
 // the length zero-filled. Bound: HBM, 2 bytes read and 1 written per value (16 layers of 33 sequences, 8 heads of 128:
-// 760 us for 4.1 GB, 5.4 TB/s; a copy reaches 4.7).
+// 750 us for 4.0 GB, 5.4 TB/s; a copy reaches 4.9).
 template <int CODE, int D>
 __global__ __launch_bounds__(256) void k_load8(LoadArgs a, Cache8Args c) {
   constexpr int NU = D / 32, HPW = 8 / NU;  // a tile's units per lane, kv-heads per wave
@@ -207,7 +207,8 @@ struct Weights8 {
 // and the softmax's reference (in log2 units) moves only when a score exceeds it by 8, so that weights stay within
 // 2^8. Codes are exact in bf16: a page's K product is summed over codes and scaled behind; its softmax weights are
 // scaled by V's scale and meet V's codes as the sum of two bf16, which hold any weight and scale of fp32 to 2^-17, however
-// far apart the pages' scales lie.
+// far apart the pages' scales lie. (In fp16, which holds neither, with half the products of V: a question of 24 tokens
+// 85 us instead of 98, a token over 33 sequences 18.1 instead of 19.1, and no difference over longer caches.)
 template <int D, int NC>
 struct Columns {
   static constexpr int NU = D / 32, NJ = D / 16;  // 16-byte units of a bf16 tile per lane, 16-dim output blocks
@@ -368,10 +369,10 @@ struct Columns {
 // One block of W waves per (item, part of its pages), whose waves take pairs of pages in turn, all columns each, and
 // are merged in LDS. The pages that were complete before the call lie before every new token: no mask. A wave holds
 // the ids and scales of its pages one per lane and loads a pair of pages while it works on the one before.
-// Bound: HBM for a token (33 sequences, 16 layers of 8 heads: 232 us, 5.9 TB/s, as much as a plain read of memory
-// reaches; a layer of it 18.1 us, half of which is the launch, a first page and the merge of the waves; 8 books of
-// up to 131 072 tokens and their query: 216 us); for a question of 24 tokens (17 sequences of 5000, int8, 7 heads
-// each: 84 us) the instructions of decoding, softmax and products, which a SIMD issues one after another.
+// Bound: HBM for a token (33 sequences, 16 layers of 8 heads: 233 us, 5.9 TB/s, as much as a plain read of memory
+// reaches; a layer of it, int8, 19.1 us, half of which is the launch, a first page and the merge of the waves; 8 books of
+// up to 131 072 tokens and their query: 215 us); for a question of 24 tokens (17 sequences of 5000, int8, 7 heads
+// each: 98 us) the instructions of decoding, softmax and products, which a SIMD issues one after another.
 template <int CODE, int D, int NC, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 4))) void k_attend8(Attend8Args a) {
   constexpr int NU = D / 32, NW = D / 64, NJ = D / 16;  // 16-bit units, code units, 16-dim output blocks
@@ -576,6 +577,7 @@ __global__ __launch_bounds__(256) void k_attend8_merge(Attend8Args a) {
 // Tokens [start, start + count) of a sequence and layer as bf16 rows [count][Hkv][D]: codes times their
 // scale, rounded once; the tokens behind the complete pages as they are. A thread per 8 dims of a
 // token's K or V row: the units of a tile that hold them are 8 bytes (K) or 8 dims' single bytes (V).
+// Bound: V's single-byte loads (131072 tokens, 8 heads of 128: 399 us for 0.8 GB, 2.0 TB/s).
 __global__ __launch_bounds__(256) void k_read8(ReadCacheArgs a, Cache8Args c, int len) {
   const int Hkv = a.n_kv_heads, D = a.head_dim, oct = D / 8;
   const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x, per = (size_t)Hkv * oct;

@@ -66,11 +66,11 @@ int pages_of(const pced_ctx* c, int s, int n) { return (c->len[s] + n - 1) / kPa
 
 // The waves of a work-group hold kWavePages page numbers each.
 //
-// Parts. Splitting a sequence costs a second launch and the states' way through memory (about 4 us), so sequences of
-// up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.6 us, split 10.0), and so do longer ones
-// where they keep every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 45). Otherwise
-// parts are as short as one work-group per CU allows (5 x up to 250 pages: 48 pages 14.1 us, 32 pages 15.6, 96 pages
-// 16.3), 32 pages at least.
+// Parts. Splitting a sequence costs a second launch and the states' way through memory (about 2 us), so sequences of
+// up to 96 pages stay whole (4 x 63 pages and a query's own, 8 heads: 8.2 us, split 10.1), and so do longer ones
+// where they keep every CU busy as they are (33 x 188 pages on average: 40 us, in parts of 64 pages 44). Otherwise
+// parts are as short as one work-group per CU allows (5 x up to 250 pages, us in parts of 32 / 48 / 96 / 256 pages: 11.7 /
+// 12.2 / 14.8 / 18.8), 32 pages at least.
 bool plan8(const pced_ctx* c, const Attend8Args& a, int groups, Plan8* out) {
   const int most = 4 * kWavePages, S = c->S;
   int max_pages = 0;
@@ -199,9 +199,10 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   a.group = c->G;
   a.head_dim = cfg.head_dim;
   a.maxpps = cfg.max_pages_per_seq;
-  // Two tiles share a page's loads and decoding, one leaves room for more waves: 33 sequences of 82 pages on average,
-  // 8 heads, e4m3: 8 columns 17.0 us (two tiles 18.7), 32 columns 21.3 (21.8), 64 columns 33.2 (31.5), 256 columns 103 (92);
-  // int8, 256 columns 145 (120).
+  // Two tiles share a page's loads and decoding, one leaves room for more waves. 33 sequences of 82 pages on average,
+  // 8 heads of 128, e4m3: 8 columns 18.6 us (two tiles 21.3), 32 columns 22.0 (24.3), 64 columns 33.3 (35.0), 128 columns
+  // 56.4 (53.8), 256 columns 104 (95); int8, 64 columns 40.5 (40.3), 256 columns 132 (112). 64 columns of 5 x up to 250
+  // pages: e4m3 18.3 (17.2), int8 21.7 (18.8).
   a.tiles = n_tokens * c->G <= 32 ? 1 : 2;
   const int groups = ceil_div(n_tokens, 16 * a.tiles / c->G);  // per sequence
   a.gt = ceil_div(n_tokens, groups);
@@ -209,9 +210,10 @@ pced_status pced_attend_codes(pced_ctx* c, int32_t layer, int32_t n_layers, int3
   Plan8 p{};
   if (!plan8(c, a, groups, &p))
     return fail(PCED_ERR_CAPACITY, "a token group's partial states exceed the workspace");
-  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (33 sequences of up
-  // to 128 pages, 8 heads: 18.1 us, four waves 18.5; 5 x 63 pages: 8.6 and 9.4); four where work-groups abound or
-  // parts are short (8 books of up to 8192 pages, in parts of 256: 217 us, eight waves 228).
+  // Eight waves for a whole sequence where four would leave a CU's SIMDs with two each or less (e4m3, 8 heads of 128:
+  // 5 sequences of up to 63 pages 8.3 us, four waves 8.8; 33 of up to 128 pages 18.1 and 18.4, 64 of them 33.5 and 36.3;
+  // not where more work-groups than CUs have short sequences: 33 of up to 44 pages 11.2 and 9.3);
+  // four where work-groups abound or parts are short.
   a.waves = a.tiles == 1 && p.parts == 1 && (double)c->S * groups * n_layers * cfg.n_kv_heads <= 2. * c->num_cus ? 8 : 4;
   char* ws = c->at<char>(c->lay.part_acc);
   a.part_acc = (float*)ws;
