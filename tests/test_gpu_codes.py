@@ -258,13 +258,13 @@ def test_attend(code, heads, layers, lens, T):
     _check_attend(m, q, x, T, lens)
 
 
-# more than 64 columns (q-heads of a kv-head times new tokens), which a work-group's waves divide
+# more than 64 columns (q-heads of a kv-head times new tokens), which go in groups of whole tokens, at most 32 columns each
 COLUMNS = [
-    ((28, 4, 128), 1, [200, 17, 4], 24),       # one group, six waves, the last one with a tile and a half
-    ((4, 4, 64), 2, [31, 300], 65),            # one column past 64
-    ((4, 4, 128), 1, [70, 16], 200),           # two groups, several open pages before a column's own
-    ((12, 1, 64), 1, [90, 48, 1], 31),         # groups of 16 and 15 tokens
-    ((16, 1, 128), 2, [257 * 16 - 3, 9], 13),  # parts that end inside a chunk of pages
+    ((28, 4, 128), 1, [200, 17, 4], 24),       # six groups of four tokens, 28 columns
+    ((4, 4, 64), 2, [31, 300], 65),            # three groups of 22 and 21 tokens
+    ((4, 4, 128), 1, [70, 16], 200),           # seven groups, several open pages before a column's own
+    ((12, 1, 64), 1, [90, 48, 1], 31),         # fifteen groups of two tokens, one of one
+    ((16, 1, 128), 2, [257 * 16 - 3, 9], 13),  # parts of 32 pages, the last of two
     ((8, 2, 128), 1, [48, 1] * 9, 24),
     ((20, 4, 64), 1, [15, 63], 193),
     ((4, 1, 128), 1, [5000, 2], 20),
